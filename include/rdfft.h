@@ -212,6 +212,168 @@ RDFFT_API int bca_backward_batched(int count, const void *const *x, const void *
                                    const bca_grads_t *grads, int64_t d_in, int64_t d_out, int64_t p, int64_t tokens,
                                    rdfft_dtype_t dtype, rdfft_stream_t stream);
 
+/* -------------------------------------------------------------------------------------------
+ * The operators around the adapter in a fine-tuned layer: activations kept for the backward pass
+ * in 8 bits, layer norm, and the dense product that the adapter is added to.
+ *
+ * They share the conventions above, with these differences:
+ * - Tensors of `dtype` are rows of consecutive elements with a row stride of their own (in
+ *   elements, at least the row's length), and start at any multiple of the element's size; rows that
+ *   start at multiples of 16 bytes are the fast case.  Nothing outside a row's elements is
+ *   read or written.
+ * - A checkpoint is contiguous: codes [rows][n] and scales [rows][ceil(n/32)].
+ * - A call that needs scratch memory takes it from the caller (16-byte aligned; its size from the
+ *   matching _workspace call).  Its contents need not be kept between calls.
+ * - Sums, means and variances are float32.  Results do not depend on the order in which the
+ *   device executes (no atomics).
+ * - An output overlaps no input unless said otherwise -> RDFFT_EINVAL.
+ */
+
+/*
+ * The 8-bit format.  32 consecutive values of a row (the last block of a row may be short) share a power of
+ * two 2^e, the least one with max|x| <= 127 * 2^e and e >= -127.  A value is held as the int8 code
+ * rint(x / 2^e) (half to even) and stands for code * 2^e; the block's scale is the byte e + 127.
+ * A block with an infinity or a NaN has scale byte 255, codes 0, and stands for NaN throughout.
+ * The error of a value is at most 2^(e-1), 1/126 of the block's largest |x| (down to 2^-121).
+ */
+typedef struct {
+  int8_t *codes;
+  uint8_t *scales;
+} act8_t;
+
+/* act8_quantize / act8_dequantize -- rows x n values into their checkpoint, and back (the values
+ * that it stands for, rounded to dtype).  n >= 1; rows == 0 is a no-op. */
+RDFFT_API int act8_quantize(const void *x, int64_t ldx, const act8_t *to, int64_t rows, int64_t n, rdfft_dtype_t dtype,
+                            rdfft_stream_t stream);
+RDFFT_API int act8_dequantize(const act8_t *from, void *out, int64_t ldo, int64_t rows, int64_t n, rdfft_dtype_t dtype,
+                              rdfft_stream_t stream);
+
+/*
+ * layer_norm_forward -- per row, u = x (+ residual), y = (u - mean(u)) * rstd * weight + bias with
+ * rstd = (mean((u - mean(u))^2) + eps)^(-1/2).  1 <= n <= 16384 (more -> RDFFT_EUNSUPPORTED).
+ *   residual   may be null.  weight, bias: float32 [n]; bias may be null.
+ *   y          may be x or residual itself (same pointer and stride).
+ *   mean, rstd float32 [rows], written; either may be null.
+ *   checkpoint of u (of the float32 sum where there is a residual), written; codes null: none.
+ *   eps        >= 0.
+ */
+typedef struct {
+  const void *x;
+  int64_t ldx;
+  const void *residual;
+  int64_t ldr;
+  const float *weight;
+  const float *bias;
+  void *y;
+  int64_t ldy;
+  float *mean;
+  float *rstd;
+  act8_t checkpoint;
+} layer_norm_forward_t;
+RDFFT_API int layer_norm_forward(const layer_norm_forward_t *a, int64_t rows, int64_t n, float eps, rdfft_dtype_t dtype,
+                                 rdfft_stream_t stream);
+
+/*
+ * layer_norm_backward -- with xh = (u - mean) * rstd, g = dy * weight:
+ *   dx = rstd * (g - mean(g) - xh * mean(g * xh)), the gradient of x and of residual,
+ *   dweight = sum over rows of dy * xh,  dbias = sum over rows of dy  (float32 [n], overwritten).
+ *   u          x (+ residual), or with x null (and residual null) what the checkpoint stands for.
+ *   mean, rstd as layer_norm_forward left them.
+ *   dx         may be dy itself (same pointer and stride).
+ * rows == 0 writes zeros into dweight and dbias.
+ */
+typedef struct {
+  const void *dy;
+  int64_t ldg;
+  const void *x;
+  int64_t ldx;
+  const void *residual;
+  int64_t ldr;
+  act8_t checkpoint;
+  const float *weight;
+  const float *mean;
+  const float *rstd;
+  void *dx;
+  int64_t ldd;
+  float *dweight;
+  float *dbias;
+  void *workspace;
+  int64_t workspace_bytes;
+} layer_norm_backward_t;
+RDFFT_API int64_t layer_norm_backward_workspace(int64_t rows, int64_t n); /* bytes, or a negative rdfft_status_t */
+RDFFT_API int layer_norm_backward(const layer_norm_backward_t *a, int64_t rows, int64_t n, rdfft_dtype_t dtype,
+                                  rdfft_stream_t stream);
+
+typedef enum {
+  RDFFT_ACT_NONE = 0,
+  RDFFT_ACT_RELU = 1,
+  RDFFT_ACT_GELU = 2, /* z * Phi(z), Phi the normal distribution function */
+  RDFFT_ACT_SILU = 3  /* z / (1 + exp(-z)) */
+} rdfft_activation_t;
+
+/*
+ * linear_forward -- per token z = W x + bias, y = act(z) + residual.
+ *   x [tokens][d_in], w [d_out][d_in], bias [d_out] or null, residual [tokens][d_out] or null, all in dtype.
+ *   y          [tokens][d_out]; may be residual itself (same pointer and stride).
+ *   checkpoint of z (of its float32 value), written, for linear_backward; codes null: none.
+ * Products of dtype's values are summed in float32 (matrix cores); y is rounded once.
+ * d_in, d_out >= 1, at most 2^20, strides at most 2^21, tokens at most 2^22 (more -> RDFFT_EUNSUPPORTED).
+ */
+typedef struct {
+  const void *x;
+  int64_t ldx;
+  const void *w;
+  int64_t ldw;
+  const void *bias;
+  const void *residual;
+  int64_t ldr;
+  void *y;
+  int64_t ldy;
+  act8_t checkpoint;
+  void *workspace;
+  int64_t workspace_bytes;
+} linear_forward_t;
+/* bytes (0: none is needed), or a negative rdfft_status_t */
+RDFFT_API int64_t linear_forward_workspace(int64_t d_in, int64_t d_out, int64_t tokens, rdfft_dtype_t dtype);
+RDFFT_API int linear_forward(const linear_forward_t *a, int64_t d_in, int64_t d_out, int64_t tokens,
+                             rdfft_activation_t act, rdfft_dtype_t dtype, rdfft_stream_t stream);
+
+/*
+ * linear_backward -- with dz = dy * act'(z), z being what the checkpoint stands for:
+ *   dx = dz W (+ add),  dw = dz^T x,  db = sum over tokens of dz.
+ * Each of dx, dw, db is computed if its pointer is not null.  (The residual's gradient is dy.)
+ *   checkpoint unused (and may be null) for RDFFT_ACT_NONE.
+ *   x          needed for dw only, w for dx only.
+ *   add        [tokens][d_in] or null: a gradient that reaches x another way; dx may be add itself
+ *              (same pointer and stride).
+ *   dw [d_out][d_in], db [d_out] in dtype, overwritten.
+ * As an operand of the products dz is rounded to dtype (act != RDFFT_ACT_NONE); db sums the float32 dz.
+ * tokens == 0 writes zeros into dw and db.
+ */
+typedef struct {
+  const void *dy;
+  int64_t ldg;
+  act8_t checkpoint;
+  const void *x;
+  int64_t ldx;
+  const void *w;
+  int64_t ldw;
+  const void *add;
+  int64_t lda;
+  void *dx;
+  int64_t ldd;
+  void *dw;
+  int64_t lddw;
+  void *db;
+  void *workspace;
+  int64_t workspace_bytes;
+} linear_backward_t;
+/* for the gradients that are wanted (nonzero) */
+RDFFT_API int64_t linear_backward_workspace(int64_t d_in, int64_t d_out, int64_t tokens, int dx, int dw, int db,
+                                            rdfft_activation_t act, rdfft_dtype_t dtype);
+RDFFT_API int linear_backward(const linear_backward_t *a, int64_t d_in, int64_t d_out, int64_t tokens,
+                              rdfft_activation_t act, rdfft_dtype_t dtype, rdfft_stream_t stream);
+
 /* Uploads the twiddle table to the current device (synchronously) if not done yet.
  * Optional: every entry point does it on first use.  Returns RDFFT_OK or RDFFT_EDEVICE. */
 RDFFT_API int rdfft_init(void);

@@ -15,6 +15,11 @@ RDFFT_F32 = 0
 RDFFT_BF16 = 1
 RDFFT_F16 = 2
 
+RDFFT_ACT_NONE = 0
+RDFFT_ACT_RELU = 1
+RDFFT_ACT_GELU = 2
+RDFFT_ACT_SILU = 3
+
 RDFFT_OK = 0
 RDFFT_EINVAL = -1
 RDFFT_EUNSUPPORTED = -2
@@ -34,6 +39,15 @@ EXPORTS = (
     "bca_backward_keep",
     "bca_forward_batched",
     "bca_backward_batched",
+    "act8_quantize",
+    "act8_dequantize",
+    "layer_norm_forward",
+    "layer_norm_backward_workspace",
+    "layer_norm_backward",
+    "linear_forward_workspace",
+    "linear_forward",
+    "linear_backward_workspace",
+    "linear_backward",
     "rdfft_init",
     "rdfft_table_bytes",
     "rdfft_status_string",
@@ -44,6 +58,44 @@ class BcaGrads(ctypes.Structure):
     """bca_grads_t"""
 
     _fields_ = [("dx", ctypes.c_void_p), ("dc", ctypes.c_void_p)]
+
+
+class Act8(ctypes.Structure):
+    """act8_t"""
+
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+
+
+def _fields(text):
+    """Pointers and int64 sizes (those named ld* and *_bytes) of a struct, in order."""
+    kinds = {"checkpoint": Act8}
+    return [(n, kinds.get(n, ctypes.c_int64 if n.startswith("ld") or n.endswith("_bytes") else ctypes.c_void_p))
+            for n in text.split()]
+
+
+class LayerNormForward(ctypes.Structure):
+    """layer_norm_forward_t"""
+
+    _fields_ = _fields("x ldx residual ldr weight bias y ldy mean rstd checkpoint")
+
+
+class LayerNormBackward(ctypes.Structure):
+    """layer_norm_backward_t"""
+
+    _fields_ = _fields("dy ldg x ldx residual ldr checkpoint weight mean rstd dx ldd dweight dbias workspace "
+                       "workspace_bytes")
+
+
+class LinearForward(ctypes.Structure):
+    """linear_forward_t"""
+
+    _fields_ = _fields("x ldx w ldw bias residual ldr y ldy checkpoint workspace workspace_bytes")
+
+
+class LinearBackward(ctypes.Structure):
+    """linear_backward_t"""
+
+    _fields_ = _fields("dy ldg checkpoint x ldx w ldw add lda dx ldd dw lddw db workspace workspace_bytes")
 
 
 _lib = None
@@ -71,6 +123,21 @@ def load() -> ctypes.CDLL:
     lib.bca_forward_batched.restype = i32
     lib.bca_backward_batched.argtypes = [i32, pp, pp, pp, ctypes.POINTER(BcaGrads), i64, i64, i64, i64, i32, vp]
     lib.bca_backward_batched.restype = i32
+    f32 = ctypes.c_float
+    lib.act8_quantize.argtypes = [vp, i64, ctypes.POINTER(Act8), i64, i64, i32, vp]
+    lib.act8_dequantize.argtypes = [ctypes.POINTER(Act8), vp, i64, i64, i64, i32, vp]
+    lib.layer_norm_forward.argtypes = [ctypes.POINTER(LayerNormForward), i64, i64, f32, i32, vp]
+    lib.layer_norm_backward.argtypes = [ctypes.POINTER(LayerNormBackward), i64, i64, i32, vp]
+    lib.linear_forward.argtypes = [ctypes.POINTER(LinearForward), i64, i64, i64, i32, i32, vp]
+    lib.linear_backward.argtypes = [ctypes.POINTER(LinearBackward), i64, i64, i64, i32, i32, vp]
+    for name in ("act8_quantize", "act8_dequantize", "layer_norm_forward", "layer_norm_backward", "linear_forward",
+                 "linear_backward"):
+        getattr(lib, name).restype = i32
+    lib.layer_norm_backward_workspace.argtypes = [i64, i64]
+    lib.linear_forward_workspace.argtypes = [i64, i64, i64, i32]
+    lib.linear_backward_workspace.argtypes = [i64, i64, i64, i32, i32, i32, i32, i32]
+    for name in ("layer_norm_backward_workspace", "linear_forward_workspace", "linear_backward_workspace"):
+        getattr(lib, name).restype = i64
     lib.rdfft_init.argtypes = []
     lib.rdfft_init.restype = i32
     lib.rdfft_table_bytes.argtypes = []

@@ -239,6 +239,264 @@ def bca_backward_batched(xs, c_spectras, gys, dxs, dcs):
     return dxs, dcs
 
 
+# -------------------------------------------------------------------------------------------------
+# The operators around the adapter.  Tensors of the storage type are two-dimensional with
+# consecutive elements in a row; a row stride of their own (a slice of wider rows) is fine.  A checkpoint is the
+# pair (codes, scales): int8 (rows, n) and uint8 (rows, ceil(n / 32)).
+
+CHECKPOINT_BLOCK = 32
+ACTIVATIONS = {"none": _lib.RDFFT_ACT_NONE, "relu": _lib.RDFFT_ACT_RELU, "gelu": _lib.RDFFT_ACT_GELU,
+               "silu": _lib.RDFFT_ACT_SILU}
+
+
+def _rows(t: torch.Tensor, name: str, like: torch.Tensor, shape) -> tuple[int, int]:
+    """(pointer, row stride) of a (rows, n) tensor of ``like``'s type and device."""
+    if t.dtype != like.dtype:
+        raise TypeError(f"{name} is {t.dtype}, expected {like.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if not t.is_cuda or t.get_device() != like.get_device():
+        raise ValueError(f"{name} must be a device tensor on {like.device}, is on {t.device}")
+    rows, n = shape
+    s0, s1 = t.stride()
+    if (s1 != 1 and n > 1) or (s0 < n and rows > 1):
+        raise ValueError(f"{name} must have consecutive elements in a row, and rows apart, got strides {t.stride()}")
+    return t.data_ptr(), max(s0, n)
+
+
+def _vector(t: torch.Tensor, name: str, like: torch.Tensor, n: int, dtype: torch.dtype) -> int:
+    if t.dtype != dtype:
+        raise TypeError(f"{name} is {t.dtype}, expected {dtype}")
+    if t.shape != (n,):
+        raise ValueError(f"{name} must have shape ({n},), got {tuple(t.shape)}")
+    if not t.is_cuda or t.get_device() != like.get_device():
+        raise ValueError(f"{name} must be a device tensor on {like.device}, is on {t.device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _matrix(t: torch.Tensor, name: str) -> tuple[int, int]:
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be two-dimensional, got shape {tuple(t.shape)}")
+    return t.shape
+
+
+def _held(checkpoint, like: torch.Tensor, rows: int, n: int):
+    """act8_t of a (codes, scales) pair for (rows, n) values, or of none."""
+    if checkpoint is None:
+        return _lib.Act8(None, None)
+    codes, scales = checkpoint
+    for name, t, dtype, shape in (("codes", codes, torch.int8, (rows, n)),
+                                  ("scales", scales, torch.uint8, (rows, -(-n // CHECKPOINT_BLOCK)))):
+        if t.dtype != dtype:
+            raise TypeError(f"a checkpoint's {name} are {dtype}, got {t.dtype}")
+        if t.shape != shape:
+            raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
+        if not t.is_cuda or t.get_device() != like.get_device():
+            raise ValueError(f"{name} must be a device tensor on {like.device}, is on {t.device}")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+    return _lib.Act8(codes.data_ptr(), scales.data_ptr())
+
+
+def _scratch(need: int, given, like: torch.Tensor, what: str):
+    """(tensor to keep alive, pointer, bytes) of a workspace; one is allocated if none is given."""
+    if need < 0:
+        _check(need, what)
+    if need == 0:
+        return None, None, 0
+    if given is None:
+        given = torch.empty(need, dtype=torch.uint8, device=like.device)
+    elif not given.is_cuda or given.get_device() != like.get_device() or not given.is_contiguous():
+        raise ValueError(f"the workspace must be a contiguous tensor on {like.device}")
+    size = given.numel() * given.element_size()
+    if size < need:
+        raise ValueError(f"the workspace has {size} bytes, {what} needs {need}")
+    return given, given.data_ptr(), size
+
+
+def checkpoint_like(x: torch.Tensor) -> tuple[torch.Tensor, torch.Tensor]:
+    """An empty 8-bit checkpoint (codes, scales) for the values of a (rows, n) tensor."""
+    rows, n = _matrix(x, "x")
+    return (torch.empty((rows, n), dtype=torch.int8, device=x.device),
+            torch.empty((rows, -(-n // CHECKPOINT_BLOCK)), dtype=torch.uint8, device=x.device))
+
+
+def act8_quantize(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor):
+    """The 8-bit checkpoint of x (rows, n): int8 codes, and one scale byte for 32 values of a row."""
+    rows, n = _matrix(x, "x")
+    code = _code(x)
+    p, ld = _rows(x, "x", x, x.shape)
+    held = _held((codes, scales), x, rows, n)
+    _check(_lib.load().act8_quantize(p, ld, ctypes.byref(held), rows, n, code, _stream(x)), "act8_quantize")
+    return codes, scales
+
+
+def act8_dequantize(codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor) -> torch.Tensor:
+    """What a checkpoint stands for, in ``out``'s type (exact in float32 and bfloat16)."""
+    rows, n = _matrix(out, "out")
+    code = _code(out)
+    p, ld = _rows(out, "out", out, out.shape)
+    held = _held((codes, scales), out, rows, n)
+    _check(_lib.load().act8_dequantize(ctypes.byref(held), p, ld, rows, n, code, _stream(out)), "act8_dequantize")
+    return out
+
+
+def layer_norm_forward(x, weight, bias, y, *, residual=None, mean=None, rstd=None, checkpoint=None, eps=1e-5):
+    """y = norm(x (+ residual)) * weight (+ bias) per row; weight, bias, mean and rstd are float32.
+
+    ``mean`` and ``rstd`` (rows,) and ``checkpoint``, of the norm's input, are written if given.
+    ``y`` may be ``x`` or ``residual``.
+    """
+    rows, n = shape = _matrix(x, "x")
+    code = _code(x)
+    a = _lib.LayerNormForward()
+    a.x, a.ldx = _rows(x, "x", x, shape)
+    if residual is not None:
+        a.residual, a.ldr = _rows(residual, "residual", x, shape)
+    a.weight = _vector(weight, "weight", x, n, torch.float32)
+    if bias is not None:
+        a.bias = _vector(bias, "bias", x, n, torch.float32)
+    a.y, a.ldy = _rows(y, "y", x, shape)
+    if mean is not None:
+        a.mean = _vector(mean, "mean", x, rows, torch.float32)
+    if rstd is not None:
+        a.rstd = _vector(rstd, "rstd", x, rows, torch.float32)
+    a.checkpoint = _held(checkpoint, x, rows, n)
+    st = _lib.load().layer_norm_forward(ctypes.byref(a), rows, n, eps, code, _stream(x))
+    _check(st, "layer_norm_forward")
+    return y
+
+
+def layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, *, residual=None, workspace=None):
+    """Writes the norm's gradients: dx (of x and of the residual alike), and float32 dweight and dbias.
+
+    ``x`` is the forward's x, or the checkpoint (codes, scales) of the norm's input; ``dx`` may be ``dy``.
+    ``workspace``: ``layer_norm_backward_workspace(rows, n)`` bytes, allocated if not given.
+    """
+    rows, n = shape = _matrix(dy, "dy")
+    code = _code(dy)
+    a = _lib.LayerNormBackward()
+    a.dy, a.ldg = _rows(dy, "dy", dy, shape)
+    if isinstance(x, torch.Tensor):
+        a.x, a.ldx = _rows(x, "x", dy, shape)
+        if residual is not None:
+            a.residual, a.ldr = _rows(residual, "residual", dy, shape)
+    else:
+        if residual is not None:
+            raise ValueError("a checkpoint is of the norm's input, residual included")
+        a.checkpoint = _held(x, dy, rows, n)
+    a.weight = _vector(weight, "weight", dy, n, torch.float32)
+    a.mean = _vector(mean, "mean", dy, rows, torch.float32)
+    a.rstd = _vector(rstd, "rstd", dy, rows, torch.float32)
+    a.dx, a.ldd = _rows(dx, "dx", dy, shape)
+    a.dweight = _vector(dweight, "dweight", dy, n, torch.float32)
+    a.dbias = _vector(dbias, "dbias", dy, n, torch.float32)
+    lib = _lib.load()
+    _keep, a.workspace, a.workspace_bytes = _scratch(lib.layer_norm_backward_workspace(rows, n), workspace, dy,
+                                                     "layer_norm_backward")
+    _check(lib.layer_norm_backward(ctypes.byref(a), rows, n, code, _stream(dy)), "layer_norm_backward")
+    return dx, dweight, dbias
+
+
+def layer_norm_backward_workspace(rows: int, n: int) -> int:
+    need = int(_lib.load().layer_norm_backward_workspace(rows, n))
+    if need < 0:
+        _check(need, "layer_norm_backward_workspace")
+    return need
+
+
+def _activation(name: str) -> int:
+    act = ACTIVATIONS.get(name)
+    if act is None:
+        raise ValueError(f"activation must be one of {', '.join(ACTIVATIONS)}, got {name!r}")
+    return act
+
+
+def linear_forward(x, w, y, *, bias=None, activation="none", residual=None, checkpoint=None, workspace=None):
+    """y = act(x w^T + bias) + residual, with x (tokens, d_in), w (d_out, d_in) and the rest of one storage type.
+
+    ``checkpoint``, of the pre-activation, is written if given.  ``y`` may be ``residual``.
+    ``workspace``: ``linear_forward_workspace(...)`` bytes, allocated if not given.
+    """
+    tokens, d_in = _matrix(x, "x")
+    d_out = _matrix(w, "w")[0]
+    code, act = _code(x), _activation(activation)
+    a = _lib.LinearForward()
+    a.x, a.ldx = _rows(x, "x", x, (tokens, d_in))
+    a.w, a.ldw = _rows(w, "w", x, (d_out, d_in))
+    if bias is not None:
+        a.bias = _vector(bias, "bias", x, d_out, x.dtype)
+    if residual is not None:
+        a.residual, a.ldr = _rows(residual, "residual", x, (tokens, d_out))
+    a.y, a.ldy = _rows(y, "y", x, (tokens, d_out))
+    a.checkpoint = _held(checkpoint, x, tokens, d_out)
+    lib = _lib.load()
+    _keep, a.workspace, a.workspace_bytes = _scratch(lib.linear_forward_workspace(d_in, d_out, tokens, code), workspace,
+                                                     x, "linear_forward")
+    _check(lib.linear_forward(ctypes.byref(a), d_in, d_out, tokens, act, code, _stream(x)), "linear_forward")
+    return y
+
+
+def linear_forward_workspace(d_in: int, d_out: int, tokens: int, dtype: torch.dtype) -> int:
+    need = int(_lib.load().linear_forward_workspace(d_in, d_out, tokens, _CODES[dtype]))
+    if need < 0:
+        _check(need, "linear_forward_workspace")
+    return need
+
+
+def linear_backward(dy, x, w, *, dx=None, dw=None, db=None, activation="none", checkpoint=None, add=None,
+                    workspace=None):
+    """Writes those of dx = dz w (+ add), dw = dz^T x and db = sum of dz that are given, dz = dy act'(z).
+
+    z is what ``checkpoint`` stands for (not needed without an activation).  ``x`` may be None without dw, ``w``
+    without dx; ``dx`` may be ``add``.  ``workspace``: ``linear_backward_workspace(...)`` bytes, allocated if not given.
+    """
+    tokens, d_out = _matrix(dy, "dy")
+    code, act = _code(dy), _activation(activation)
+    a = _lib.LinearBackward()
+    a.dy, a.ldg = _rows(dy, "dy", dy, (tokens, d_out))
+    d_in = None
+    for t, name, other in ((dx, "dx", w), (dw, "dw", x)):
+        if t is not None:
+            if other is None:
+                raise ValueError("dx needs w" if name == "dx" else "dw needs x")
+            width = _matrix(t, name)[1]
+            if d_in is not None and width != d_in:
+                raise ValueError(f"dx and dw have {d_in} and {width} columns")
+            d_in = width
+    if dx is not None:
+        a.dx, a.ldd = _rows(dx, "dx", dy, (tokens, d_in))
+        a.w, a.ldw = _rows(w, "w", dy, (d_out, d_in))
+        if add is not None:
+            a.add, a.lda = _rows(add, "add", dy, (tokens, d_in))
+    if dw is not None:
+        a.dw, a.lddw = _rows(dw, "dw", dy, (d_out, d_in))
+        a.x, a.ldx = _rows(x, "x", dy, (tokens, d_in))
+    if db is not None:
+        a.db = _vector(db, "db", dy, d_out, dy.dtype)
+    if act != _lib.RDFFT_ACT_NONE:
+        if checkpoint is None:
+            raise ValueError(f"the gradient through {activation} needs the checkpoint of the pre-activation")
+        a.checkpoint = _held(checkpoint, dy, tokens, d_out)
+    d_in = 1 if d_in is None else d_in  # (db alone)
+    lib = _lib.load()
+    need = lib.linear_backward_workspace(d_in, d_out, tokens, dx is not None, dw is not None, db is not None, act, code)
+    _keep, a.workspace, a.workspace_bytes = _scratch(need, workspace, dy, "linear_backward")
+    _check(lib.linear_backward(ctypes.byref(a), d_in, d_out, tokens, act, code, _stream(dy)), "linear_backward")
+    return dx, dw, db
+
+
+def linear_backward_workspace(d_in: int, d_out: int, tokens: int, dtype: torch.dtype, activation: str = "none", *,
+                              dx: bool = True, dw: bool = True, db: bool = True) -> int:
+    need = int(_lib.load().linear_backward_workspace(d_in, d_out, tokens, dx, dw, db, _activation(activation),
+                                                     _CODES[dtype]))
+    if need < 0:
+        _check(need, "linear_backward_workspace")
+    return need
+
+
 def rdfft_init() -> None:
     _check(_lib.load().rdfft_init(), "rdfft_init")
 

@@ -19,7 +19,7 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "librdfft.so")
 
-SOURCES = ["bca_block_bf16.hip", "bca_block_f16.hip", "bca_block_f32.hip", "bca_store_bf16.hip", "bca_store_f16.hip", "bca_store_f32.hip", "rdfft_kernels.hip", "rdfft_hc_kernels.hip", "bca_kernels.hip", "bca_multipass.hip", "layout_kernels.hip", "mixed_kernels.hip", "capi.cpp", "twiddles.cpp"]
+SOURCES = ["bca_block_bf16.hip", "bca_block_f16.hip", "bca_block_f32.hip", "bca_store_bf16.hip", "bca_store_f16.hip", "bca_store_f32.hip", "rdfft_kernels.hip", "rdfft_hc_kernels.hip", "bca_kernels.hip", "bca_multipass.hip", "layout_kernels.hip", "mixed_kernels.hip", "act8_kernels.hip", "norm_kernels.hip", "linear_bf16.hip", "linear_f16.hip", "linear_f32.hip", "linear.hip", "capi.cpp", "capi_dense.cpp", "twiddles.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
@@ -46,7 +46,7 @@ COMMON = [
 
 def _compile(src: str) -> str:
     obj = os.path.join(BUILD, os.path.splitext(src)[0] + ".o")
-    # capi.cpp calls the HIP runtime, so it is compiled as HIP; twiddles.cpp is plain C++
+    # capi.cpp and capi_dense.cpp call the HIP runtime, so they are compiled as HIP; twiddles.cpp is plain C++
     lang = ["-x", "c++"] if src == "twiddles.cpp" else ["-x", "hip"]
     cmd = [HIPCC, *COMMON, *lang, "-c", os.path.join(CSRC, src), "-o", obj]
     res = subprocess.run(cmd, capture_output=True, text=True)

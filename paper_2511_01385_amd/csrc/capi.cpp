@@ -14,6 +14,7 @@
 #include <mutex>
 #include <vector>
 
+#include "capi_util.hpp"
 #include "launch.hpp"
 #include "plan.hpp"
 #include "rdfft.h"
@@ -39,23 +40,9 @@ int ilog2(int64_t v) {
   return l;
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+}  // namespace
 
-// [a, a+na) and [b, b+nb) share a byte
-bool overlaps(const void* a, int64_t na, const void* b, int64_t nb) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return na > 0 && nb > 0 && x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
-}
-
-int elem_bytes(int dtype) { return dtype == RDFFT_F32 ? 4 : 2; }
-
-// products of sizes that must not overflow int64
-bool mul_ok(int64_t a, int64_t b, int64_t* out) {
-  if (a < 0 || b < 0) return false;
-  if (a != 0 && b > INT64_MAX / a) return false;
-  *out = a * b;
-  return true;
-}
+namespace rdfft {
 
 int ensure_device(const float2** tw, int* num_cu) {
   int dev = -1;
@@ -69,8 +56,8 @@ int ensure_device(const float2** tw, int* num_cu) {
       hipDeviceProp_t prop;
       if (hipGetDeviceProperties(&prop, dev) != hipSuccess) return RDFFT_EDEVICE;
       if (strncmp(prop.gcnArchName, "gfx950", 6) != 0) return RDFFT_EDEVICE;
-      static const std::vector<rdfft::HostC32> host = rdfft::build_twiddle_table();
-      if (rdfft::upload_twiddles(host.data(), host.size() * sizeof(rdfft::HostC32), &p) != hipSuccess)
+      static const std::vector<HostC32> host = build_twiddle_table();
+      if (upload_twiddles(host.data(), host.size() * sizeof(HostC32), &p) != hipSuccess)
         return RDFFT_EDEVICE;
       st.num_cu = prop.multiProcessorCount;
       st.tw.store(p, std::memory_order_release);
@@ -80,6 +67,16 @@ int ensure_device(const float2** tw, int* num_cu) {
   if (num_cu) *num_cu = st.num_cu;
   return RDFFT_OK;
 }
+
+}  // namespace rdfft
+
+namespace {
+
+using rdfft::aligned16;
+using rdfft::elem_bytes;
+using rdfft::ensure_device;
+using rdfft::mul_ok;
+using rdfft::overlaps;
 
 int check_transform(const void* buf, int64_t rows, int64_t n, int dtype) {
   if (dtype != RDFFT_F32 && dtype != RDFFT_BF16 && dtype != RDFFT_F16) return RDFFT_EINVAL;

@@ -1,0 +1,484 @@
+// linear_kernels.hpp -- the dense product with its epilogue on the matrix cores, as templates over
+// the storage type (linear_{f32,bf16,f16}.hip instantiate them).
+//
+//   D(m, n) = sum over k of A(m, k) B(n, k)
+//
+// Three products have this form: y = x W^T (A = x, B = W), dx = dz W (A = dz, B = W with its
+// rows along k) and dW = dz^T x (both with their rows along k).  An operand is "along k" when
+// its rows in memory are runs of k (element (m, k) at a[m * lda + k]) and "across k" when they
+// are runs of m (a[k * lda + m]).
+//
+// A workgroup computes a BM x BN tile of D; a stage of 128 bytes of k (64 16-bit values, 32
+// floats) of both operands lies in LDS, two stages in turn.  The stage after the one being
+// multiplied is under way in the meantime: by loads that go straight to LDS (16 bytes a lane), or
+// through registers where a row of an operand does not start at a multiple of 16 bytes.
+//
+// LDS layouts (units of 16 bytes, `pos` of a row holding chunk `pos ^ swizzle`):
+//   along k:   [BM rows][8 chunks], swizzle row & 7: the 16 rows of a fragment, read at one chunk,
+//              fall on all banks evenly;
+//   across k:  [k rows][BM * S / 16 chunks], swizzle (k & 3) * 2 for 16-bit values, whose
+//              fragments are read transposed, four k rows of 16 values (32 bytes) at a time, and
+//              (k / 4 & 3) * 4 for floats, read one by one in runs of 16 at four k rows.
+//
+// The matrix instructions take n as their row and m as their column, so that a lane's four
+// results are consecutive in n, the direction in which D, the bias, the residual and the 8-bit
+// blocks run.  k is spread over a fragment's four lane groups in runs of one chunk, for both
+// operands alike.  Sums are float32 throughout.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "dense_device.hpp"
+#include "dense_launch.hpp"
+
+namespace rdfft {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+// One chunk of k (16 bytes a lane and lane group): 16 x 16 results
+template <class E>
+__device__ __forceinline__ f32x4 mfma_chunk(u32x4 a, u32x4 b, f32x4 c) {
+  if constexpr (E::kId == kStorageBF16) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0,
+                                                   0);
+  } else if constexpr (E::kId == kStorageF16) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[i]), __uint_as_float(b[i]), c, 0, 0, 0);
+    return c;
+  }
+}
+
+// ----------------------------------------------------------------------------------
+// activations.  erf by Abramowitz and Stegun's 7.1.26 (absolute error 1.5e-7), whose exp(-x^2) is
+// also the density in gelu's slope.
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float rcp_fast(float x) { return __builtin_amdgcn_rcpf(x); }
+constexpr float kLog2e = 1.44269504088896341f;
+
+// normal distribution function of z, and e = exp(-z^2 / 2)
+__device__ __forceinline__ float normal_cdf(float z, float* e) {
+  const float x = fabsf(z) * 0.70710678118654752f;
+  const float t = rcp_fast(fmaf(0.3275911f, x, 1.f));
+  const float g = exp2_fast(-kLog2e * x * x);
+  float p = fmaf(1.061405429f, t, -1.453152027f);
+  p = fmaf(p, t, 1.421413741f);
+  p = fmaf(p, t, -0.284496736f);
+  p = fmaf(p, t, 0.254829592f);
+  *e = g;
+  const float tail = 0.5f * p * t * g;  // 1 - cdf(|z|)
+  return z < 0.f ? tail : 1.f - tail;
+}
+
+__device__ __forceinline__ float activate(int act, float z) {
+  if (act == kActRelu) return z < 0.f ? 0.f : z;  // (a NaN stays)
+  if (act == kActGelu) {
+    float e;
+    const float c = normal_cdf(z, &e);
+    return c == 0.f ? c * 0.f : z * c;  // -infinity to zero, not NaN
+  }
+  if (act == kActSilu) {
+    const float d = 1.f + exp2_fast(-kLog2e * z);
+    return z * rcp_fast(d);
+  }
+  return z;
+}
+
+__device__ __forceinline__ float activation_slope(int act, float z) {
+  if (act == kActRelu) return z != z ? z : z > 0.f ? 1.f : 0.f;
+  if (act == kActGelu) {
+    float e;
+    const float c = normal_cdf(z, &e);
+    return fmaf(z * 0.39894228040143268f, e, c);
+  }
+  if (act == kActSilu) {
+    const float s = rcp_fast(1.f + exp2_fast(-kLog2e * z));
+    return s * fmaf(z, 1.f - s, 1.f);
+  }
+  return 1.f;
+}
+
+// ----------------------------------------------------------------------------------
+// operands
+
+constexpr int kStageBytes = 128;  // of k, per row and stage
+
+// Loads that go straight to LDS: 64 lanes of 16 bytes from `base` + their offset to consecutive LDS
+// bytes from `lds`.  A lane whose offset is kNowhere stores zeros.  They are written as
+// assembly because the compiler, which cannot tell the two stages apart, would wait for them before
+// each LDS read; stage_wait() is the wait.  (No register receives anything.)
+constexpr uint32_t kNowhere = 0x80000000u;
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void load_to_lds(const char* base, uint32_t offset, uint32_t lds) {
+  // (base and lds are the same in all lanes, which the compiler does not always see)
+  const uint64_t p = reinterpret_cast<uint64_t>(base);
+  const uint64_t u = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(p >> 32)) << 32 |
+                     (uint32_t)__builtin_amdgcn_readfirstlane((int)p);
+  lds = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds);
+  const __amdgpu_buffer_rsrc_t r =
+      __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<char*>(u), 0, (int)(kNowhere - 1), 0x00020000);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(r)
+               : "memory", "m0");
+}
+#pragma clang diagnostic pop
+// all loads to LDS done, all LDS reads done, every wave here
+__device__ __forceinline__ void stage_wait() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// R rows (m or n) of one operand's stage.  ACROSS: memory rows run along m.  DMA: straight to
+// LDS, for which a memory row starts at a multiple of 16 bytes and holds whole chunks.
+template <class E, int R, int WAVES, bool ACROSS, bool DMA>
+struct Operand {
+  using T = typename E::T;
+  static constexpr int S = sizeof(T), EPC = 16 / S, BK = kStageBytes / S;
+  static constexpr int CPR = ACROSS ? R * S / 16 : 8;  // chunks of an LDS row
+  static constexpr int BYTES = R * kStageBytes;
+  static constexpr int LINES = BYTES / 1024 / WAVES;   // 64 chunks each, a wave's share
+  static_assert(LINES * WAVES * 1024 == BYTES && 64 % CPR == 0);
+
+  const T* base;    // row 0 and k 0 of this workgroup's tile
+  int64_t ld;
+  int rows, depth;  // rows of the tile that exist, k that is left
+  int wave, lane;
+  uint32_t offset[DMA ? LINES : 1];
+  u32x4 held[DMA ? 1 : LINES];
+
+  __device__ __forceinline__ static int swizzle(int k) { return S == 2 ? (k & 3) << 1 : (k >> 2 & 3) << 2; }
+  // LDS row and chunk of this lane's part of line j
+  __device__ __forceinline__ int row_of(int j) const { return (wave * LINES + j) * (64 / CPR) + lane / CPR; }
+  __device__ __forceinline__ int chunk_of(int j) const {
+    return (lane % CPR) ^ (ACROSS ? swizzle(row_of(j)) : row_of(j) & 7);
+  }
+
+  __device__ __forceinline__ void init(const T* origin, int64_t ld_, int64_t r0, int64_t r_end, int64_t k0, int64_t k_end,
+                                       int wave_, int lane_) {
+    ld = ld_;
+    base = origin + (ACROSS ? k0 * ld + r0 : r0 * ld + k0);
+    rows = (int)(r_end - r0 < R ? r_end - r0 : R);
+    depth = (int)(k_end - k0);
+    wave = wave_;
+    lane = lane_;
+    if constexpr (DMA) {
+#pragma unroll
+      for (int j = 0; j < LINES; ++j) {
+        const int r = row_of(j), c = chunk_of(j);
+        const bool in = ACROSS ? c * EPC < rows : r < rows;
+        offset[j] = in ? (uint32_t)r * (uint32_t)(ld * S) + (uint32_t)c * 16u : kNowhere;
+      }
+    }
+  }
+
+  // starts the loads of the next stage (the LDS region `lds` for DMA) and steps on
+  __device__ __forceinline__ void fetch(uint32_t lds) {
+    if constexpr (DMA) {
+      const char* const p = reinterpret_cast<const char*>(base);
+      if (depth >= BK) {
+#pragma unroll
+        for (int j = 0; j < LINES; ++j) load_to_lds(p, offset[j], lds + (uint32_t)(wave * LINES + j) * 1024u);
+      } else {
+#pragma unroll
+        for (int j = 0; j < LINES; ++j) {
+          const int k = ACROSS ? row_of(j) : chunk_of(j) * EPC;
+          load_to_lds(p, k < depth ? offset[j] : kNowhere, lds + (uint32_t)(wave * LINES + j) * 1024u);
+        }
+      }
+    } else {
+      // (a stage in the interior is loaded without branches)
+      if (rows == R && depth >= BK) {
+#pragma unroll
+        for (int j = 0; j < LINES; ++j) {
+          const Bytes16 v = *reinterpret_cast<const Bytes16*>(base + row_of(j) * ld + chunk_of(j) * EPC);
+          held[j] = u32x4{v.w[0], v.w[1], v.w[2], v.w[3]};
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < LINES; ++j) {
+          const int r = row_of(j), i = chunk_of(j) * EPC;
+          const int r_end = ACROSS ? min(depth, BK) : rows, i_end = ACROSS ? rows : min(depth, BK);
+          const T* const p = base + r * ld + i;
+          u32x4 h = {0, 0, 0, 0};
+          if (r < r_end) {
+            if (i + EPC <= i_end) {
+              const Bytes16 v = *reinterpret_cast<const Bytes16*>(p);
+              h = u32x4{v.w[0], v.w[1], v.w[2], v.w[3]};
+            } else {
+#pragma unroll
+              for (int e = 0; e < EPC; ++e)
+                if (i + e < i_end) {
+                  if constexpr (S == 4) h[e] = __builtin_bit_cast(uint32_t, p[e]);
+                  else h[e / 2] |= (uint32_t)p[e] << (16 * (e % 2));
+                }
+            }
+          }
+          held[j] = h;
+        }
+      }
+    }
+    base += ACROSS ? BK * ld : BK;
+    depth -= BK;
+  }
+  // puts fetched registers into LDS
+  __device__ __forceinline__ void commit(char* lds) const {
+    if constexpr (!DMA) {
+#pragma unroll
+      for (int j = 0; j < LINES; ++j)
+        *reinterpret_cast<u32x4*>(lds + (wave * LINES + j) * 1024 + lane * 16) = held[j];
+    }
+  }
+};
+
+// Fragments of one operand: 16 rows at row0 + 16 f, k chunk group kk (of two).
+template <class E, int R, bool ACROSS>
+struct Fragments {
+  static constexpr int S = sizeof(typename E::T), ROWB = R * S;
+  uint32_t at[ACROSS ? 4 : 2];
+  __device__ __forceinline__ void init(int row0, int lane) {
+    const int g = lane >> 4, j = lane & 15;
+    if constexpr (!ACROSS) {
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk)
+        at[kk] = (uint32_t)((row0 + j) * kStageBytes + ((kk * 4 + g) ^ (j & 7)) * 16);
+    } else if constexpr (S == 2) {
+      // (row0 is a multiple of 32: its chunks leave the swizzled bits alone but for the lowest f's)
+#pragma unroll
+      for (int f = 0; f < 4; ++f) {
+        const int chunk = (row0 / 8 + f * 2 + ((j & 3) >> 1)) ^ ((j >> 2) << 1);
+        at[f] = (uint32_t)((g * 8 + (j >> 2)) * ROWB + chunk * 16 + (j & 1) * 8);
+      }
+    } else {
+#pragma unroll
+      for (int f = 0; f < 4; ++f) {
+        const int chunk = (row0 / 4 + f * 4 + (j >> 2)) ^ (g << 2);
+        at[f] = (uint32_t)(g * 4 * ROWB + chunk * 16 + (j & 3) * 4);
+      }
+    }
+  }
+  __device__ __forceinline__ u32x4 read(const char* lds, int f, int kk) const {
+    if constexpr (!ACROSS) {
+      return *reinterpret_cast<const u32x4*>(lds + at[kk] + f * 16 * kStageBytes);
+    } else if constexpr (S == 2) {
+      // four groups of 16 rows are 128 bytes: f / 4 steps over the swizzle
+      const char* const p = lds + at[f & 3] + (f >> 2) * 128 + kk * 32 * ROWB;
+      typedef __attribute__((address_space(3))) s16x4 Lds;
+      const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)p));
+      const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(p + 4 * ROWB)));
+      return u32x4{lo[0], lo[1], hi[0], hi[1]};
+    } else {
+      const char* const p = lds + at[f & 3] + (f >> 2) * 256 + kk * 16 * ROWB;
+      u32x4 v;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint32_t*>(p + i * ROWB);
+      return v;
+    }
+  }
+};
+
+// ----------------------------------------------------------------------------------
+// epilogue of eight consecutive results z of row m, from column n (a multiple of eight); four
+// consecutive lanes hold an 8-bit block, all of them here.  bias: of these columns.
+template <class E>
+__device__ __forceinline__ void finish_group(const GemmArgs& g, int64_t m, int64_t n, const float* bias, float* z) {
+  using T = typename E::T;
+  const bool in = m < g.m && n < g.n;
+  if (g.partial != nullptr) {
+    if (in) write_group<ElemF32>(g.partial + m * g.n, n, g.n, z);
+    return;
+  }
+  const int left = in ? (int)min(g.n - n, (int64_t)kVec) : 0;
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) z[i] = i < left ? z[i] + bias[i] : 0.f;
+  if (g.ck.codes != nullptr) {
+    const int s = ck_scale_byte(quad_max(max_bits8(z)));
+    if (in) {
+      write_codes(g.ck.codes + m * g.n, n, g.n, ck_encode(z, s));
+      if (n % kCkBlock == 0) g.ck.scales[m * ((g.n + kCkBlock - 1) / kCkBlock) + n / kCkBlock] = (uint8_t)s;
+    }
+  }
+  if (!in) return;
+  if (g.act != kActNone) {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) z[i] = activate(g.act, z[i]);
+  }
+  if (g.residual != nullptr) {
+    float add[kVec];
+    read_group<E>(static_cast<const T*>(g.residual) + m * g.ldr, n, g.n, add);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) z[i] += add[i];
+  }
+  write_group<E>(static_cast<T*>(g.d) + m * g.ldd, n, g.n, z);
+}
+template <class E>
+__device__ __forceinline__ void read_bias(const GemmArgs& g, int64_t n, float* bias) {
+  if (g.bias != nullptr && n < g.n) {
+    read_group<E>(static_cast<const typename E::T*>(g.bias), n, g.n, bias);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) bias[i] = 0.f;
+  }
+}
+
+// D's tile (or split) of this workgroup.  Workgroups are dealt to the eight XCDs in turn; each XCD
+// takes a run of tiles, ordered so that eight rows of tiles share the columns that its L2 holds.
+struct TileAt {
+  int tm, tn, split;
+};
+__device__ __forceinline__ TileAt tile_of(int id, int tiles_m, int tiles_n, int splits) {
+  const int total = tiles_m * tiles_n * splits;
+  constexpr int XCDS = 8, GROUP = 8;
+  const int each = total / XCDS, more = total % XCDS;
+  const int x = id % XCDS;
+  int t = x * each + min(x, more) + id / XCDS;
+  const int split = t / (tiles_m * tiles_n);
+  t -= split * tiles_m * tiles_n;
+  const int band = t / (GROUP * tiles_n), first = band * GROUP;
+  const int high = min(GROUP, tiles_m - first);
+  t -= band * GROUP * tiles_n;
+  return {first + t % high, t / high, split};
+}
+
+template <class E, int BM, int BN, int WM, int WN, bool AX, bool BX, bool DMA>
+__global__ void __launch_bounds__(WM * WN * 64) linear_kernel(GemmArgs g) {
+  using T = typename E::T;
+  constexpr int WAVES = WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
+  constexpr int BK = kStageBytes / (int)sizeof(T);
+  static_assert(FN % 2 == 0, "a wave holds whole blocks of 32 values");
+  using OpA = Operand<E, BM, WAVES, AX, DMA>;
+  using OpB = Operand<E, BN, WAVES, BX, DMA>;
+  constexpr int STAGE = OpA::BYTES + OpB::BYTES;
+  extern __shared__ __attribute__((aligned(1024))) char linear_lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
+  const int wm = wave / WN, wn = wave % WN;
+  const TileAt at = tile_of((int)blockIdx.x, g.tiles_m, g.tiles_n, g.splits);
+  const int64_t m0 = (int64_t)at.tm * BM, n0 = (int64_t)at.tn * BN;
+  const int64_t k0 = (int64_t)at.split * g.k_split, k1 = min(k0 + g.k_split, g.k);
+
+  OpA a;
+  OpB b;
+  a.init(static_cast<const T*>(g.a), g.lda, m0, g.m, k0, k1, wave, lane);
+  b.init(static_cast<const T*>(g.b), g.ldb, n0, g.n, k0, k1, wave, lane);
+  Fragments<E, BM, AX> fa;
+  Fragments<E, BN, BX> fb;
+  fa.init(wm * TM, lane);
+  fb.init(wn * TN, lane);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)linear_lds;
+
+  f32x4 acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  const int steps = (int)((k1 - k0 + BK - 1) / BK);
+  if (steps > 0) {
+    a.fetch(lds0);
+    b.fetch(lds0 + OpA::BYTES);
+    a.commit(linear_lds);
+    b.commit(linear_lds + OpA::BYTES);
+    stage_wait();
+  }
+  for (int t = 0; t < steps; ++t) {
+    const int cur = t & 1;
+    const char* const la = linear_lds + cur * STAGE;
+    const char* const lb = la + OpA::BYTES;
+    const bool more = t + 1 < steps;
+    if (more) {
+      a.fetch(lds0 + (uint32_t)(cur ^ 1) * STAGE);
+      b.fetch(lds0 + (uint32_t)(cur ^ 1) * STAGE + OpA::BYTES);
+    }
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      u32x4 va[FM], vb[FN];
+#pragma unroll
+      for (int j = 0; j < FN; ++j) vb[j] = fb.read(lb, j, kk);
+#pragma unroll
+      for (int i = 0; i < FM; ++i) va[i] = fa.read(la, i, kk);
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = mfma_chunk<E>(vb[j], va[i], acc[i][j]);
+    }
+    if (more) {
+      a.commit(linear_lds + (cur ^ 1) * STAGE);
+      b.commit(linear_lds + (cur ^ 1) * STAGE + OpA::BYTES);
+    }
+    stage_wait();
+  }
+
+  // Each wave turns its results, 16 rows at a time, through LDS of its own into runs of eight
+  // along n: eight lanes then write whole cache lines of D.  (The last stage_wait let go of the LDS.)
+  constexpr int PITCH = TN + 4, RUNS = TN / kVec, ROWS = 64 / RUNS;
+  static_assert(WAVES * 16 * PITCH * 4 <= 2 * STAGE && 16 % ROWS == 0);
+  float* const turn = reinterpret_cast<float*>(linear_lds) + wave * 16 * PITCH;
+  const int64_t n = n0 + wn * TN + lane % RUNS * kVec;
+  float bias[kVec];
+  read_bias<E>(g, n, bias);
+  if (g.partial != nullptr) g.partial += (int64_t)at.split * g.m * g.n;
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+      *reinterpret_cast<f32x4*>(turn + (lane & 15) * PITCH + j * 16 + (lane >> 4) * 4) = acc[i][j];
+#pragma unroll
+    for (int h = 0; h < 16 / ROWS; ++h) {
+      const int r = h * ROWS + lane / RUNS;
+      float z[kVec];
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const f32x4 v = *reinterpret_cast<const f32x4*>(turn + r * PITCH + lane % RUNS * kVec + q * 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[q * 4 + e] = v[e];
+      }
+      finish_group<E>(g, m0 + wm * TM + i * 16 + r, n, bias, z);
+    }
+  }
+}
+
+template <class E, int BM, int BN, int WM, int WN, bool AX, bool BX, bool DMA>
+hipError_t linear_launch(const GemmArgs& g, hipStream_t stream) {
+  constexpr int lds = 2 * (BM + BN) * kStageBytes;
+  const auto kernel = linear_kernel<E, BM, BN, WM, WN, AX, BX, DMA>;
+  static const hipError_t ready = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                                      hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (ready != hipSuccess) return ready;
+  GemmArgs t = g;
+  t.tiles_m = (int)((g.m + BM - 1) / BM);
+  t.tiles_n = (int)((g.n + BN - 1) / BN);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(t.tiles_m * t.tiles_n * t.splits)), dim3(WM * WN * 64), lds, stream, t);
+  return hipGetLastError();
+}
+
+template <class E>
+LinearTable make_linear_table() {
+  LinearTable t{};
+  const auto fill = [&](LinearFn(&row)[2], auto ax, auto bx, auto tile) {
+    constexpr bool AX = decltype(ax)::value, BX = decltype(bx)::value;
+    if constexpr (decltype(tile)::value == kTile256) {
+      // (float32 products are bound by the matrix cores at any tile; rows that start anywhere are rare)
+      if constexpr (E::kId != kStorageF32) row[1] = linear_launch<E, 256, 256, 2, 4, AX, BX, true>;
+    } else {
+      row[0] = linear_launch<E, 128, 128, 2, 2, AX, BX, false>;
+      row[1] = linear_launch<E, 128, 128, 2, 2, AX, BX, true>;
+    }
+  };
+  const auto operands = [&](auto tile) {
+    constexpr int i = decltype(tile)::value;
+    fill(t.fn[i][kForward], std::false_type{}, std::false_type{}, tile);
+    fill(t.fn[i][kGradX], std::false_type{}, std::true_type{}, tile);
+    fill(t.fn[i][kGradW], std::true_type{}, std::true_type{}, tile);
+  };
+  operands(std::integral_constant<int, kTile128>{});
+  operands(std::integral_constant<int, kTile256>{});
+  return t;
+}
+
+}  // namespace rdfft
