@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "librdfft.so")
 
@@ -60,43 +61,17 @@ class BcaGrads(ctypes.Structure):
     _fields_ = [("dx", ctypes.c_void_p), ("dc", ctypes.c_void_p)]
 
 
-class Act8(ctypes.Structure):
-    """act8_t"""
-
-    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
-
-
-def _fields(text):
-    """Pointers and int64 sizes (those named ld* and *_bytes) of a struct, in order."""
-    kinds = {"checkpoint": Act8}
-    return [(n, kinds.get(n, ctypes.c_int64 if n.startswith("ld") or n.endswith("_bytes") else ctypes.c_void_p))
-            for n in text.split()]
-
-
-class LayerNormForward(ctypes.Structure):
-    """layer_norm_forward_t"""
-
-    _fields_ = _fields("x ldx residual ldr weight bias y ldy mean rstd checkpoint")
-
-
-class LayerNormBackward(ctypes.Structure):
-    """layer_norm_backward_t"""
-
-    _fields_ = _fields("dy ldg x ldx residual ldr checkpoint weight mean rstd dx ldd dweight dbias workspace "
-                       "workspace_bytes")
-
-
-class LinearForward(ctypes.Structure):
-    """linear_forward_t"""
-
-    _fields_ = _fields("x ldx w ldw bias residual ldr y ldy checkpoint workspace workspace_bytes")
-
-
-class LinearBackward(ctypes.Structure):
-    """linear_backward_t"""
-
-    _fields_ = _fields("dy ldg checkpoint x ldx w ldw add lda dx ldd dw lddw db workspace workspace_bytes")
-
+# The argument structs of the operators around the adapter, every field of which is a pointer or an
+# int64, as packers of their fields in order (a third of a ctypes.Structure's time).
+_FIELDS = {
+    "act8": "codes scales",
+    "layer_norm_forward": "x ldx residual ldr weight bias y ldy mean rstd codes scales",
+    "layer_norm_backward": "dy ldg x ldx residual ldr codes scales weight mean rstd dx ldd dweight dbias workspace "
+                           "workspace_bytes",
+    "linear_forward": "x ldx w ldw bias residual ldr y ldy codes scales workspace workspace_bytes",
+    "linear_backward": "dy ldg codes scales x ldx w ldw add lda dx ldd dw lddw db workspace workspace_bytes",
+}
+pack = {name: struct.Struct(f"{len(fields.split())}q").pack for name, fields in _FIELDS.items()}
 
 _lib = None
 
@@ -124,12 +99,13 @@ def load() -> ctypes.CDLL:
     lib.bca_backward_batched.argtypes = [i32, pp, pp, pp, ctypes.POINTER(BcaGrads), i64, i64, i64, i64, i32, vp]
     lib.bca_backward_batched.restype = i32
     f32 = ctypes.c_float
-    lib.act8_quantize.argtypes = [vp, i64, ctypes.POINTER(Act8), i64, i64, i32, vp]
-    lib.act8_dequantize.argtypes = [ctypes.POINTER(Act8), vp, i64, i64, i64, i32, vp]
-    lib.layer_norm_forward.argtypes = [ctypes.POINTER(LayerNormForward), i64, i64, f32, i32, vp]
-    lib.layer_norm_backward.argtypes = [ctypes.POINTER(LayerNormBackward), i64, i64, i32, vp]
-    lib.linear_forward.argtypes = [ctypes.POINTER(LinearForward), i64, i64, i64, i32, i32, vp]
-    lib.linear_backward.argtypes = [ctypes.POINTER(LinearBackward), i64, i64, i64, i32, i32, vp]
+    # (the structs come as bytes, see pack)
+    lib.act8_quantize.argtypes = [vp, i64, vp, i64, i64, i32, vp]
+    lib.act8_dequantize.argtypes = [vp, vp, i64, i64, i64, i32, vp]
+    lib.layer_norm_forward.argtypes = [vp, i64, i64, f32, i32, vp]
+    lib.layer_norm_backward.argtypes = [vp, i64, i64, i32, vp]
+    lib.linear_forward.argtypes = [vp, i64, i64, i64, i32, i32, vp]
+    lib.linear_backward.argtypes = [vp, i64, i64, i64, i32, i32, vp]
     for name in ("act8_quantize", "act8_dequantize", "layer_norm_forward", "layer_norm_backward", "linear_forward",
                  "linear_backward"):
         getattr(lib, name).restype = i32

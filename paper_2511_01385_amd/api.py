@@ -8,6 +8,7 @@ operation touches the data.
 from __future__ import annotations
 
 import ctypes
+import functools
 
 import torch
 
@@ -249,14 +250,16 @@ ACTIVATIONS = {"none": _lib.RDFFT_ACT_NONE, "relu": _lib.RDFFT_ACT_RELU, "gelu":
                "silu": _lib.RDFFT_ACT_SILU}
 
 
-def _rows(t: torch.Tensor, name: str, like: torch.Tensor, shape) -> tuple[int, int]:
-    """(pointer, row stride) of a (rows, n) tensor of ``like``'s type and device."""
-    if t.dtype != like.dtype:
-        raise TypeError(f"{name} is {t.dtype}, expected {like.dtype}")
+def _rows(t: torch.Tensor, name: str, dtype: torch.dtype, device: int, shape) -> tuple[int, int]:
+    """(pointer, row stride) of a (rows, n) tensor of that type and device."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr(), shape[1]
+    if t.dtype != dtype:
+        raise TypeError(f"{name} is {t.dtype}, expected {dtype}")
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if not t.is_cuda or t.get_device() != like.get_device():
-        raise ValueError(f"{name} must be a device tensor on {like.device}, is on {t.device}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be on cuda:{device}, is on {t.device}")
     rows, n = shape
     s0, s1 = t.stride()
     if (s1 != 1 and n > 1) or (s0 < n and rows > 1):
@@ -264,83 +267,95 @@ def _rows(t: torch.Tensor, name: str, like: torch.Tensor, shape) -> tuple[int, i
     return t.data_ptr(), max(s0, n)
 
 
-def _vector(t: torch.Tensor, name: str, like: torch.Tensor, n: int, dtype: torch.dtype) -> int:
+def _vector(t: torch.Tensor, name: str, dtype: torch.dtype, device: int, n: int) -> int:
+    if t.dtype is dtype and t.shape == (n,) and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
     if t.dtype != dtype:
         raise TypeError(f"{name} is {t.dtype}, expected {dtype}")
     if t.shape != (n,):
         raise ValueError(f"{name} must have shape ({n},), got {tuple(t.shape)}")
-    if not t.is_cuda or t.get_device() != like.get_device():
-        raise ValueError(f"{name} must be a device tensor on {like.device}, is on {t.device}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return t.data_ptr()
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be on cuda:{device}, is on {t.device}")
+    raise ValueError(f"{name} must be contiguous")
 
 
-def _matrix(t: torch.Tensor, name: str) -> tuple[int, int]:
-    if t.dim() != 2:
-        raise ValueError(f"{name} must be two-dimensional, got shape {tuple(t.shape)}")
-    return t.shape
+def _first(t: torch.Tensor, name: str):
+    """(rows, n), storage type, its code, device and stream of a call, by its first tensor."""
+    shape = t.shape
+    if len(shape) != 2:
+        raise ValueError(f"{name} must be two-dimensional, got shape {tuple(shape)}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    return shape, t.dtype, _code(t), t.get_device(), _stream(t)
 
 
-def _held(checkpoint, like: torch.Tensor, rows: int, n: int):
-    """act8_t of a (codes, scales) pair for (rows, n) values, or of none."""
-    if checkpoint is None:
-        return _lib.Act8(None, None)
+def _held(checkpoint, device: int, rows: int, n: int) -> tuple[int, int]:
+    """Pointers of a (codes, scales) pair for (rows, n) values."""
     codes, scales = checkpoint
     for name, t, dtype, shape in (("codes", codes, torch.int8, (rows, n)),
                                   ("scales", scales, torch.uint8, (rows, -(-n // CHECKPOINT_BLOCK)))):
-        if t.dtype != dtype:
+        if t.dtype is not dtype:
             raise TypeError(f"a checkpoint's {name} are {dtype}, got {t.dtype}")
         if t.shape != shape:
             raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
-        if not t.is_cuda or t.get_device() != like.get_device():
-            raise ValueError(f"{name} must be a device tensor on {like.device}, is on {t.device}")
+        if t.get_device() != device:
+            raise ValueError(f"{name} must be on cuda:{device}, is on {t.device}")
         if not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous")
-    return _lib.Act8(codes.data_ptr(), scales.data_ptr())
+    return codes.data_ptr(), scales.data_ptr()
 
 
-def _scratch(need: int, given, like: torch.Tensor, what: str):
+def _scratch(need: int, given, device: int, what: str):
     """(tensor to keep alive, pointer, bytes) of a workspace; one is allocated if none is given."""
-    if need < 0:
-        _check(need, what)
     if need == 0:
-        return None, None, 0
+        return None, 0, 0
     if given is None:
-        given = torch.empty(need, dtype=torch.uint8, device=like.device)
-    elif not given.is_cuda or given.get_device() != like.get_device() or not given.is_contiguous():
-        raise ValueError(f"the workspace must be a contiguous tensor on {like.device}")
+        given = torch.empty(need, dtype=torch.uint8, device=torch.device("cuda", device))
+    elif given.get_device() != device or not given.is_contiguous():
+        raise ValueError(f"the workspace must be a contiguous tensor on cuda:{device}")
     size = given.numel() * given.element_size()
     if size < need:
         raise ValueError(f"the workspace has {size} bytes, {what} needs {need}")
     return given, given.data_ptr(), size
 
 
+# (the sizes of workspaces follow from their arguments alone)
+@functools.lru_cache(maxsize=4096)
+def _need(name: str, *args: int) -> int:
+    need = int(getattr(_lib.load(), name)(*args))
+    if need < 0:
+        _check(need, name)
+    return need
+
+
 def checkpoint_like(x: torch.Tensor) -> tuple[torch.Tensor, torch.Tensor]:
     """An empty 8-bit checkpoint (codes, scales) for the values of a (rows, n) tensor."""
-    rows, n = _matrix(x, "x")
+    rows, n = x.shape
     return (torch.empty((rows, n), dtype=torch.int8, device=x.device),
             torch.empty((rows, -(-n // CHECKPOINT_BLOCK)), dtype=torch.uint8, device=x.device))
 
 
 def act8_quantize(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor):
     """The 8-bit checkpoint of x (rows, n): int8 codes, and one scale byte for 32 values of a row."""
-    rows, n = _matrix(x, "x")
-    code = _code(x)
-    p, ld = _rows(x, "x", x, x.shape)
-    held = _held((codes, scales), x, rows, n)
-    _check(_lib.load().act8_quantize(p, ld, ctypes.byref(held), rows, n, code, _stream(x)), "act8_quantize")
+    shape, dtype, code, device, stream = _first(x, "x")
+    rows, n = shape
+    p, ld = _rows(x, "x", dtype, device, shape)
+    held = _lib.pack["act8"](*_held((codes, scales), device, rows, n))
+    _check(_lib.load().act8_quantize(p, ld, held, rows, n, code, stream), "act8_quantize")
     return codes, scales
 
 
 def act8_dequantize(codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor) -> torch.Tensor:
     """What a checkpoint stands for, in ``out``'s type (exact in float32 and bfloat16)."""
-    rows, n = _matrix(out, "out")
-    code = _code(out)
-    p, ld = _rows(out, "out", out, out.shape)
-    held = _held((codes, scales), out, rows, n)
-    _check(_lib.load().act8_dequantize(ctypes.byref(held), p, ld, rows, n, code, _stream(out)), "act8_dequantize")
+    shape, dtype, code, device, stream = _first(out, "out")
+    rows, n = shape
+    p, ld = _rows(out, "out", dtype, device, shape)
+    held = _lib.pack["act8"](*_held((codes, scales), device, rows, n))
+    _check(_lib.load().act8_dequantize(held, p, ld, rows, n, code, stream), "act8_dequantize")
     return out
+
+
+_F32 = torch.float32
 
 
 def layer_norm_forward(x, weight, bias, y, *, residual=None, mean=None, rstd=None, checkpoint=None, eps=1e-5):
@@ -349,23 +364,18 @@ def layer_norm_forward(x, weight, bias, y, *, residual=None, mean=None, rstd=Non
     ``mean`` and ``rstd`` (rows,) and ``checkpoint``, of the norm's input, are written if given.
     ``y`` may be ``x`` or ``residual``.
     """
-    rows, n = shape = _matrix(x, "x")
-    code = _code(x)
-    a = _lib.LayerNormForward()
-    a.x, a.ldx = _rows(x, "x", x, shape)
-    if residual is not None:
-        a.residual, a.ldr = _rows(residual, "residual", x, shape)
-    a.weight = _vector(weight, "weight", x, n, torch.float32)
-    if bias is not None:
-        a.bias = _vector(bias, "bias", x, n, torch.float32)
-    a.y, a.ldy = _rows(y, "y", x, shape)
-    if mean is not None:
-        a.mean = _vector(mean, "mean", x, rows, torch.float32)
-    if rstd is not None:
-        a.rstd = _vector(rstd, "rstd", x, rows, torch.float32)
-    a.checkpoint = _held(checkpoint, x, rows, n)
-    st = _lib.load().layer_norm_forward(ctypes.byref(a), rows, n, eps, code, _stream(x))
-    _check(st, "layer_norm_forward")
+    shape, dtype, code, device, stream = _first(x, "x")
+    rows, n = shape
+    a = _lib.pack["layer_norm_forward"](
+        *_rows(x, "x", dtype, device, shape),
+        *((0, 0) if residual is None else _rows(residual, "residual", dtype, device, shape)),
+        _vector(weight, "weight", _F32, device, n),
+        0 if bias is None else _vector(bias, "bias", _F32, device, n),
+        *_rows(y, "y", dtype, device, shape),
+        0 if mean is None else _vector(mean, "mean", _F32, device, rows),
+        0 if rstd is None else _vector(rstd, "rstd", _F32, device, rows),
+        *((0, 0) if checkpoint is None else _held(checkpoint, device, rows, n)))
+    _check(_lib.load().layer_norm_forward(a, rows, n, eps, code, stream), "layer_norm_forward")
     return y
 
 
@@ -375,36 +385,29 @@ def layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, *, residu
     ``x`` is the forward's x, or the checkpoint (codes, scales) of the norm's input; ``dx`` may be ``dy``.
     ``workspace``: ``layer_norm_backward_workspace(rows, n)`` bytes, allocated if not given.
     """
-    rows, n = shape = _matrix(dy, "dy")
-    code = _code(dy)
-    a = _lib.LayerNormBackward()
-    a.dy, a.ldg = _rows(dy, "dy", dy, shape)
+    shape, dtype, code, device, stream = _first(dy, "dy")
+    rows, n = shape
     if isinstance(x, torch.Tensor):
-        a.x, a.ldx = _rows(x, "x", dy, shape)
-        if residual is not None:
-            a.residual, a.ldr = _rows(residual, "residual", dy, shape)
+        inputs = (*_rows(x, "x", dtype, device, shape),
+                  *((0, 0) if residual is None else _rows(residual, "residual", dtype, device, shape)), 0, 0)
     else:
         if residual is not None:
             raise ValueError("a checkpoint is of the norm's input, residual included")
-        a.checkpoint = _held(x, dy, rows, n)
-    a.weight = _vector(weight, "weight", dy, n, torch.float32)
-    a.mean = _vector(mean, "mean", dy, rows, torch.float32)
-    a.rstd = _vector(rstd, "rstd", dy, rows, torch.float32)
-    a.dx, a.ldd = _rows(dx, "dx", dy, shape)
-    a.dweight = _vector(dweight, "dweight", dy, n, torch.float32)
-    a.dbias = _vector(dbias, "dbias", dy, n, torch.float32)
-    lib = _lib.load()
-    _keep, a.workspace, a.workspace_bytes = _scratch(lib.layer_norm_backward_workspace(rows, n), workspace, dy,
-                                                     "layer_norm_backward")
-    _check(lib.layer_norm_backward(ctypes.byref(a), rows, n, code, _stream(dy)), "layer_norm_backward")
+        inputs = (0, 0, 0, 0, *_held(x, device, rows, n))
+    keep, scratch, size = _scratch(_need("layer_norm_backward_workspace", rows, n), workspace, device,
+                                   "layer_norm_backward")
+    a = _lib.pack["layer_norm_backward"](
+        *_rows(dy, "dy", dtype, device, shape), *inputs, _vector(weight, "weight", _F32, device, n),
+        _vector(mean, "mean", _F32, device, rows), _vector(rstd, "rstd", _F32, device, rows),
+        *_rows(dx, "dx", dtype, device, shape), _vector(dweight, "dweight", _F32, device, n),
+        _vector(dbias, "dbias", _F32, device, n), scratch, size)
+    _check(_lib.load().layer_norm_backward(a, rows, n, code, stream), "layer_norm_backward")
     return dx, dweight, dbias
 
 
 def layer_norm_backward_workspace(rows: int, n: int) -> int:
-    need = int(_lib.load().layer_norm_backward_workspace(rows, n))
-    if need < 0:
-        _check(need, "layer_norm_backward_workspace")
-    return need
+    """Bytes of workspace that ``layer_norm_backward`` needs."""
+    return _need("layer_norm_backward_workspace", rows, n)
 
 
 def _activation(name: str) -> int:
@@ -420,30 +423,26 @@ def linear_forward(x, w, y, *, bias=None, activation="none", residual=None, chec
     ``checkpoint``, of the pre-activation, is written if given.  ``y`` may be ``residual``.
     ``workspace``: ``linear_forward_workspace(...)`` bytes, allocated if not given.
     """
-    tokens, d_in = _matrix(x, "x")
-    d_out = _matrix(w, "w")[0]
-    code, act = _code(x), _activation(activation)
-    a = _lib.LinearForward()
-    a.x, a.ldx = _rows(x, "x", x, (tokens, d_in))
-    a.w, a.ldw = _rows(w, "w", x, (d_out, d_in))
-    if bias is not None:
-        a.bias = _vector(bias, "bias", x, d_out, x.dtype)
-    if residual is not None:
-        a.residual, a.ldr = _rows(residual, "residual", x, (tokens, d_out))
-    a.y, a.ldy = _rows(y, "y", x, (tokens, d_out))
-    a.checkpoint = _held(checkpoint, x, tokens, d_out)
-    lib = _lib.load()
-    _keep, a.workspace, a.workspace_bytes = _scratch(lib.linear_forward_workspace(d_in, d_out, tokens, code), workspace,
-                                                     x, "linear_forward")
-    _check(lib.linear_forward(ctypes.byref(a), d_in, d_out, tokens, act, code, _stream(x)), "linear_forward")
+    shape, dtype, code, device, stream = _first(x, "x")
+    tokens, d_in = shape
+    d_out = w.shape[0]
+    act = _activation(activation)
+    out = (tokens, d_out)
+    keep, scratch, size = _scratch(_need("linear_forward_workspace", d_in, d_out, tokens, code), workspace, device,
+                                   "linear_forward")
+    a = _lib.pack["linear_forward"](
+        *_rows(x, "x", dtype, device, shape), *_rows(w, "w", dtype, device, (d_out, d_in)),
+        0 if bias is None else _vector(bias, "bias", dtype, device, d_out),
+        *((0, 0) if residual is None else _rows(residual, "residual", dtype, device, out)),
+        *_rows(y, "y", dtype, device, out),
+        *((0, 0) if checkpoint is None else _held(checkpoint, device, tokens, d_out)), scratch, size)
+    _check(_lib.load().linear_forward(a, d_in, d_out, tokens, act, code, stream), "linear_forward")
     return y
 
 
 def linear_forward_workspace(d_in: int, d_out: int, tokens: int, dtype: torch.dtype) -> int:
-    need = int(_lib.load().linear_forward_workspace(d_in, d_out, tokens, _CODES[dtype]))
-    if need < 0:
-        _check(need, "linear_forward_workspace")
-    return need
+    """Bytes of workspace that ``linear_forward`` needs (0: none)."""
+    return _need("linear_forward_workspace", d_in, d_out, tokens, _CODES[dtype])
 
 
 def linear_backward(dy, x, w, *, dx=None, dw=None, db=None, activation="none", checkpoint=None, add=None,
@@ -453,48 +452,45 @@ def linear_backward(dy, x, w, *, dx=None, dw=None, db=None, activation="none", c
     z is what ``checkpoint`` stands for (not needed without an activation).  ``x`` may be None without dw, ``w``
     without dx; ``dx`` may be ``add``.  ``workspace``: ``linear_backward_workspace(...)`` bytes, allocated if not given.
     """
-    tokens, d_out = _matrix(dy, "dy")
-    code, act = _code(dy), _activation(activation)
-    a = _lib.LinearBackward()
-    a.dy, a.ldg = _rows(dy, "dy", dy, (tokens, d_out))
-    d_in = None
-    for t, name, other in ((dx, "dx", w), (dw, "dw", x)):
-        if t is not None:
-            if other is None:
-                raise ValueError("dx needs w" if name == "dx" else "dw needs x")
-            width = _matrix(t, name)[1]
-            if d_in is not None and width != d_in:
-                raise ValueError(f"dx and dw have {d_in} and {width} columns")
-            d_in = width
+    shape, dtype, code, device, stream = _first(dy, "dy")
+    tokens, d_out = shape
+    act = _activation(activation)
+    d_in = 1  # (db alone)
     if dx is not None:
-        a.dx, a.ldd = _rows(dx, "dx", dy, (tokens, d_in))
-        a.w, a.ldw = _rows(w, "w", dy, (d_out, d_in))
-        if add is not None:
-            a.add, a.lda = _rows(add, "add", dy, (tokens, d_in))
+        if w is None:
+            raise ValueError("dx needs w")
+        d_in = dx.shape[-1]
     if dw is not None:
-        a.dw, a.lddw = _rows(dw, "dw", dy, (d_out, d_in))
-        a.x, a.ldx = _rows(x, "x", dy, (tokens, d_in))
-    if db is not None:
-        a.db = _vector(db, "db", dy, d_out, dy.dtype)
+        if x is None:
+            raise ValueError("dw needs x")
+        if dx is not None and dw.shape[-1] != d_in:
+            raise ValueError(f"dx and dw have {d_in} and {dw.shape[-1]} columns")
+        d_in = dw.shape[-1]
+    held = (0, 0)
     if act != _lib.RDFFT_ACT_NONE:
         if checkpoint is None:
             raise ValueError(f"the gradient through {activation} needs the checkpoint of the pre-activation")
-        a.checkpoint = _held(checkpoint, dy, tokens, d_out)
-    d_in = 1 if d_in is None else d_in  # (db alone)
-    lib = _lib.load()
-    need = lib.linear_backward_workspace(d_in, d_out, tokens, dx is not None, dw is not None, db is not None, act, code)
-    _keep, a.workspace, a.workspace_bytes = _scratch(need, workspace, dy, "linear_backward")
-    _check(lib.linear_backward(ctypes.byref(a), d_in, d_out, tokens, act, code, _stream(dy)), "linear_backward")
+        held = _held(checkpoint, device, tokens, d_out)
+    none = (0, 0)
+    keep, scratch, size = _scratch(
+        _need("linear_backward_workspace", d_in, d_out, tokens, dx is not None, dw is not None, db is not None, act, code),
+        workspace, device, "linear_backward")
+    a = _lib.pack["linear_backward"](
+        *_rows(dy, "dy", dtype, device, shape), *held,
+        *(none if dw is None else _rows(x, "x", dtype, device, (tokens, d_in))),
+        *(none if dx is None else _rows(w, "w", dtype, device, (d_out, d_in))),
+        *(none if dx is None or add is None else _rows(add, "add", dtype, device, (tokens, d_in))),
+        *(none if dx is None else _rows(dx, "dx", dtype, device, (tokens, d_in))),
+        *(none if dw is None else _rows(dw, "dw", dtype, device, (d_out, d_in))),
+        0 if db is None else _vector(db, "db", dtype, device, d_out), scratch, size)
+    _check(_lib.load().linear_backward(a, d_in, d_out, tokens, act, code, stream), "linear_backward")
     return dx, dw, db
 
 
 def linear_backward_workspace(d_in: int, d_out: int, tokens: int, dtype: torch.dtype, activation: str = "none", *,
                               dx: bool = True, dw: bool = True, db: bool = True) -> int:
-    need = int(_lib.load().linear_backward_workspace(d_in, d_out, tokens, dx, dw, db, _activation(activation),
-                                                     _CODES[dtype]))
-    if need < 0:
-        _check(need, "linear_backward_workspace")
-    return need
+    """Bytes of workspace that ``linear_backward`` needs for the gradients that are wanted."""
+    return _need("linear_backward_workspace", d_in, d_out, tokens, dx, dw, db, _activation(activation), _CODES[dtype])
 
 
 def rdfft_init() -> None:

@@ -45,12 +45,40 @@ __device__ __forceinline__ void group_sums(float* v, float* red, int& turn) {
   }
 }
 
+// Eight values of a row from i0, zeros past its end.  EXACT: n is a multiple of eight, so a group is in the
+// row or out of it and its load needs no branch (an absent group's reads the row's start).
+template <class E, bool EXACT>
+struct RowGroup {
+  using T = typename E::T;
+  typename E::Raw raw;
+  __device__ __forceinline__ void load(const T* row, int i0, int n) {
+    if constexpr (EXACT) raw = E::load(row + (i0 < n ? i0 : 0));
+  }
+  __device__ __forceinline__ void widen(const T* row, int i0, int n, float* v) const {
+    if constexpr (EXACT) {
+      E::widen(raw, v);
+#pragma unroll
+      for (int k = 0; k < kVec; ++k) v[k] = i0 < n ? v[k] : 0.f;
+    } else {
+      read_group<E>(row, i0, n, v);
+    }
+  }
+};
+template <class E, bool EXACT>
+__device__ __forceinline__ void store_group(typename E::T* row, int i0, int n, const float* v) {
+  if constexpr (EXACT) {
+    if (i0 < n) E::store(row + i0, v);
+  } else {
+    write_group<E>(row, i0, n, v);
+  }
+}
+
 template <int TPR>
 constexpr int norm_fwd_wg() {
   return TPR > 256 ? TPR : 256;
 }
 
-template <class E, int TPR, int C>
+template <class E, int TPR, int C, bool EXACT>
 __global__ void __launch_bounds__(norm_fwd_wg<TPR>()) layer_norm_forward_kernel(NormArgs a) {
   using T = typename E::T;
   constexpr int WG = norm_fwd_wg<TPR>(), GROUPS = TPR > 64 ? 1 : WG / TPR;
@@ -58,14 +86,15 @@ __global__ void __launch_bounds__(norm_fwd_wg<TPR>()) layer_norm_forward_kernel(
   __shared__ float red[2 * (WG / 64)];
   int turn = 0;
   const int lane = threadIdx.x % TPR;
-  const int64_t n = a.n;
+  const int n = (int)a.n, blocks = (n + kCkBlock - 1) / kCkBlock;
   const float count = (float)n;
+  int at[C];
   float w[C][kVec], b[C][kVec];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    const int64_t i = (int64_t)(c * TPR + lane) * kVec;
-    read_group<ElemF32>(a.weight, i, n, w[c]);
-    if (a.bias != nullptr) read_group<ElemF32>(a.bias, i, n, b[c]);
+    at[c] = (c * TPR + lane) * kVec;
+    read_group<ElemF32>(a.weight, at[c], n, w[c]);
+    if (a.bias != nullptr) read_group<ElemF32>(a.bias, at[c], n, b[c]);
     else
 #pragma unroll
       for (int k = 0; k < kVec; ++k) b[c][k] = 0.f;
@@ -73,39 +102,24 @@ __global__ void __launch_bounds__(norm_fwd_wg<TPR>()) layer_norm_forward_kernel(
   const int64_t step = (int64_t)gridDim.x * GROUPS;
   for (int64_t row = (int64_t)blockIdx.x * GROUPS + threadIdx.x / TPR; row < a.rows; row += step) {
     const T* const x = static_cast<const T*>(a.x) + row * a.ldx;
+    const T* const r = static_cast<const T*>(a.residual) + row * a.ldr;
     float u[C][kVec];
-    if (n >= kVec) {
-      typename E::Raw raw[C], more[C];
+    RowGroup<E, EXACT> xs[C], rs[C];
 #pragma unroll
-      for (int c = 0; c < C; ++c) raw[c] = load_group<E>(x, (int64_t)(c * TPR + lane) * kVec, n);
-      if (a.residual != nullptr) {
-        const T* const r = static_cast<const T*>(a.residual) + row * a.ldr;
+    for (int c = 0; c < C; ++c) xs[c].load(x, at[c], n);
+    if (a.residual != nullptr) {
 #pragma unroll
-        for (int c = 0; c < C; ++c) more[c] = load_group<E>(r, (int64_t)(c * TPR + lane) * kVec, n);
+      for (int c = 0; c < C; ++c) rs[c].load(r, at[c], n);
+    }
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const int64_t i = (int64_t)(c * TPR + lane) * kVec;
-          float v[kVec];
-          widen_group<E>(raw[c], x, i, n, u[c]);
-          widen_group<E>(more[c], r, i, n, v);
-#pragma unroll
-          for (int k = 0; k < kVec; ++k) u[c][k] += v[k];
-        }
-      } else {
-#pragma unroll
-        for (int c = 0; c < C; ++c) widen_group<E>(raw[c], x, (int64_t)(c * TPR + lane) * kVec, n, u[c]);
-      }
-    } else {
+    for (int c = 0; c < C; ++c) xs[c].widen(x, at[c], n, u[c]);
+    if (a.residual != nullptr) {
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        const int64_t i = (int64_t)(c * TPR + lane) * kVec;
-        read_group<E>(x, i, n, u[c]);
-        if (a.residual != nullptr) {
-          float v[kVec];
-          read_group<E>(static_cast<const T*>(a.residual) + row * a.ldr, i, n, v);
+        float v[kVec];
+        rs[c].widen(r, at[c], n, v);
 #pragma unroll
-          for (int k = 0; k < kVec; ++k) u[c][k] += v[k];
-        }
+        for (int k = 0; k < kVec; ++k) u[c][k] += v[k];
       }
     }
     float s[1] = {0.f};
@@ -114,31 +128,29 @@ __global__ void __launch_bounds__(norm_fwd_wg<TPR>()) layer_norm_forward_kernel(
 #pragma unroll
       for (int k = 0; k < kVec; ++k) s[0] += u[c][k];
     group_sums<TPR, 1>(s, red, turn);
-    const float mean = s[0] / count;
+    const float mean = s[0] / count;  // (not times 1 / n: a constant row's mean is its value)
     if (a.ck.codes != nullptr) {
-      const int64_t blocks = (n + kCkBlock - 1) / kCkBlock;
+      int8_t* const codes = a.ck.codes + row * n;
+      uint8_t* const scales = a.ck.scales + row * blocks;
 #pragma unroll
-      for (int c = 0; c < C; ++c)
-        write_checkpoint(a.ck.codes + row * n, a.ck.scales + row * blocks, (int64_t)(c * TPR + lane) * kVec, n, u[c]);
-    }
-    s[0] = 0.f;
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int64_t i = (int64_t)(c * TPR + lane) * kVec;
-      if (i + kVec <= n) {
-#pragma unroll
-        for (int k = 0; k < kVec; ++k) {
-          u[c][k] -= mean;
-          s[0] = fmaf(u[c][k], u[c][k], s[0]);
-        }
-      } else {
-#pragma unroll
-        for (int k = 0; k < kVec; ++k) {
-          u[c][k] = i + k < n ? u[c][k] - mean : 0.f;
-          s[0] = fmaf(u[c][k], u[c][k], s[0]);
+      for (int c = 0; c < C; ++c) {
+        const int byte = ck_scale_byte(quad_max(max_bits8(u[c])));
+        if (at[c] < n) {
+          if constexpr (EXACT) *reinterpret_cast<Bytes8*>(codes + at[c]) = ck_encode(u[c], byte);
+          else write_codes(codes, at[c], n, ck_encode(u[c], byte));
+          if (at[c] % kCkBlock == 0) scales[at[c] / kCkBlock] = (uint8_t)byte;
         }
       }
     }
+    s[0] = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int k = 0; k < kVec; ++k) {
+        const bool in = EXACT ? at[c] < n : at[c] + k < n;
+        u[c][k] = in ? u[c][k] - mean : 0.f;
+        s[0] = fmaf(u[c][k], u[c][k], s[0]);
+      }
     group_sums<TPR, 1>(s, red, turn);
     const float rstd = 1.0f / sqrtf(s[0] / count + a.eps);
     if (lane == 0) {
@@ -151,121 +163,134 @@ __global__ void __launch_bounds__(norm_fwd_wg<TPR>()) layer_norm_forward_kernel(
       float v[kVec];
 #pragma unroll
       for (int k = 0; k < kVec; ++k) v[k] = fmaf(u[c][k] * rstd, w[c][k], b[c][k]);
-      write_group<E>(y, (int64_t)(c * TPR + lane) * kVec, n, v);
+      store_group<E, EXACT>(y, at[c], n, v);
     }
   }
 }
 
-template <int TPR>
-constexpr int norm_bwd_wg() {
-  return TPR > 256 ? TPR : 1024;
+constexpr int kNormBwdWG = 1024;
+template <int TPR, int C>
+constexpr int norm_bwd_lds() {
+  const int groups = kNormBwdWG / TPR;
+  return groups == 1 ? 0 : groups * 2 * TPR * C * kVec * 4;
 }
 
+// A row's dy and the norm's input (or its checkpoint), on their way from memory
+template <class E, int TPR, int C, bool CK, bool EXACT>
+struct NormRow {
+  using T = typename E::T;
+  RowGroup<E, EXACT> dy[C], x[CK ? 1 : C], r[CK ? 1 : C];
+  Bytes8 codes[CK ? C : 1];
+  int scale[CK ? C : 1];
+  float mean, rstd;
+
+  __device__ __forceinline__ void load(const NormGradArgs& a, int64_t row, const int* at, int n, int blocks) {
+    mean = a.mean[row];
+    rstd = a.rstd[row];
+    if constexpr (EXACT) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        dy[c].load(static_cast<const T*>(a.dy) + row * a.ldg, at[c], n);
+        const int i = at[c] < n ? at[c] : 0;
+        if constexpr (CK) {
+          codes[c] = *reinterpret_cast<const Bytes8*>(a.ck.codes + row * n + i);
+          scale[c] = a.ck.scales[row * blocks + i / kCkBlock];
+        } else {
+          x[c].load(static_cast<const T*>(a.x) + row * a.ldx, at[c], n);
+          if (a.residual != nullptr) r[c].load(static_cast<const T*>(a.residual) + row * a.ldr, at[c], n);
+        }
+      }
+    }
+  }
+  // g: dy, u: the norm's input
+  __device__ __forceinline__ void widen(const NormGradArgs& a, int64_t row, const int* at, int n, int blocks,
+                                        float (*g)[kVec], float (*u)[kVec]) const {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      dy[c].widen(static_cast<const T*>(a.dy) + row * a.ldg, at[c], n, g[c]);
+      if constexpr (CK && EXACT) {
+        ck_decode(codes[c], ck_scale(scale[c]), u[c]);
+      } else if constexpr (CK) {
+        const int s = at[c] < n ? a.ck.scales[row * blocks + at[c] / kCkBlock] : 0;
+        ck_decode(tail_codes(a.ck.codes + row * n, at[c], n), ck_scale(s), u[c]);
+      } else {
+        x[c].widen(static_cast<const T*>(a.x) + row * a.ldx, at[c], n, u[c]);
+        if (a.residual != nullptr) {
+          float v[kVec];
+          r[c].widen(static_cast<const T*>(a.residual) + row * a.ldr, at[c], n, v);
+#pragma unroll
+          for (int k = 0; k < kVec; ++k) u[c][k] += v[k];
+        }
+      }
+    }
+  }
+};
+
 // Each workgroup's sums go to dw_out + blockIdx.x * stride and db_out + blockIdx.x * stride.
-template <class E, int TPR, int C, bool CK>
-__global__ void __launch_bounds__(norm_bwd_wg<TPR>())
+template <class E, int TPR, int C, bool CK, bool EXACT>
+__global__ void __launch_bounds__(kNormBwdWG)
     layer_norm_backward_kernel(NormGradArgs a, float* dw_out, float* db_out, int64_t stride) {
   using T = typename E::T;
-  constexpr int WG = norm_bwd_wg<TPR>(), GROUPS = WG / TPR;
+  constexpr int WG = kNormBwdWG, GROUPS = WG / TPR;
   __shared__ float red[4 * (WG / 64)];
   int turn = 0;
   const int lane = threadIdx.x % TPR, grp = threadIdx.x / TPR;
-  const int64_t n = a.n, blocks = (n + kCkBlock - 1) / kCkBlock;
-  const float count = (float)n;
+  const int n = (int)a.n, blocks = (n + kCkBlock - 1) / kCkBlock;
+  const float inv_n = 1.0f / (float)n;
+  int at[C];
   float w[C][kVec], dw[C][kVec], db[C][kVec];
+  NormRow<E, TPR, C, CK, EXACT> next;
+  const int64_t step = (int64_t)gridDim.x * GROUPS;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    read_group<ElemF32>(a.weight, (int64_t)(c * TPR + lane) * kVec, n, w[c]);
+    at[c] = (c * TPR + lane) * kVec;
+    read_group<ElemF32>(a.weight, at[c], n, w[c]);
 #pragma unroll
     for (int k = 0; k < kVec; ++k) dw[c][k] = db[c][k] = 0.f;
   }
-  const int64_t step = (int64_t)gridDim.x * GROUPS;
+  // the next row is on its way while this one is worked on, where the registers hold both
+  constexpr bool AHEAD = C == 1;
+  int64_t row = (int64_t)blockIdx.x * GROUPS + grp;
+  if (AHEAD && row < a.rows) next.load(a, row, at, n, blocks);
   // (the groups of a workgroup take the same number of rows: they meet at barriers)
-  for (int64_t row0 = (int64_t)blockIdx.x * GROUPS; row0 < a.rows; row0 += step) {
-    const int64_t row = row0 + grp;
+  for (int64_t row0 = (int64_t)blockIdx.x * GROUPS; row0 < a.rows; row0 += step, row += step) {
     const bool act = row < a.rows;
-    float xh[C][kVec], g[C][kVec];
+    float u[C][kVec], g[C][kVec];
     float mean = 0.f, rstd = 0.f;
-    const T* const dy = static_cast<const T*>(a.dy) + (act ? row : 0) * a.ldg;
     if (act) {
-      mean = a.mean[row];
-      rstd = a.rstd[row];
-      if constexpr (CK) {
-        const int8_t* const codes = a.ck.codes + row * n;
-        const uint8_t* const scales = a.ck.scales + row * blocks;
-        if (n >= kVec) {
-          typename E::Raw raw[C];
-          Bytes8 held[C];
-          int sc[C];
-#pragma unroll
-          for (int c = 0; c < C; ++c) {
-            const int64_t i = (int64_t)(c * TPR + lane) * kVec;
-            raw[c] = load_group<E>(dy, i, n);
-            held[c] = load_codes(codes, i, n);
-            sc[c] = scales[i < n ? i / kCkBlock : 0];
-          }
-#pragma unroll
-          for (int c = 0; c < C; ++c) {
-            const int64_t i = (int64_t)(c * TPR + lane) * kVec;
-            widen_group<E>(raw[c], dy, i, n, g[c]);
-            if (i + kVec > n) held[c] = tail_codes(codes, i, n);
-            ck_decode(held[c], ck_scale(sc[c]), xh[c]);
-          }
-        } else {
-#pragma unroll
-          for (int c = 0; c < C; ++c) {
-            const int64_t i = (int64_t)(c * TPR + lane) * kVec;
-            read_group<E>(dy, i, n, g[c]);
-            ck_decode(tail_codes(codes, i, n), ck_scale(scales[0]), xh[c]);
-          }
-        }
-      } else {
-        const T* const x = static_cast<const T*>(a.x) + row * a.ldx;
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const int64_t i = (int64_t)(c * TPR + lane) * kVec;
-          read_group<E>(dy, i, n, g[c]);
-          read_group<E>(x, i, n, xh[c]);
-        }
-        if (a.residual != nullptr) {
-          const T* const r = static_cast<const T*>(a.residual) + row * a.ldr;
-#pragma unroll
-          for (int c = 0; c < C; ++c) {
-            float v[kVec];
-            read_group<E>(r, (int64_t)(c * TPR + lane) * kVec, n, v);
-#pragma unroll
-            for (int k = 0; k < kVec; ++k) xh[c][k] += v[k];
-          }
-        }
-      }
+      if constexpr (!AHEAD) next.load(a, row, at, n, blocks);
+      mean = next.mean;
+      rstd = next.rstd;
+      next.widen(a, row, at, n, blocks, g, u);
+      if (AHEAD && row + step < a.rows) next.load(a, row + step, at, n, blocks);
     } else {
 #pragma unroll
       for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int k = 0; k < kVec; ++k) g[c][k] = xh[c][k] = 0.f;
+        for (int k = 0; k < kVec; ++k) g[c][k] = u[c][k] = 0.f;
     }
     float s[2] = {0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int k = 0; k < kVec; ++k) {
-        xh[c][k] = (xh[c][k] - mean) * rstd;
-        dw[c][k] = fmaf(g[c][k], xh[c][k], dw[c][k]);
+        u[c][k] = (u[c][k] - mean) * rstd;
+        dw[c][k] = fmaf(g[c][k], u[c][k], dw[c][k]);
         db[c][k] += g[c][k];
         g[c][k] *= w[c][k];
         s[0] += g[c][k];
-        s[1] = fmaf(g[c][k], xh[c][k], s[1]);
+        s[1] = fmaf(g[c][k], u[c][k], s[1]);
       }
     group_sums<TPR, 2>(s, red, turn);
     if (!act) continue;
-    const float m0 = s[0] / count, m1 = s[1] / count;
+    const float m0 = s[0] * inv_n, m1 = s[1] * inv_n;
     T* const dx = static_cast<T*>(a.dx) + row * a.ldd;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       float v[kVec];
 #pragma unroll
-      for (int k = 0; k < kVec; ++k) v[k] = rstd * (g[c][k] - m0 - xh[c][k] * m1);
-      write_group<E>(dx, (int64_t)(c * TPR + lane) * kVec, n, v);
+      for (int k = 0; k < kVec; ++k) v[k] = rstd * (g[c][k] - m0 - u[c][k] * m1);
+      store_group<E, EXACT>(dx, at[c], n, v);
     }
   }
   dw_out += blockIdx.x * stride;
@@ -273,54 +298,50 @@ __global__ void __launch_bounds__(norm_bwd_wg<TPR>())
   if constexpr (GROUPS == 1) {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int64_t i = (int64_t)(c * TPR + lane) * kVec;
-      write_group<ElemF32>(dw_out, i, n, dw[c]);
-      write_group<ElemF32>(db_out, i, n, db[c]);
+      write_group<ElemF32>(dw_out, at[c], n, dw[c]);
+      write_group<ElemF32>(db_out, at[c], n, db[c]);
     }
   } else {
     constexpr int COLS = TPR * C * kVec;
-    __shared__ float sums[2 * COLS];
-    for (int o = 0; o < GROUPS; ++o) {
-      if (grp == o) {
+    extern __shared__ float sums[];  // [GROUPS][2][COLS]
 #pragma unroll
-        for (int c = 0; c < C; ++c)
+    for (int c = 0; c < C; ++c)
 #pragma unroll
-          for (int k = 0; k < kVec; ++k) {
-            // value k of all lanes side by side: no two lanes of a wave meet in a bank
-            const int at = (c * kVec + k) * TPR + lane;
-            sums[at] = o == 0 ? dw[c][k] : sums[at] + dw[c][k];
-            sums[COLS + at] = o == 0 ? db[c][k] : sums[COLS + at] + db[c][k];
-          }
+      for (int k = 0; k < kVec; ++k) {
+        // value k of all lanes side by side: no two lanes of a wave meet in a bank
+        sums[grp * 2 * COLS + (c * kVec + k) * TPR + lane] = dw[c][k];
+        sums[grp * 2 * COLS + COLS + (c * kVec + k) * TPR + lane] = db[c][k];
       }
-      __syncthreads();
-    }
-    for (int64_t i = threadIdx.x; i < n; i += WG) {
-      const int at = (int)((i / (TPR * kVec) * kVec + i % kVec) * TPR + i / kVec % TPR);
-      dw_out[i] = sums[at];
-      db_out[i] = sums[COLS + at];
+    __syncthreads();
+    for (int p = threadIdx.x; p < 2 * COLS; p += WG) {
+      float v = sums[p];
+#pragma unroll
+      for (int o = 1; o < GROUPS; ++o) v += sums[o * 2 * COLS + p];
+      const int q = p % COLS, i = (q / TPR / kVec * TPR + q % TPR) * kVec + q / TPR % kVec;
+      if (i < n) (p < COLS ? dw_out : db_out)[i] = v;
     }
   }
 }
 
-// Sixteen waves share 64 columns; wave k adds rows k, k + 16, ...
-constexpr int kFinishWaves = 16;
+// 32 threads along the columns (a cache line), 32 of them to a column: thread k adds rows k, k + 32, ...
+constexpr int kFinishCols = 32, kFinishRows = 32;
 template <class E>
-__global__ void __launch_bounds__(64 * kFinishWaves)
+__global__ void __launch_bounds__(kFinishCols * kFinishRows)
     column_finish_kernel(const float* __restrict__ partials, int64_t groups, int64_t cols, int64_t n,
                          typename E::T* __restrict__ out0, typename E::T* __restrict__ out1) {
-  __shared__ float part[kFinishWaves][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-  const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+  __shared__ float part[kFinishRows][kFinishCols + 1];
+  const int x = threadIdx.x % kFinishCols, y = threadIdx.x / kFinishCols;
+  const int64_t c = (int64_t)blockIdx.x * kFinishCols + x;
   float s = 0.f;
   if (c < cols) {
 #pragma unroll 8
-    for (int64_t g = wave; g < groups; g += kFinishWaves) s += partials[g * cols + c];
+    for (int64_t g = y; g < groups; g += kFinishRows) s += partials[g * cols + c];
   }
-  part[wave][lane] = s;
+  part[y][x] = s;
   __syncthreads();
-  if (wave != 0 || c >= cols) return;
+  if (y != 0 || c >= cols) return;
 #pragma unroll
-  for (int w = 1; w < kFinishWaves; ++w) s += part[w][lane];
+  for (int w = 1; w < kFinishRows; ++w) s += part[w][x];
   if (c < n) E::put(out0 + c, s);
   else E::put(out1 + (c - n), s);
 }
@@ -329,7 +350,8 @@ hipError_t launch_column_finish(const float* partials, int64_t groups, int64_t c
                                 int storage, hipStream_t stream) {
   return with_elem(storage, [&](auto e) {
     using E = decltype(e);
-    hipLaunchKernelGGL(column_finish_kernel<E>, dim3((unsigned)((cols + 63) / 64)), dim3(64 * kFinishWaves), 0, stream,
+    hipLaunchKernelGGL(column_finish_kernel<E>, dim3((unsigned)((cols + kFinishCols - 1) / kFinishCols)),
+                       dim3(kFinishCols * kFinishRows), 0, stream,
                        partials, groups, cols, n, static_cast<typename E::T*>(out0), static_cast<typename E::T*>(out1));
     return hipGetLastError();
   });
@@ -348,15 +370,38 @@ static hipError_t with_row(int64_t n, F&& fn) {
   return go(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
 }
 
+// The backward has 1024 threads to a workgroup and so 128 registers: one group of eight to a thread.
+template <class F>
+static hipError_t with_row_backward(int64_t n, F&& fn) {
+  using std::integral_constant;
+  const auto go = [&](auto tpr, auto c) { return fn(tpr, c); };
+  if (n <= 512) return go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+  if (n <= 1024) return go(integral_constant<int, 128>{}, integral_constant<int, 1>{});
+  if (n <= 2048) return go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+  if (n <= 4096) return go(integral_constant<int, 512>{}, integral_constant<int, 1>{});
+  if (n <= 8192) return go(integral_constant<int, 1024>{}, integral_constant<int, 1>{});
+  return go(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+}
+
+// whether rows are loaded and stored in whole groups only
+static bool exact_rows(int64_t n) { return n % kVec == 0; }
+template <class F>
+static hipError_t with_exact(int64_t n, F&& fn) {
+  return exact_rows(n) ? fn(std::true_type{}) : fn(std::false_type{});
+}
+
 hipError_t launch_layer_norm_forward(const NormArgs& a, hipStream_t stream, int num_cu) {
   return with_elem(a.storage, [&](auto e) {
     return with_row(a.n, [&](auto tpr, auto c) {
-      constexpr int TPR = decltype(tpr)::value, C = decltype(c)::value, WG = norm_fwd_wg<TPR>();
-      constexpr int groups = TPR > 64 ? 1 : WG / TPR;
-      // as many workgroups as are on the chip at once
-      const int64_t grid = std::min((a.rows + groups - 1) / groups, (int64_t)num_cu * (2048 / WG));
-      hipLaunchKernelGGL((layer_norm_forward_kernel<decltype(e), TPR, C>), dim3((unsigned)grid), dim3(WG), 0, stream, a);
-      return hipGetLastError();
+      return with_exact(a.n, [&](auto exact) {
+        constexpr int TPR = decltype(tpr)::value, C = decltype(c)::value, WG = norm_fwd_wg<TPR>();
+        constexpr int groups = TPR > 64 ? 1 : WG / TPR;
+        // as many workgroups as are on the chip at once
+        const int64_t grid = std::min((a.rows + groups - 1) / groups, (int64_t)num_cu * (2048 / WG));
+        hipLaunchKernelGGL((layer_norm_forward_kernel<decltype(e), TPR, C, decltype(exact)::value>),
+                           dim3((unsigned)grid), dim3(WG), 0, stream, a);
+        return hipGetLastError();
+      });
     });
   });
 }
@@ -366,12 +411,22 @@ hipError_t launch_layer_norm_forward(const NormArgs& a, hipStream_t stream, int 
 constexpr int64_t kNormMaxPartials = 256;
 int64_t norm_partials(int64_t rows, int64_t n) {
   int64_t groups = 1;
-  (void)with_row(n, [&](auto tpr, auto) {
-    constexpr int TPR = decltype(tpr)::value;
-    groups = norm_bwd_wg<TPR>() / TPR;
+  (void)with_row_backward(n, [&](auto tpr, auto) {
+    groups = kNormBwdWG / decltype(tpr)::value;
     return hipSuccess;
   });
   return std::max<int64_t>(1, std::min((rows + groups - 1) / groups, kNormMaxPartials));
+}
+
+template <class E, int TPR, int C, bool CK, bool EXACT>
+static hipError_t backward_launch(const NormGradArgs& a, int64_t grid, float* dw, float* db, hipStream_t stream) {
+  constexpr int lds = norm_bwd_lds<TPR, C>();
+  const auto kernel = layer_norm_backward_kernel<E, TPR, C, CK, EXACT>;
+  static const hipError_t ready = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                                      hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (ready != hipSuccess) return ready;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kNormBwdWG), lds, stream, a, dw, db, 2 * a.n);
+  return hipGetLastError();
 }
 
 hipError_t launch_layer_norm_backward(const NormGradArgs& a, hipStream_t stream) {
@@ -379,17 +434,15 @@ hipError_t launch_layer_norm_backward(const NormGradArgs& a, hipStream_t stream)
   // a single workgroup's sums are the result
   float* const dw = grid == 1 ? a.dweight : a.partials;
   float* const db = grid == 1 ? a.dbias : a.partials + a.n;
-  const int64_t stride = 2 * a.n;
   const hipError_t err = with_elem(a.storage, [&](auto e) {
-    return with_row(a.n, [&](auto tpr, auto c) {
-      constexpr int TPR = decltype(tpr)::value, C = decltype(c)::value, WG = norm_bwd_wg<TPR>();
-      if (a.x == nullptr)
-        hipLaunchKernelGGL((layer_norm_backward_kernel<decltype(e), TPR, C, true>), dim3((unsigned)grid), dim3(WG), 0,
-                           stream, a, dw, db, stride);
-      else
-        hipLaunchKernelGGL((layer_norm_backward_kernel<decltype(e), TPR, C, false>), dim3((unsigned)grid), dim3(WG), 0,
-                           stream, a, dw, db, stride);
-      return hipGetLastError();
+    return with_row_backward(a.n, [&](auto tpr, auto c) {
+      return with_exact(a.n, [&](auto exact) {
+        using E = decltype(e);
+        constexpr int TPR = decltype(tpr)::value, C = decltype(c)::value;
+        constexpr bool EXACT = decltype(exact)::value;
+        return a.x == nullptr ? backward_launch<E, TPR, C, true, EXACT>(a, grid, dw, db, stream)
+                              : backward_launch<E, TPR, C, false, EXACT>(a, grid, dw, db, stream);
+      });
     });
   });
   if (err != hipSuccess || grid == 1) return err;
