@@ -89,12 +89,14 @@ struct GemmArgs {
   int64_t k_split;
   int tiles_m, tiles_n;
 };
-// the tiles that are built, and the instances for one storage type: [tile][operands][load path]
-enum LinearTile { kTile128, kTile256, kLinearTiles };
+// the instances for one storage type; null where one is not built.  Last index: 1 with loads straight to LDS
+enum LinearTile { kTile64, kTile128, kTile128x256, kTile256, kLinearTiles };
 enum LinearOperands { kForward, kGradX, kGradW, kLinearOperands };
 using LinearFn = hipError_t (*)(const GemmArgs&, hipStream_t);
+constexpr int64_t kFewTokens = 64;
 struct LinearTable {
-  LinearFn fn[kLinearTiles][kLinearOperands][2];  // [1]: straight to LDS
+  LinearFn fn[kLinearTiles][kLinearOperands][2];
+  LinearFn few[3][2][2];  // the forward of 16, 32, 64 tokens at most, 16 or 32 rows of W to a workgroup
 };
 LinearTable linear_table_f32();
 LinearTable linear_table_bf16();

@@ -106,32 +106,67 @@ static int64_t slope_parts(int64_t rows, int64_t n) {
 // ----------------------------------------------------------------------------------
 // plans
 
+// What a tile costs, in us, from products of 768 to 8192: a stage (128 bytes of k) where a CU has one workgroup
+// of them, a stage of each where it has more (`together` fit), and what comes before and after.  The largest tile
+// reaches 1390 to 1420 TFLOP/s (16-bit) where its tiles fill the chip in whole rounds; the smaller ones
+// 1270, 1200 and 780, but leave fewer CUs idle: 4096 x 768 x 768 (12 stages) takes 10 us in tiles of 128 or 64 and 15 and 23
+// in the larger two, 2045 x 4096 x 4096 58 us in 128 x 256, 61, 81 and 92 in 128, 256 and 64.
+struct TileCost {
+  int bm, bn, together;
+  double alone, each, ends;
+};
+constexpr TileCost kCost16[kLinearTiles] = {
+    {64, 64, 4, 0.25, 0.175, 3.6}, {128, 128, 2, 0.50, 0.445, 4.0}, {128, 256, 1, 0.82, 0.82, 4.8}, {256, 256, 1, 1.30, 1.30, 13.0}};
+constexpr TileCost kCost32 = {64, 64, 4, 0.62, 0.45, 3.6};
+
 struct Plan {
   LinearTile tile;
   int64_t splits, k_split;
 };
 
-// Tiles of 256 where they fill the chip, else of 128; k is split where even those leave CUs without
-// work, into ranges of four stages at least.
-static Plan plan_of(int64_t m, int64_t n, int64_t k, int storage) {
-  const int64_t bk = kStageBytes / (storage == kStorageF32 ? 4 : 2), stages = (k + bk - 1) / bk;
-  const auto tiles = [&](int64_t b) { return ((m + b - 1) / b) * ((n + b - 1) / b); };
-  if (storage != kStorageF32 && tiles(256) >= kCUs * 3 / 4) return {kTile256, 1, std::max<int64_t>(k, 1)};
-  const int64_t t = std::max<int64_t>(tiles(128), 1);
-  int64_t splits = std::max<int64_t>(1, std::min(kCUs * 2 / t, stages / 4));
-  const int64_t each = std::max<int64_t>(1, (stages + splits - 1) / splits);
-  splits = std::max<int64_t>(1, (stages + each - 1) / each);
-  return {kTile128, splits, each * bk};
+// The tile and the number of k ranges that cost least.  The join of s ranges costs a launch (3 us) and 8 s bytes a
+// result, at 4 TB/s.
+static Plan plan_of(int64_t m, int64_t n, int64_t k, int storage, bool direct) {
+  const bool f32 = storage == kStorageF32;
+  const int64_t bk = kStageBytes / (f32 ? 4 : 2), stages = std::max<int64_t>(1, (k + bk - 1) / bk);
+  Plan best{kTile64, 1, stages * bk};
+  double least = 0;
+  for (int t = 0; t < kLinearTiles; ++t) {
+    if (t != kTile64 && (f32 || (!direct && t != kTile128))) continue;
+    const TileCost& c = f32 ? kCost32 : kCost16[t];
+    const int64_t tiles = ((m + c.bm - 1) / c.bm) * ((n + c.bn - 1) / c.bn);
+    for (int64_t want = 1; want <= 16; ++want) {
+      const int64_t each = (stages + want - 1) / want, splits = (stages + each - 1) / each;
+      if (splits != want) continue;  // (as many ranges of another length)
+      if (splits > 1 && (each < 2 || tiles * splits > 4 * kCUs)) break;
+      const int64_t per_cu = std::max<int64_t>(1, (tiles * splits + kCUs - 1) / kCUs);
+      const double stage = per_cu == 1 ? c.alone : c.each * (double)per_cu;
+      double cost = (double)each * stage + c.ends * (double)((per_cu + c.together - 1) / c.together);
+      if (splits > 1) cost += 3.0 + 8.0 * (double)splits * (double)m * (double)n / 4e6;
+      if (least == 0 || cost < least) {
+        least = cost;
+        best = {(LinearTile)t, splits, each * bk};
+      }
+    }
+  }
+  return best;
 }
+// (whether rows are aligned is not known here: the larger of both plans' needs)
 static int64_t split_bytes(int64_t m, int64_t n, int64_t k, int storage) {
-  const Plan p = plan_of(m, n, k, storage);
-  return p.splits > 1 ? p.splits * m * n * 4 : 0;
+  int64_t most = 0;
+  for (const bool direct : {false, true}) {
+    const Plan p = plan_of(m, n, k, storage, direct);
+    if (p.splits > 1) most = std::max(most, p.splits * m * n * 4);
+  }
+  return most;
 }
 
 static int64_t round_up(int64_t bytes) { return (bytes + 255) & ~(int64_t)255; }
 static int storage_bytes(int storage) { return storage == kStorageF32 ? 4 : 2; }
 
-int64_t linear_forward_workspace(const LinearSizes& s) { return split_bytes(s.tokens, s.d_out, s.d_in, s.storage); }
+int64_t linear_forward_workspace(const LinearSizes& s) {
+  return s.tokens <= kFewTokens ? 0 : split_bytes(s.tokens, s.d_out, s.d_in, s.storage);
+}
 
 // dz, then the partial sums of whichever pass runs (they follow each other on the stream)
 static int64_t slope_bytes(const LinearSizes& s) {
@@ -153,16 +188,21 @@ static bool whole_chunks(const void* p, int64_t ld, int64_t len, int storage) {
 
 static hipError_t product(GemmArgs& g, LinearOperands kind, int storage, void* workspace, hipStream_t stream) {
   static const LinearTable tables[] = {linear_table_f32(), linear_table_bf16(), linear_table_f16()};
-  const Plan p = plan_of(g.m, g.n, g.k, storage);
+  const LinearTable& t = tables[storage];
+  const bool direct = whole_chunks(g.a, g.lda, kind == kGradW ? g.m : g.k, storage) &&
+                      whole_chunks(g.b, g.ldb, kind == kForward ? g.k : g.n, storage);
+  g.splits = 1;
+  if (kind == kForward && g.m <= kFewTokens) {
+    // 32 rows of W to a workgroup where that still fills the chip (x is read half as often: 64 tokens of 8192 x 8192
+    // 22.6 us, else 31.0) or a checkpoint's blocks ask for it; 16 otherwise (one token of 4096 x 4096 4.8 us, else 6.1)
+    const bool wide = g.ck.codes != nullptr || g.n >= 32 * kCUs;
+    return t.few[g.m <= 16 ? 0 : g.m <= 32 ? 1 : 2][wide][direct](g, stream);
+  }
+  const Plan p = plan_of(g.m, g.n, g.k, storage, direct);
   g.splits = (int)p.splits;
   g.k_split = p.k_split;
   g.partial = p.splits > 1 ? static_cast<float*>(workspace) : nullptr;
-  const bool direct = whole_chunks(g.a, g.lda, kind == kGradW ? g.m : g.k, storage) &&
-                      whole_chunks(g.b, g.ldb, kind == kForward ? g.k : g.n, storage);
-  const LinearTable& t = tables[storage];
-  LinearFn fn = t.fn[p.tile][kind][direct];
-  if (fn == nullptr) fn = t.fn[kTile128][kind][direct];
-  const hipError_t e = fn(g, stream);
+  const hipError_t e = t.fn[p.tile][kind][direct](g, stream);
   if (e != hipSuccess || g.partial == nullptr) return e;
   return with_elem(storage, [&](auto elem) { return join<decltype(elem)>(g, stream); });
 }

@@ -130,9 +130,28 @@ __device__ __forceinline__ void load_to_lds(const char* base, uint32_t offset, u
                : "memory", "m0");
 }
 #pragma clang diagnostic pop
-// all loads to LDS done, all LDS reads done, every wave here
+// all but the last LEFT of this wave's loads to LDS done, its LDS reads done, every wave here
+template <int LEFT>
 __device__ __forceinline__ void stage_wait() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  static_assert(LEFT < 64);
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((LEFT & 15) | 7 << 4 | (LEFT >> 4) << 14);  // vmcnt(LEFT) lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// the same within a wave: all but the last LEFT loads to LDS done; its LDS reads done
+template <int LEFT>
+__device__ __forceinline__ void loads_wait() {
+  static_assert(LEFT < 64);
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((LEFT & 15) | 7 << 4 | 15 << 8 | (LEFT >> 4) << 14);  // vmcnt(LEFT)
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void reads_wait() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(15 | 7 << 4 | 3 << 14);  // lgkmcnt(0)
+  asm volatile("" ::: "memory");
 }
 
 // R rows (m or n) of one operand's stage.  ACROSS: memory rows run along m.  DMA: straight to
@@ -178,11 +197,13 @@ struct Operand {
     }
   }
 
-  // starts the loads of the next stage (the LDS region `lds` for DMA) and steps on
+  // starts the loads of the next stage (to the LDS region `lds` for DMA) and steps on.  WHOLE: the stage
+  // is known to lie in front of the end of k.
+  template <bool WHOLE = false>
   __device__ __forceinline__ void fetch(uint32_t lds) {
     if constexpr (DMA) {
       const char* const p = reinterpret_cast<const char*>(base);
-      if (depth >= BK) {
+      if (WHOLE || depth >= BK) {
 #pragma unroll
         for (int j = 0; j < LINES; ++j) load_to_lds(p, offset[j], lds + (uint32_t)(wave * LINES + j) * 1024u);
       } else {
@@ -346,8 +367,9 @@ __device__ __forceinline__ TileAt tile_of(int id, int tiles_m, int tiles_n, int 
   return {first + t % high, t / high, split};
 }
 
-template <class E, int BM, int BN, int WM, int WN, bool AX, bool BX, bool DMA>
-__global__ void __launch_bounds__(WM * WN * 64) linear_kernel(GemmArgs g) {
+template <class E, int BM, int BN, int WM, int WN, int STAGES, bool AX, bool BX, bool DMA>
+__global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2)))  // 256 registers, no second file
+    linear_kernel(GemmArgs g) {
   using T = typename E::T;
   constexpr int WAVES = WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
   constexpr int BK = kStageBytes / (int)sizeof(T);
@@ -378,46 +400,109 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_kernel(GemmArgs g) {
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
+  // Half a stage's fragments (chunk group kk), and their products.  A half is read while the one before it
+  // is multiplied: reads and products are dealt out in turn.
+  struct Half {
+    u32x4 a[FM], b[FN];
+  };
+  const auto read = [&](Half& h, const char* la, int kk) {
+#pragma unroll
+    for (int j = 0; j < FN; ++j) h.b[j] = fb.read(la + OpA::BYTES, j, kk);
+#pragma unroll
+    for (int i = 0; i < FM; ++i) h.a[i] = fa.read(la, i, kk);
+  };
+  const auto multiply = [&](const Half& h) {
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) acc[i][j] = mfma_chunk<E>(h.b[j], h.a[i], acc[i][j]);
+  };
+  // instructions of a half, for the scheduler
+  constexpr int PRODUCTS = FM * FN * (E::kId == kStorageF32 ? 4 : 1);
+  constexpr int READS = FM * (!AX ? 1 : sizeof(T) == 2 ? 2 : 4) + FN * (!BX ? 1 : sizeof(T) == 2 ? 2 : 4);
+  const auto interleave = [&] {
+    constexpr int GROUPS = READS < PRODUCTS ? READS : PRODUCTS;
+#pragma unroll
+    for (int q = 0; q < GROUPS; ++q) {
+      __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS / GROUPS, 0);  // matrix instructions
+      __builtin_amdgcn_sched_group_barrier(0x100, READS / GROUPS, 0);    // LDS reads
+    }
+  };
   const int steps = (int)((k1 - k0 + BK - 1) / BK);
-  if (steps > 0) {
-    a.fetch(lds0);
-    b.fetch(lds0 + OpA::BYTES);
-    a.commit(linear_lds);
-    b.commit(linear_lds + OpA::BYTES);
-    stage_wait();
+  if constexpr (DMA) {
+    // STAGES - 1 stages are under way ahead of the one being multiplied.  The barrier sits
+    // between a stage's two halves: every wave has read all of the stage by then, so that its
+    // region can be loaded anew, and the next stage's first half is read under the second's products.
+    constexpr int EACH = OpA::LINES + OpB::LINES;
+    const auto fetch = [&](int slot, auto whole) {
+      a.template fetch<decltype(whole)::value>(lds0 + (uint32_t)slot * STAGE);
+      b.template fetch<decltype(whole)::value>(lds0 + (uint32_t)slot * STAGE + OpA::BYTES);
+    };
+    Half h0, h1;
+#pragma unroll
+    for (int q = 0; q < STAGES; ++q)
+      if (q < steps) fetch(q, std::false_type{});
+    if (steps > 0) {
+      if (steps >= STAGES) stage_wait<(STAGES - 1) * EACH>();
+      else stage_wait<0>();
+      read(h0, linear_lds, 0);
+    }
+    int cur = 0, t = 0;
+    const auto next = [](int slot) { return slot + 1 == STAGES ? 0 : slot + 1; };
+    for (; t + STAGES < steps - 1; ++t) {  // (the stage that is fetched is not the last)
+      read(h1, linear_lds + cur * STAGE, 1);
+      multiply(h0);
+      interleave();
+      stage_wait<(STAGES - 2) * EACH>();
+      fetch(cur, std::true_type{});
+      cur = next(cur);
+      read(h0, linear_lds + cur * STAGE, 0);
+      multiply(h1);
+      interleave();
+    }
+    for (; t < steps; ++t) {
+      read(h1, linear_lds + cur * STAGE, 1);
+      multiply(h0);
+      if (t + 1 < steps) {
+        // this stage is read; the next has landed when those after it are all that is left
+        if (STAGES > 2 && t + STAGES - 1 < steps) stage_wait<(STAGES - 2) * EACH>();
+        else stage_wait<0>();
+        if (t + STAGES < steps) fetch(cur, std::false_type{});
+        cur = next(cur);
+        read(h0, linear_lds + cur * STAGE, 0);
+      }
+      multiply(h1);
+    }
+  } else {
+    static_assert(DMA || STAGES == 2);
+    if (steps > 0) {
+      a.fetch(0);
+      b.fetch(0);
+    }
+    for (int t = 0; t < steps; ++t) {
+      char* const la = linear_lds + (t & 1) * STAGE;
+      a.commit(la);
+      b.commit(la + OpA::BYTES);
+      // (the other region's last reads lie before the barrier that follows)
+      stage_wait<0>();
+      if (t + 1 < steps) {
+        a.fetch(0);
+        b.fetch(0);
+      }
+      Half h;
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        read(h, la, kk);
+        multiply(h);
+      }
+    }
   }
-  for (int t = 0; t < steps; ++t) {
-    const int cur = t & 1;
-    const char* const la = linear_lds + cur * STAGE;
-    const char* const lb = la + OpA::BYTES;
-    const bool more = t + 1 < steps;
-    if (more) {
-      a.fetch(lds0 + (uint32_t)(cur ^ 1) * STAGE);
-      b.fetch(lds0 + (uint32_t)(cur ^ 1) * STAGE + OpA::BYTES);
-    }
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      u32x4 va[FM], vb[FN];
-#pragma unroll
-      for (int j = 0; j < FN; ++j) vb[j] = fb.read(lb, j, kk);
-#pragma unroll
-      for (int i = 0; i < FM; ++i) va[i] = fa.read(la, i, kk);
-#pragma unroll
-      for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = mfma_chunk<E>(vb[j], va[i], acc[i][j]);
-    }
-    if (more) {
-      a.commit(linear_lds + (cur ^ 1) * STAGE);
-      b.commit(linear_lds + (cur ^ 1) * STAGE + OpA::BYTES);
-    }
-    stage_wait();
-  }
+  stage_wait<0>();
 
   // Each wave turns its results, 16 rows at a time, through LDS of its own into runs of eight
-  // along n: eight lanes then write whole cache lines of D.  (The last stage_wait let go of the LDS.)
+  // along n: eight lanes then write whole cache lines of D.  (No wave reads stages any more.)
   constexpr int PITCH = TN + 4, RUNS = TN / kVec, ROWS = 64 / RUNS;
-  static_assert(WAVES * 16 * PITCH * 4 <= 2 * STAGE && 16 % ROWS == 0);
+  static_assert(WAVES * 16 * PITCH * 4 <= STAGES * STAGE && 16 % ROWS == 0);
   float* const turn = reinterpret_cast<float*>(linear_lds) + wave * 16 * PITCH;
   const int64_t n = n0 + wn * TN + lane % RUNS * kVec;
   float bias[kVec];
@@ -443,10 +528,10 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_kernel(GemmArgs g) {
   }
 }
 
-template <class E, int BM, int BN, int WM, int WN, bool AX, bool BX, bool DMA>
+template <class E, int BM, int BN, int WM, int WN, int STAGES, bool AX, bool BX, bool DMA>
 hipError_t linear_launch(const GemmArgs& g, hipStream_t stream) {
-  constexpr int lds = 2 * (BM + BN) * kStageBytes;
-  const auto kernel = linear_kernel<E, BM, BN, WM, WN, AX, BX, DMA>;
+  constexpr int lds = STAGES * (BM + BN) * kStageBytes;
+  const auto kernel = linear_kernel<E, BM, BN, WM, WN, STAGES, AX, BX, DMA>;
   static const hipError_t ready = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                                       hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (ready != hipSuccess) return ready;
@@ -457,27 +542,191 @@ hipError_t linear_launch(const GemmArgs& g, hipStream_t stream) {
   return hipGetLastError();
 }
 
+// ----------------------------------------------------------------------------------
+// Few tokens (at most 16 MT): y = act(x W^T + b) + r is bound by reading W once.  A workgroup takes 16 NT of
+// W's rows, each of its waves a range of k.  With DMA a wave streams its part of both operands through LDS
+// of its own, STAGES stages of 128 bytes of k a row, without a barrier: whole cache lines, many of them in
+// flight, and no registers held for them.  Without (rows that start anywhere) the fragments come from
+// memory, half a line a row and instruction.  The waves' sums meet in LDS.
+template <class E, int MT, int NT, int WAVES, int STAGES, bool DMA>
+__global__ void __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(2))) linear_few_kernel(GemmArgs g) {
+  using T = typename E::T;
+  constexpr int BK = kStageBytes / (int)sizeof(T), STAGE = 16 * (MT + NT) * kStageBytes;
+  constexpr int PRIVATE = DMA ? STAGES * STAGE : NT * MT * 1024;
+  static_assert(PRIVATE >= NT * MT * 1024);
+  extern __shared__ __attribute__((aligned(1024))) char linear_lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
+  char* const mine = linear_lds + wave * PRIVATE;
+  const int64_t n0 = (int64_t)blockIdx.x * (16 * NT);
+  f32x4 acc[NT][MT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int i = 0; i < MT; ++i) acc[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const auto multiply = [&](const u32x4* w, const u32x4* x) {
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < MT; ++i) acc[j][i] = mfma_chunk<E>(w[j], x[i], acc[j][i]);
+  };
+  const int64_t stages = (g.k + BK - 1) / BK, per = (stages + WAVES - 1) / WAVES * BK;
+  const int64_t k0 = min(wave * per, g.k), k1 = min(k0 + per, g.k);
+
+  if constexpr (DMA) {
+    Operand<E, 16 * NT, 1, false, true> w;
+    Operand<E, 16 * MT, 1, false, true> x;
+    w.init(static_cast<const T*>(g.b), g.ldb, n0, g.n, k0, k1, 0, lane);
+    x.init(static_cast<const T*>(g.a), g.lda, 0, g.m, k0, k1, 0, lane);
+    Fragments<E, 16, false> f;
+    f.init(0, lane);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mine;
+    const int steps = (int)((k1 - k0 + BK - 1) / BK);
+    constexpr int EACH = w.LINES + x.LINES;
+    const auto fetch = [&](int slot) {
+      w.fetch(lds0 + (uint32_t)slot * STAGE);
+      x.fetch(lds0 + (uint32_t)slot * STAGE + w.BYTES);
+    };
+#pragma unroll
+    for (int q = 0; q < STAGES; ++q)
+      if (q < steps) fetch(q);
+    int slot = 0;
+    for (int t = 0; t < steps; ++t) {
+      if (t + STAGES <= steps) loads_wait<(STAGES - 1) * EACH>();
+      else loads_wait<0>();
+      const char* const at = mine + slot * STAGE;
+      u32x4 vw[2][NT], vx[2][MT];
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j) vw[kk][j] = f.read(at, j, kk);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) vx[kk][i] = f.read(at + w.BYTES, i, kk);
+      }
+      if (t + STAGES < steps) {
+        reads_wait();
+        fetch(slot);
+      }
+      slot = slot + 1 == STAGES ? 0 : slot + 1;
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) multiply(vw[kk], vx[kk]);
+    }
+    reads_wait();
+  } else {
+    // rows beyond the last stand for it; their results are not stored
+    constexpr int EPC = 16 / (int)sizeof(T), HALF = BK / 2, U = NT + MT > 4 ? 4 : 8;
+    const int r = lane & 15, grp = lane >> 4;
+    const T *wp[NT], *xp[MT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+      wp[j] = static_cast<const T*>(g.b) + min(n0 + j * 16 + r, g.n - 1) * g.ldb + k0 + grp * EPC;
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+      xp[i] = static_cast<const T*>(g.a) + min((int64_t)(i * 16 + r), g.m - 1) * g.lda + k0 + grp * EPC;
+    const auto whole = [](const T* p) {
+      const Bytes16 v = *reinterpret_cast<const Bytes16*>(p);
+      return u32x4{v.w[0], v.w[1], v.w[2], v.w[3]};
+    };
+    const int depth = (int)(k1 - k0);
+    const auto step = [&](int s, int count, auto load) {
+      u32x4 vw[U][NT], vx[U][MT];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (u >= count) break;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) vw[u][j] = load(wp[j] + (s + u) * HALF, s + u);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) vx[u][i] = load(xp[i] + (s + u) * HALF, s + u);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (u >= count) break;
+        multiply(vw[u], vx[u]);
+      }
+    };
+    int s = 0;
+    for (; (s + U) * HALF <= depth; s += U) step(s, U, [&](const T* p, int) { return whole(p); });
+    for (; s * HALF < depth; ++s)
+      step(s, 1, [&](const T* p, int at) {
+        const int left = depth - at * HALF - grp * EPC;
+        if (left >= EPC) return whole(p);
+        u32x4 h = {0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < EPC; ++e)
+          if (e < left) {
+            if constexpr (sizeof(T) == 4) h[e] = __builtin_bit_cast(uint32_t, p[e]);
+            else h[e / 2] |= (uint32_t)p[e] << (16 * (e % 2));
+          }
+        return h;
+      });
+  }
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int i = 0; i < MT; ++i) reinterpret_cast<f32x4*>(mine)[(j * MT + i) * 64 + lane] = acc[j][i];
+  __syncthreads();
+  // eight results of one token to a thread, groups of a row side by side
+  constexpr int UNITS = MT * 16 * NT * 2;
+  static_assert(UNITS <= WAVES * 64);
+  const int unit = threadIdx.x;
+  if (unit >= UNITS) return;
+  const int q = unit % (NT * 2), m = unit / (NT * 2);
+  const int at = (q / 2 * MT + m / 16) * 64 + (q & 1) * 32 + (m & 15);
+  float z[kVec] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, bias[kVec];
+  read_bias<E>(g, n0 + q * kVec, bias);
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    const f32x4* const part = reinterpret_cast<const f32x4*>(linear_lds + w * PRIVATE);
+    const f32x4 lo = part[at], hi = part[at + 16];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      z[e] += lo[e];
+      z[4 + e] += hi[e];
+    }
+  }
+  finish_group<E>(g, m, n0 + q * kVec, bias, z);
+}
+
+template <class E, int MT, int NT, int WAVES, int STAGES, bool DMA>
+hipError_t few_launch(const GemmArgs& g, hipStream_t stream) {
+  constexpr int lds = WAVES * (DMA ? STAGES * 16 * (MT + NT) * kStageBytes : NT * MT * 1024);
+  const auto kernel = linear_few_kernel<E, MT, NT, WAVES, STAGES, DMA>;
+  static const hipError_t ready = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                                      hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (ready != hipSuccess) return ready;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((g.n + 16 * NT - 1) / (16 * NT))), dim3(WAVES * 64), lds, stream, g);
+  return hipGetLastError();
+}
+
 template <class E>
 LinearTable make_linear_table() {
   LinearTable t{};
-  const auto fill = [&](LinearFn(&row)[2], auto ax, auto bx, auto tile) {
+  const auto operands = [&](auto ax, auto bx, LinearOperands o) {
     constexpr bool AX = decltype(ax)::value, BX = decltype(bx)::value;
-    if constexpr (decltype(tile)::value == kTile256) {
-      // (float32 products are bound by the matrix cores at any tile; rows that start anywhere are rare)
-      if constexpr (E::kId != kStorageF32) row[1] = linear_launch<E, 256, 256, 2, 4, AX, BX, true>;
-    } else {
-      row[0] = linear_launch<E, 128, 128, 2, 2, AX, BX, false>;
-      row[1] = linear_launch<E, 128, 128, 2, 2, AX, BX, true>;
+    t.fn[kTile64][o][0] = linear_launch<E, 64, 64, 2, 2, 2, AX, BX, false>;
+    t.fn[kTile64][o][1] = linear_launch<E, 64, 64, 2, 2, 2, AX, BX, true>;
+    // (float32 products are bound by the matrix cores in the smallest tile already: 142 to 144 TFLOP/s)
+    if constexpr (E::kId != kStorageF32) {
+      t.fn[kTile128][o][0] = linear_launch<E, 128, 128, 2, 4, 2, AX, BX, false>;
+      t.fn[kTile128][o][1] = linear_launch<E, 128, 128, 2, 4, 2, AX, BX, true>;
+      t.fn[kTile128x256][o][1] = linear_launch<E, 128, 256, 2, 4, 3, AX, BX, true>;
+      t.fn[kTile256][o][1] = linear_launch<E, 256, 256, 2, 4, 2, AX, BX, true>;
     }
   };
-  const auto operands = [&](auto tile) {
-    constexpr int i = decltype(tile)::value;
-    fill(t.fn[i][kForward], std::false_type{}, std::false_type{}, tile);
-    fill(t.fn[i][kGradX], std::false_type{}, std::true_type{}, tile);
-    fill(t.fn[i][kGradW], std::true_type{}, std::true_type{}, tile);
-  };
-  operands(std::integral_constant<int, kTile128>{});
-  operands(std::integral_constant<int, kTile256>{});
+  operands(std::false_type{}, std::false_type{}, kForward);
+  operands(std::false_type{}, std::true_type{}, kGradX);
+  operands(std::true_type{}, std::true_type{}, kGradW);
+  t.few[0][0][1] = few_launch<E, 1, 1, 8, 4, true>;
+  t.few[0][1][1] = few_launch<E, 1, 2, 4, 6, true>;
+  t.few[1][0][1] = few_launch<E, 2, 1, 4, 6, true>;
+  t.few[1][1][1] = few_launch<E, 2, 2, 4, 4, true>;
+  t.few[2][0][1] = few_launch<E, 4, 1, 4, 4, true>;
+  t.few[2][1][1] = few_launch<E, 4, 2, 4, 3, true>;
+  t.few[0][0][0] = few_launch<E, 1, 1, 8, 0, false>;
+  t.few[0][1][0] = few_launch<E, 1, 2, 8, 0, false>;
+  t.few[1][0][0] = few_launch<E, 2, 1, 8, 0, false>;
+  t.few[1][1][0] = few_launch<E, 2, 2, 8, 0, false>;
+  t.few[2][0][0] = few_launch<E, 4, 1, 8, 0, false>;
+  t.few[2][1][0] = few_launch<E, 4, 2, 8, 0, false>;
   return t;
 }
 
