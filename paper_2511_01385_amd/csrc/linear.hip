@@ -51,35 +51,66 @@ static hipError_t join(GemmArgs g, hipStream_t stream) {
 // dz = dy act'(z), z from its checkpoint, rounded once to the storage type (it is a matrix operand),
 // and the column sums of the unrounded dz.  A workgroup takes a strip of 512 columns, its four
 // waves every fourth row of its range; partials[blockIdx.y][n] receive the sums.
-constexpr int kSlopeWG = 256, kSlopeWaves = 4, kSlopeStrip = 64 * kVec;
-constexpr int64_t kSlopeMaxParts = 128;
+constexpr int kSlopeWG = 256, kSlopeWaves = 4, kSlopeStrip = 64 * kVec, kSlopeAhead = 4;
+constexpr int64_t kSlopeMaxParts = 256;
 
-template <class E>
+template <class E, bool EXACT>
 __global__ void __launch_bounds__(kSlopeWG)
     linear_slope_kernel(const typename E::T* __restrict__ dy, int64_t ldg, Checkpoint ck, typename E::T* __restrict__ dz,
-                        float* __restrict__ partials, int64_t rows, int64_t per, int64_t n, int act) {
+                        float* __restrict__ partials, int rows, int per, int n, int act) {
   __shared__ float sums[kSlopeWaves][kSlopeStrip];
   const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-  const int64_t i = (int64_t)blockIdx.x * kSlopeStrip + lane * kVec;
-  const int64_t blocks = (n + kCkBlock - 1) / kCkBlock;
-  const int64_t r1 = min(rows, (int64_t)(blockIdx.y + 1) * per);
+  const int i = blockIdx.x * kSlopeStrip + lane * kVec;
+  const int blocks = (n + kCkBlock - 1) / kCkBlock;
+  const int r0 = blockIdx.y * per + wave, r1 = min(rows, (int)(blockIdx.y + 1) * per);
   float s[kVec] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   if (i < n) {
-#pragma unroll 2
-    for (int64_t r = (int64_t)blockIdx.y * per + wave; r < r1; r += kSlopeWaves) {
-      float g[kVec];
-      read_group<E>(dy + r * ldg, i, n, g);
-      if (ck.codes != nullptr) {
-        const int8_t* const row = ck.codes + r * n;
-        const Bytes8 c = i + kVec <= n ? *reinterpret_cast<const Bytes8*>(row + i) : tail_codes(row, i, n);
+    const auto row = [&](int r, float* g, const Bytes8& code, int byte) {
+      if (act != kActNone) {
         float z[kVec];
-        ck_decode(c, ck_scale(ck.scales[r * blocks + i / kCkBlock]), z);
-#pragma unroll
-        for (int k = 0; k < kVec; ++k) g[k] *= activation_slope(act, z[k]);
-        write_group<E>(dz + r * n, i, n, g);
+        ck_decode(code, ck_scale(byte), z);
+        times_slope8(act, z, g);
+        if constexpr (EXACT) E::store(dz + (int64_t)r * n + i, g);
+        else write_group<E>(dz + (int64_t)r * n, i, n, g);
       }
 #pragma unroll
       for (int k = 0; k < kVec; ++k) s[k] += g[k];
+    };
+    int r = r0;
+    if constexpr (EXACT) {
+      // several rows under way at once
+      for (; r + (kSlopeAhead - 1) * kSlopeWaves < r1; r += kSlopeAhead * kSlopeWaves) {
+        typename E::Raw raw[kSlopeAhead];
+        Bytes8 code[kSlopeAhead];
+        int byte[kSlopeAhead];
+#pragma unroll
+        for (int u = 0; u < kSlopeAhead; ++u) raw[u] = E::load(dy + (int64_t)(r + u * kSlopeWaves) * ldg + i);
+        if (act != kActNone) {
+#pragma unroll
+          for (int u = 0; u < kSlopeAhead; ++u) {
+            code[u] = *reinterpret_cast<const Bytes8*>(ck.codes + (int64_t)(r + u * kSlopeWaves) * n + i);
+            byte[u] = ck.scales[(int64_t)(r + u * kSlopeWaves) * blocks + i / kCkBlock];
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < kSlopeAhead; ++u) {
+          float g[kVec];
+          E::widen(raw[u], g);
+          row(r + u * kSlopeWaves, g, code[u], byte[u]);
+        }
+      }
+    }
+#pragma unroll 1
+    for (; r < r1; r += kSlopeWaves) {
+      float g[kVec];
+      Bytes8 code = {{0, 0}};
+      int byte = 0;
+      read_group<E>(dy + (int64_t)r * ldg, i, n, g);
+      if (act != kActNone) {
+        code = tail_codes(ck.codes + (int64_t)r * n, i, n);
+        byte = ck.scales[(int64_t)r * blocks + i / kCkBlock];
+      }
+      row(r, g, code, byte);
     }
   }
   if (partials == nullptr) return;
@@ -87,20 +118,20 @@ __global__ void __launch_bounds__(kSlopeWG)
   for (int k = 0; k < kVec; ++k) sums[wave][k * 64 + lane] = s[k];
   __syncthreads();
   for (int c = threadIdx.x; c < kSlopeStrip; c += kSlopeWG) {
-    const int64_t col = (int64_t)blockIdx.x * kSlopeStrip + c;
+    const int col = blockIdx.x * kSlopeStrip + c;
     if (col >= n) break;
     const int at = c % kVec * 64 + c / kVec;
     float v = sums[0][at];
 #pragma unroll
     for (int w = 1; w < kSlopeWaves; ++w) v += sums[w][at];
-    partials[blockIdx.y * n + col] = v;
+    partials[(int64_t)blockIdx.y * n + col] = v;
   }
 }
 
-// row ranges that fill the chip a few times over, of eight rows at least
+// row ranges that fill the chip's wave slots (eight workgroups a CU), of sixteen rows at least
 static int64_t slope_parts(int64_t rows, int64_t n) {
   const int64_t strips = (n + kSlopeStrip - 1) / kSlopeStrip;
-  return std::max<int64_t>(1, std::min({(kCUs * 8 + strips - 1) / strips, (rows + 7) / 8, kSlopeMaxParts}));
+  return std::max<int64_t>(1, std::min({(kCUs * 8 + strips - 1) / strips, (rows + 15) / 16, kSlopeMaxParts}));
 }
 
 // ----------------------------------------------------------------------------------
@@ -238,11 +269,13 @@ hipError_t launch_linear_backward(const LinearBackward& a, hipStream_t stream) {
     float* const partials = a.db == nullptr ? nullptr : reinterpret_cast<float*>(parts);
     e = with_elem(storage, [&](auto elem) {
       using E = decltype(elem);
-      hipLaunchKernelGGL(linear_slope_kernel<E>, dim3((unsigned)((n + kSlopeStrip - 1) / kSlopeStrip), (unsigned)count),
-                         dim3(kSlopeWG), 0, stream, static_cast<const typename E::T*>(a.dy), a.ldg,
-                         a.s.act == kActNone ? Checkpoint{} : a.ck, static_cast<typename E::T*>(a.workspace), partials, T,
-                         per, n, a.s.act);
-      return hipGetLastError();
+      const auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((n + kSlopeStrip - 1) / kSlopeStrip), (unsigned)count), dim3(kSlopeWG),
+                           0, stream, static_cast<const typename E::T*>(a.dy), a.ldg, a.ck,
+                           static_cast<typename E::T*>(a.workspace), partials, (int)T, (int)per, (int)n, a.s.act);
+        return hipGetLastError();
+      };
+      return n % kVec == 0 ? go(linear_slope_kernel<E, true>) : go(linear_slope_kernel<E, false>);
     });
     if (e == hipSuccess && a.db != nullptr)
       e = launch_column_finish(partials, count, n, n, a.db, nullptr, storage, stream);

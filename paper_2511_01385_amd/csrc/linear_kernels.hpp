@@ -106,6 +106,29 @@ __device__ __forceinline__ float activation_slope(int act, float z) {
   return 1.f;
 }
 
+// eight values; act is the same for the whole launch
+__device__ __forceinline__ void activate8(int act, float* z) {
+  const auto each = [&](auto which) {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) z[i] = activate(decltype(which)::value, z[i]);
+  };
+  using std::integral_constant;
+  if (act == kActRelu) each(integral_constant<int, kActRelu>{});
+  else if (act == kActGelu) each(integral_constant<int, kActGelu>{});
+  else if (act == kActSilu) each(integral_constant<int, kActSilu>{});
+}
+// g *= act'(z)
+__device__ __forceinline__ void times_slope8(int act, const float* z, float* g) {
+  const auto each = [&](auto which) {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) g[i] *= activation_slope(decltype(which)::value, z[i]);
+  };
+  using std::integral_constant;
+  if (act == kActRelu) each(integral_constant<int, kActRelu>{});
+  else if (act == kActGelu) each(integral_constant<int, kActGelu>{});
+  else if (act == kActSilu) each(integral_constant<int, kActSilu>{});
+}
+
 // ----------------------------------------------------------------------------------
 // operands
 
@@ -326,10 +349,7 @@ __device__ __forceinline__ void finish_group(const GemmArgs& g, int64_t m, int64
     }
   }
   if (!in) return;
-  if (g.act != kActNone) {
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) z[i] = activate(g.act, z[i]);
-  }
+  activate8(g.act, z);
   if (g.residual != nullptr) {
     float add[kVec];
     read_group<E>(static_cast<const T*>(g.residual) + m * g.ldr, n, g.n, add);
@@ -338,6 +358,51 @@ __device__ __forceinline__ void finish_group(const GemmArgs& g, int64_t m, int64
   }
   write_group<E>(static_cast<T*>(g.d) + m * g.ldd, n, g.n, z);
 }
+// The same for COUNT rows m, m + step, ... that lie in D with all their columns; take(b, z) gives row b's
+// results.  The residual's loads are all under way before the first row is worked on.
+template <class E, int COUNT, class Take>
+__device__ __forceinline__ void finish_rows(const GemmArgs& g, int64_t m, int step, int64_t n, const float* bias, Take&& take) {
+  using T = typename E::T;
+  float z[kVec];
+  if (g.partial != nullptr) {
+    float* const p = g.partial + m * g.n + n;
+#pragma unroll
+    for (int b = 0; b < COUNT; ++b) {
+      take(b, z);
+      ElemF32::store(p + (int64_t)(b * step) * g.n, z);
+    }
+    return;
+  }
+  typename E::Raw add[COUNT];
+  if (g.residual != nullptr) {
+    const T* const p = static_cast<const T*>(g.residual) + m * g.ldr + n;
+#pragma unroll
+    for (int b = 0; b < COUNT; ++b) add[b] = E::load(p + (int64_t)(b * step) * g.ldr);
+  }
+  T* const d = static_cast<T*>(g.d) + m * g.ldd + n;
+  const int64_t blocks = (g.n + kCkBlock - 1) / kCkBlock;
+#pragma unroll
+  for (int b = 0; b < COUNT; ++b) {
+    take(b, z);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) z[i] += bias[i];
+    if (g.ck.codes != nullptr) {
+      const int s = ck_scale_byte(quad_max(max_bits8(z)));
+      const int64_t row = m + b * step;
+      *reinterpret_cast<Bytes8*>(g.ck.codes + row * g.n + n) = ck_encode(z, s);
+      if (n % kCkBlock == 0) g.ck.scales[row * blocks + n / kCkBlock] = (uint8_t)s;
+    }
+    activate8(g.act, z);
+    if (g.residual != nullptr) {
+      float v[kVec];
+      E::widen(add[b], v);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) z[i] += v[i];
+    }
+    E::store(d + (int64_t)(b * step) * g.ldd, z);
+  }
+}
+
 template <class E>
 __device__ __forceinline__ void read_bias(const GemmArgs& g, int64_t n, float* bias) {
   if (g.bias != nullptr && n < g.n) {
@@ -499,31 +564,47 @@ __global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_
   }
   stage_wait<0>();
 
-  // Each wave turns its results, 16 rows at a time, through LDS of its own into runs of eight
-  // along n: eight lanes then write whole cache lines of D.  (No wave reads stages any more.)
-  constexpr int PITCH = TN + 4, RUNS = TN / kVec, ROWS = 64 / RUNS;
-  static_assert(WAVES * 16 * PITCH * 4 <= STAGES * STAGE && 16 % ROWS == 0);
-  float* const turn = reinterpret_cast<float*>(linear_lds) + wave * 16 * PITCH;
+  // Each wave turns its results through LDS of its own (no wave reads stages any more), PART blocks of 16 rows at a
+  // time, into runs of eight along n: the lanes of a row then read and write whole cache lines.  16 bytes c of a row lie
+  // at (c / 2, odd ones in the second half) xor row: neither side meets in a bank.
+  constexpr int PART = FM < 4 ? FM : 4, CH = TN / 4, RUNS = TN / kVec, ROWS = 64 / RUNS, PASSES = 16 * PART / ROWS;
+  static_assert(WAVES * PART * 16 * TN * 4 <= STAGES * STAGE && FM % PART == 0);
+  char* const turn = linear_lds + wave * (PART * 16 * TN * 4);
+  const auto slot = [](int row, int c) { return (row * CH + (((c >> 1) | (c & 1) * (CH / 2)) ^ (row & (CH - 1)))) * 16; };
   const int64_t n = n0 + wn * TN + lane % RUNS * kVec;
   float bias[kVec];
   read_bias<E>(g, n, bias);
   if (g.partial != nullptr) g.partial += (int64_t)at.split * g.m * g.n;
+  const bool inner = m0 + BM <= g.m && n0 + BN <= g.n;  // no result outside D
 #pragma unroll
-  for (int i = 0; i < FM; ++i) {
+  for (int p = 0; p < FM; p += PART) {
 #pragma unroll
-    for (int j = 0; j < FN; ++j)
-      *reinterpret_cast<f32x4*>(turn + (lane & 15) * PITCH + j * 16 + (lane >> 4) * 4) = acc[i][j];
+    for (int i = 0; i < PART; ++i)
 #pragma unroll
-    for (int h = 0; h < 16 / ROWS; ++h) {
-      const int r = h * ROWS + lane / RUNS;
-      float z[kVec];
+      for (int j = 0; j < FN; ++j)
+        *reinterpret_cast<f32x4*>(turn + slot(i * 16 + (lane & 15), j * 4 + (lane >> 4))) = acc[p + i][j];
+    const int r = lane / RUNS;
+    const int64_t m = m0 + wm * TM + p * 16 + r;
+    const auto take = [&](int row, float* z) {
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
-        const f32x4 v = *reinterpret_cast<const f32x4*>(turn + r * PITCH + lane % RUNS * kVec + q * 4);
+        const f32x4 v = *reinterpret_cast<const f32x4*>(turn + slot(row, lane % RUNS * 2 + q));
 #pragma unroll
         for (int e = 0; e < 4; ++e) z[q * 4 + e] = v[e];
       }
-      finish_group<E>(g, m0 + wm * TM + i * 16 + r, n, bias, z);
+    };
+    if (inner) {
+      constexpr int BATCH = PASSES < 4 ? PASSES : 4;
+#pragma unroll 1
+      for (int h = 0; h < PASSES; h += BATCH)
+        finish_rows<E, BATCH>(g, m + h * ROWS, ROWS, n, bias, [&](int b, float* z) { take((h + b) * ROWS + r, z); });
+    } else {
+#pragma unroll 1
+      for (int h = 0; h < PASSES; ++h) {
+        float z[kVec];
+        take(h * ROWS + r, z);
+        finish_group<E>(g, m + h * ROWS, n, bias, z);
+      }
     }
   }
 }
