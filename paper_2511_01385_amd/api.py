@@ -280,20 +280,30 @@ def _vector(t: torch.Tensor, name: str, dtype: torch.dtype, device: int, n: int)
 
 
 def _first(t: torch.Tensor, name: str):
-    """(rows, n), storage type, its code, device and stream of a call, by its first tensor."""
-    shape = t.shape
-    if len(shape) != 2:
-        raise ValueError(f"{name} must be two-dimensional, got shape {tuple(shape)}")
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a device tensor")
-    return shape, t.dtype, _code(t), t.get_device(), _stream(t)
+    """Pointer, row stride, (rows, n), storage type, its code, device and stream of a call's first tensor."""
+    shape, dtype, device = t.shape, t.dtype, t.get_device()
+    code = _CODES.get(dtype)
+    if len(shape) != 2 or code is None or device < 0 or device != _current_device():
+        if len(shape) != 2:
+            raise ValueError(f"{name} must be two-dimensional, got shape {tuple(shape)}")
+        if device < 0:
+            raise ValueError(f"{name} must be a device tensor")
+        _code(t), _stream(t)  # (one of them raises)
+    if t.is_contiguous():
+        return t.data_ptr(), shape[1], shape, dtype, code, device, _raw_stream(device)
+    return (*_rows(t, name, dtype, device, shape), shape, dtype, code, device, _raw_stream(device))
 
 
 def _held(checkpoint, device: int, rows: int, n: int) -> tuple[int, int]:
     """Pointers of a (codes, scales) pair for (rows, n) values."""
     codes, scales = checkpoint
-    for name, t, dtype, shape in (("codes", codes, torch.int8, (rows, n)),
-                                  ("scales", scales, torch.uint8, (rows, -(-n // CHECKPOINT_BLOCK)))):
+    blocks = -(-n // CHECKPOINT_BLOCK)
+    if (codes.dtype is torch.int8 and scales.dtype is torch.uint8 and codes.shape == (rows, n)
+            and scales.shape == (rows, blocks) and codes.get_device() == device and scales.get_device() == device
+            and codes.is_contiguous() and scales.is_contiguous()):
+        return codes.data_ptr(), scales.data_ptr()
+    # which of these it is
+    for name, t, dtype, shape in (("codes", codes, torch.int8, (rows, n)), ("scales", scales, torch.uint8, (rows, blocks))):
         if t.dtype is not dtype:
             raise TypeError(f"a checkpoint's {name} are {dtype}, got {t.dtype}")
         if t.shape != shape:
@@ -302,7 +312,6 @@ def _held(checkpoint, device: int, rows: int, n: int) -> tuple[int, int]:
             raise ValueError(f"{name} must be on cuda:{device}, is on {t.device}")
         if not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous")
-    return codes.data_ptr(), scales.data_ptr()
 
 
 def _scratch(need: int, given, device: int, what: str):
@@ -337,21 +346,23 @@ def checkpoint_like(x: torch.Tensor) -> tuple[torch.Tensor, torch.Tensor]:
 
 def act8_quantize(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor):
     """The 8-bit checkpoint of x (rows, n): int8 codes, and one scale byte for 32 values of a row."""
-    shape, dtype, code, device, stream = _first(x, "x")
+    p, ld, shape, dtype, code, device, stream = _first(x, "x")
     rows, n = shape
-    p, ld = _rows(x, "x", dtype, device, shape)
     held = _lib.pack["act8"](*_held((codes, scales), device, rows, n))
-    _check(_lib.load().act8_quantize(p, ld, held, rows, n, code, stream), "act8_quantize")
+    status = _lib.load().act8_quantize(p, ld, held, rows, n, code, stream)
+    if status:
+        _check(status, "act8_quantize")
     return codes, scales
 
 
 def act8_dequantize(codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor) -> torch.Tensor:
     """What a checkpoint stands for, in ``out``'s type (exact in float32 and bfloat16)."""
-    shape, dtype, code, device, stream = _first(out, "out")
+    p, ld, shape, dtype, code, device, stream = _first(out, "out")
     rows, n = shape
-    p, ld = _rows(out, "out", dtype, device, shape)
     held = _lib.pack["act8"](*_held((codes, scales), device, rows, n))
-    _check(_lib.load().act8_dequantize(held, p, ld, rows, n, code, stream), "act8_dequantize")
+    status = _lib.load().act8_dequantize(held, p, ld, rows, n, code, stream)
+    if status:
+        _check(status, "act8_dequantize")
     return out
 
 
@@ -364,10 +375,10 @@ def layer_norm_forward(x, weight, bias, y, *, residual=None, mean=None, rstd=Non
     ``mean`` and ``rstd`` (rows,) and ``checkpoint``, of the norm's input, are written if given.
     ``y`` may be ``x`` or ``residual``.
     """
-    shape, dtype, code, device, stream = _first(x, "x")
+    p, ld, shape, dtype, code, device, stream = _first(x, "x")
     rows, n = shape
     a = _lib.pack["layer_norm_forward"](
-        *_rows(x, "x", dtype, device, shape),
+        p, ld,
         *((0, 0) if residual is None else _rows(residual, "residual", dtype, device, shape)),
         _vector(weight, "weight", _F32, device, n),
         0 if bias is None else _vector(bias, "bias", _F32, device, n),
@@ -375,7 +386,9 @@ def layer_norm_forward(x, weight, bias, y, *, residual=None, mean=None, rstd=Non
         0 if mean is None else _vector(mean, "mean", _F32, device, rows),
         0 if rstd is None else _vector(rstd, "rstd", _F32, device, rows),
         *((0, 0) if checkpoint is None else _held(checkpoint, device, rows, n)))
-    _check(_lib.load().layer_norm_forward(a, rows, n, eps, code, stream), "layer_norm_forward")
+    status = _lib.load().layer_norm_forward(a, rows, n, eps, code, stream)
+    if status:
+        _check(status, "layer_norm_forward")
     return y
 
 
@@ -385,7 +398,7 @@ def layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, *, residu
     ``x`` is the forward's x, or the checkpoint (codes, scales) of the norm's input; ``dx`` may be ``dy``.
     ``workspace``: ``layer_norm_backward_workspace(rows, n)`` bytes, allocated if not given.
     """
-    shape, dtype, code, device, stream = _first(dy, "dy")
+    p, ld, shape, dtype, code, device, stream = _first(dy, "dy")
     rows, n = shape
     if isinstance(x, torch.Tensor):
         inputs = (*_rows(x, "x", dtype, device, shape),
@@ -397,11 +410,13 @@ def layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, *, residu
     keep, scratch, size = _scratch(_need("layer_norm_backward_workspace", rows, n), workspace, device,
                                    "layer_norm_backward")
     a = _lib.pack["layer_norm_backward"](
-        *_rows(dy, "dy", dtype, device, shape), *inputs, _vector(weight, "weight", _F32, device, n),
+        p, ld, *inputs, _vector(weight, "weight", _F32, device, n),
         _vector(mean, "mean", _F32, device, rows), _vector(rstd, "rstd", _F32, device, rows),
         *_rows(dx, "dx", dtype, device, shape), _vector(dweight, "dweight", _F32, device, n),
         _vector(dbias, "dbias", _F32, device, n), scratch, size)
-    _check(_lib.load().layer_norm_backward(a, rows, n, code, stream), "layer_norm_backward")
+    status = _lib.load().layer_norm_backward(a, rows, n, code, stream)
+    if status:
+        _check(status, "layer_norm_backward")
     return dx, dweight, dbias
 
 
@@ -423,7 +438,7 @@ def linear_forward(x, w, y, *, bias=None, activation="none", residual=None, chec
     ``checkpoint``, of the pre-activation, is written if given.  ``y`` may be ``residual``.
     ``workspace``: ``linear_forward_workspace(...)`` bytes, allocated if not given.
     """
-    shape, dtype, code, device, stream = _first(x, "x")
+    p, ld, shape, dtype, code, device, stream = _first(x, "x")
     tokens, d_in = shape
     d_out = w.shape[0]
     act = _activation(activation)
@@ -431,12 +446,14 @@ def linear_forward(x, w, y, *, bias=None, activation="none", residual=None, chec
     keep, scratch, size = _scratch(_need("linear_forward_workspace", d_in, d_out, tokens, code), workspace, device,
                                    "linear_forward")
     a = _lib.pack["linear_forward"](
-        *_rows(x, "x", dtype, device, shape), *_rows(w, "w", dtype, device, (d_out, d_in)),
+        p, ld, *_rows(w, "w", dtype, device, (d_out, d_in)),
         0 if bias is None else _vector(bias, "bias", dtype, device, d_out),
         *((0, 0) if residual is None else _rows(residual, "residual", dtype, device, out)),
         *_rows(y, "y", dtype, device, out),
         *((0, 0) if checkpoint is None else _held(checkpoint, device, tokens, d_out)), scratch, size)
-    _check(_lib.load().linear_forward(a, d_in, d_out, tokens, act, code, stream), "linear_forward")
+    status = _lib.load().linear_forward(a, d_in, d_out, tokens, act, code, stream)
+    if status:
+        _check(status, "linear_forward")
     return y
 
 
@@ -452,7 +469,7 @@ def linear_backward(dy, x, w, *, dx=None, dw=None, db=None, activation="none", c
     z is what ``checkpoint`` stands for (not needed without an activation).  ``x`` may be None without dw, ``w``
     without dx; ``dx`` may be ``add``.  ``workspace``: ``linear_backward_workspace(...)`` bytes, allocated if not given.
     """
-    shape, dtype, code, device, stream = _first(dy, "dy")
+    p, ld, shape, dtype, code, device, stream = _first(dy, "dy")
     tokens, d_out = shape
     act = _activation(activation)
     d_in = 1  # (db alone)
@@ -476,14 +493,16 @@ def linear_backward(dy, x, w, *, dx=None, dw=None, db=None, activation="none", c
         _need("linear_backward_workspace", d_in, d_out, tokens, dx is not None, dw is not None, db is not None, act, code),
         workspace, device, "linear_backward")
     a = _lib.pack["linear_backward"](
-        *_rows(dy, "dy", dtype, device, shape), *held,
+        p, ld, *held,
         *(none if dw is None else _rows(x, "x", dtype, device, (tokens, d_in))),
         *(none if dx is None else _rows(w, "w", dtype, device, (d_out, d_in))),
         *(none if dx is None or add is None else _rows(add, "add", dtype, device, (tokens, d_in))),
         *(none if dx is None else _rows(dx, "dx", dtype, device, (tokens, d_in))),
         *(none if dw is None else _rows(dw, "dw", dtype, device, (d_out, d_in))),
         0 if db is None else _vector(db, "db", dtype, device, d_out), scratch, size)
-    _check(_lib.load().linear_backward(a, d_in, d_out, tokens, act, code, stream), "linear_backward")
+    status = _lib.load().linear_backward(a, d_in, d_out, tokens, act, code, stream)
+    if status:
+        _check(status, "linear_backward")
     return dx, dw, db
 
 

@@ -100,7 +100,9 @@ __global__ void __launch_bounds__(norm_fwd_wg<TPR>()) layer_norm_forward_kernel(
       for (int k = 0; k < kVec; ++k) b[c][k] = 0.f;
   }
   const int64_t step = (int64_t)gridDim.x * GROUPS;
-  for (int64_t row = (int64_t)blockIdx.x * GROUPS + threadIdx.x / TPR; row < a.rows; row += step) {
+  // (a wave lies in one row: addresses of rows are scalar)
+  for (int64_t row = (int64_t)blockIdx.x * GROUPS + __builtin_amdgcn_readfirstlane((int)threadIdx.x / TPR); row < a.rows;
+       row += step) {
     const T* const x = static_cast<const T*>(a.x) + row * a.ldx;
     const T* const r = static_cast<const T*>(a.residual) + row * a.ldr;
     float u[C][kVec];
@@ -234,12 +236,11 @@ __global__ void __launch_bounds__(kNormBwdWG)
   constexpr int WG = kNormBwdWG, GROUPS = WG / TPR;
   __shared__ float red[4 * (WG / 64)];
   int turn = 0;
-  const int lane = threadIdx.x % TPR, grp = threadIdx.x / TPR;
+  const int lane = threadIdx.x % TPR, grp = __builtin_amdgcn_readfirstlane((int)threadIdx.x / TPR);  // (one in a wave)
   const int n = (int)a.n, blocks = (n + kCkBlock - 1) / kCkBlock;
   const float inv_n = 1.0f / (float)n;
   int at[C];
   float w[C][kVec], dw[C][kVec], db[C][kVec];
-  NormRow<E, TPR, C, CK, EXACT> next;
   const int64_t step = (int64_t)gridDim.x * GROUPS;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
@@ -248,27 +249,21 @@ __global__ void __launch_bounds__(kNormBwdWG)
 #pragma unroll
     for (int k = 0; k < kVec; ++k) dw[c][k] = db[c][k] = 0.f;
   }
-  // the next row is on its way while this one is worked on, where the registers hold both
-  constexpr bool AHEAD = C == 1;
   int64_t row = (int64_t)blockIdx.x * GROUPS + grp;
-  if (AHEAD && row < a.rows) next.load(a, row, at, n, blocks);
-  // (the groups of a workgroup take the same number of rows: they meet at barriers)
-  for (int64_t row0 = (int64_t)blockIdx.x * GROUPS; row0 < a.rows; row0 += step, row += step) {
-    const bool act = row < a.rows;
+  const auto work = [&](const NormRow<E, TPR, C, CK, EXACT>& in, bool act, auto&& loads) {
     float u[C][kVec], g[C][kVec];
     float mean = 0.f, rstd = 0.f;
     if (act) {
-      if constexpr (!AHEAD) next.load(a, row, at, n, blocks);
-      mean = next.mean;
-      rstd = next.rstd;
-      next.widen(a, row, at, n, blocks, g, u);
-      if (AHEAD && row + step < a.rows) next.load(a, row + step, at, n, blocks);
+      mean = in.mean;
+      rstd = in.rstd;
+      in.widen(a, row, at, n, blocks, g, u);
     } else {
 #pragma unroll
       for (int c = 0; c < C; ++c)
 #pragma unroll
         for (int k = 0; k < kVec; ++k) g[c][k] = u[c][k] = 0.f;
     }
+    loads();  // of a later row, into the registers that are free now
     float s[2] = {0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < C; ++c)
@@ -282,15 +277,38 @@ __global__ void __launch_bounds__(kNormBwdWG)
         s[1] = fmaf(g[c][k], u[c][k], s[1]);
       }
     group_sums<TPR, 2>(s, red, turn);
-    if (!act) continue;
-    const float m0 = s[0] * inv_n, m1 = s[1] * inv_n;
-    T* const dx = static_cast<T*>(a.dx) + row * a.ldd;
+    if (act) {
+      const float m0 = s[0] * inv_n, m1 = s[1] * inv_n;
+      T* const dx = static_cast<T*>(a.dx) + row * a.ldd;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      float v[kVec];
+      for (int c = 0; c < C; ++c) {
+        float v[kVec];
 #pragma unroll
-      for (int k = 0; k < kVec; ++k) v[k] = rstd * (g[c][k] - m0 - u[c][k] * m1);
-      store_group<E, EXACT>(dx, at[c], n, v);
+        for (int k = 0; k < kVec; ++k) v[k] = rstd * (g[c][k] - m0 - u[c][k] * m1);
+        store_group<E, EXACT>(dx, at[c], n, v);
+      }
+    }
+    row += step;
+  };
+  // (the groups of a workgroup take the same number of rows: they meet at barriers)
+  int64_t row0 = (int64_t)blockIdx.x * GROUPS;
+  // rows that are on their way while one is worked on, as far as the registers go
+  constexpr int AHEAD = C > 1 ? 0 : E::kId == kStorageF32 && !CK ? 1 : 2;
+  NormRow<E, TPR, C, CK, EXACT> in[AHEAD > 1 ? 2 : 1];
+  const auto load = [&](NormRow<E, TPR, C, CK, EXACT>& to, int64_t r) {
+    if (r < a.rows) to.load(a, r, at, n, blocks);
+  };
+#pragma unroll
+  for (int q = 0; q < AHEAD; ++q) load(in[q], row + q * step);
+  for (; row0 < a.rows; row0 += step) {
+    if constexpr (AHEAD == 0) load(in[0], row);
+    work(in[0], row < a.rows, [&] {
+      if constexpr (AHEAD > 0) load(in[0], row + AHEAD * step);
+    });
+    if constexpr (AHEAD > 1) {
+      row0 += step;
+      if (row0 >= a.rows) break;
+      work(in[1], row < a.rows, [&] { load(in[1], row + AHEAD * step); });
     }
   }
   dw_out += blockIdx.x * stride;
@@ -370,7 +388,7 @@ static hipError_t with_row(int64_t n, F&& fn) {
   return go(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
 }
 
-// The backward has 1024 threads to a workgroup and so 128 registers: one group of eight to a thread.
+// the same for the backward, whose threads also hold sums
 template <class F>
 static hipError_t with_row_backward(int64_t n, F&& fn) {
   using std::integral_constant;

@@ -9,7 +9,8 @@ All arithmetic on the data runs in the library's kernels; torch only allocates
 buffers, casts the parameter and reshapes.
 
 Memory: the forward keeps x and the packed spectra (q*kb*p storage elements) for the
-backward, nothing else.  The backward allocates dx and, for blocks of at most 8192, nothing
+backward, nothing else.  With ``checkpoint8=True`` it keeps x as an 8-bit checkpoint (33/32 bytes a
+value); the backward makes x of it for the time of the call, and dc is the gradient at those values.  The backward allocates dx and, for blocks of at most 8192, nothing
 more: the library only reads the upstream gradient.  Longer blocks need a copy of it as
 work space, which dx then shares (when d_in == d_out and there are at most 8 blocks per
 row; otherwise dx gets its own buffer).  With ``clobber_grad=True`` it works
@@ -29,7 +30,7 @@ from . import api
 
 class _BcaFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x2d: torch.Tensor, c: torch.Tensor, dtype: torch.dtype, clobber_grad: bool):
+    def forward(ctx, x2d: torch.Tensor, c: torch.Tensor, dtype: torch.dtype, clobber_grad: bool, checkpoint8: bool):
         q, kb, p = c.shape
         spectra = c.detach().to(dtype).contiguous()
         if spectra.data_ptr() == c.data_ptr():  # float32 layer: do not transform the parameter itself
@@ -37,14 +38,19 @@ class _BcaFunction(torch.autograd.Function):
         api.rdfft_forward(spectra.view(q * kb, p))
         y = torch.empty((x2d.shape[0], q * p), dtype=dtype, device=x2d.device)
         api.bca_forward(x2d, spectra, y)
-        ctx.save_for_backward(x2d, spectra)
+        kept = api.act8_quantize(x2d, *api.checkpoint_like(x2d)) if checkpoint8 else (x2d,)
+        ctx.save_for_backward(spectra, *kept)
         ctx.clobber_grad = clobber_grad
         return y
 
     @staticmethod
     def backward(ctx, gy: torch.Tensor):
-        x2d, spectra = ctx.saved_tensors
+        spectra, *kept = ctx.saved_tensors
         q, kb, p = spectra.shape
+        if len(kept) == 2:
+            x2d = api.act8_dequantize(*kept, torch.empty(kept[0].shape, dtype=spectra.dtype, device=spectra.device))
+        else:
+            x2d = kept[0]
         given = gy
         gy = gy.contiguous()
         if gy.dtype != x2d.dtype:
@@ -55,14 +61,14 @@ class _BcaFunction(torch.autograd.Function):
             # the library only reads the upstream gradient
             dx = torch.empty_like(x2d)
             api.bca_backward_keep(x2d, spectra, gy, dx, dc)
-            return dx, dc, None, None
+            return dx, dc, None, None, None
         if not mine:
             gy = gy.clone()  # the library overwrites it
         # dx may share the work buffer when the layer is square (for blocks beyond 8192, when
         # a per-bin product holds its q blocks)
         dx = gy if q == kb and (p <= 8192 or q <= 8) else torch.empty_like(x2d)
         api.bca_backward(x2d, spectra, gy, dx, dc)
-        return dx, dc, None, None
+        return dx, dc, None, None, None
 
 
 class BlockCirculantLinear(torch.nn.Module):
@@ -71,11 +77,12 @@ class BlockCirculantLinear(torch.nn.Module):
     x has shape (..., d_in) and the storage type ``dtype`` (bfloat16, float16 or float32); y has
     shape (..., d_out).  p must be a power of two with 2 <= p <= 65536 dividing d_in and
     d_out; blocks longer than 8192 also need (d_in/p)(d_out/p) <= 65535.  c is initialised N(0, sigma^2) with sigma = d_in^-1/2
-    unless given.
+    unless given.  ``checkpoint8`` keeps x for the backward in 8 bits.
     """
 
     def __init__(self, d_in: int, d_out: int, p: int, dtype: torch.dtype = torch.bfloat16,
-                 device: str | torch.device = "cuda", sigma: float | None = None, clobber_grad: bool = False):
+                 device: str | torch.device = "cuda", sigma: float | None = None, clobber_grad: bool = False,
+                 checkpoint8: bool = False):
         super().__init__()
         if p < 2 or p & (p - 1):
             raise ValueError(f"p must be a power of two >= 2, got {p}")
@@ -90,6 +97,7 @@ class BlockCirculantLinear(torch.nn.Module):
         self.d_in, self.d_out, self.p = d_in, d_out, p
         self.dtype = dtype
         self.clobber_grad = clobber_grad
+        self.checkpoint8 = checkpoint8
         sigma = 1.0 / math.sqrt(d_in) if sigma is None else sigma
         c = torch.randn((d_out // p, d_in // p, p), dtype=torch.float32, device=device) * sigma
         self.c = torch.nn.Parameter(c)
@@ -101,7 +109,7 @@ class BlockCirculantLinear(torch.nn.Module):
             raise TypeError(f"input is {x.dtype}, the layer stores {self.dtype}")
         lead = x.shape[:-1]
         x2d = x.reshape(-1, self.d_in).contiguous()
-        y = _BcaFunction.apply(x2d, self.c, self.dtype, self.clobber_grad)
+        y = _BcaFunction.apply(x2d, self.c, self.dtype, self.clobber_grad, self.checkpoint8)
         return y.reshape(*lead, self.d_out)
 
     def extra_repr(self) -> str:
