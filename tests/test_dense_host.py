@@ -1,0 +1,214 @@
+"""What the operators around the adapter refuse, on the host before any HIP call (no GPU needed): every call below
+must fail validation or have nothing to do, so nothing is ever launched from here."""
+
+import math
+
+import pytest
+import torch
+
+from paper_2511_01385_amd import _lib, api
+from paper_2511_01385_amd.feedforward import AdaptedFeedForward
+
+EINVAL, EUNSUP, OK = _lib.RDFFT_EINVAL, _lib.RDFFT_EUNSUPPORTED, _lib.RDFFT_OK
+F32, BF16, F16 = _lib.RDFFT_F32, _lib.RDFFT_BF16, _lib.RDFFT_F16
+
+# fake addresses, never dereferenced, 1 GiB apart
+P = [0x7F0000000000 + (i << 30) for i in range(16)]
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return _lib.load()
+
+
+def call(lib, name, fields, *args):
+    order = _lib._FIELDS[name].split()
+    assert set(fields) <= set(order)
+    return getattr(lib, name)(_lib.pack[name](*[fields.get(f, 0) for f in order]), *args)
+
+
+def quantize(lib, x=P[0], ldx=64, codes=P[1], scales=P[2], rows=4, n=64, dtype=BF16):
+    return lib.act8_quantize(x, ldx, _lib.pack["act8"](codes, scales), rows, n, dtype, None)
+
+
+def dequantize(lib, x=P[0], ldx=64, codes=P[1], scales=P[2], rows=4, n=64, dtype=BF16):
+    return lib.act8_dequantize(_lib.pack["act8"](codes, scales), x, ldx, rows, n, dtype, None)
+
+
+@pytest.mark.parametrize("change,want", [
+    (dict(x=0), EINVAL), (dict(codes=0), EINVAL), (dict(scales=0), EINVAL), (dict(x=P[0] + 1), EINVAL),
+    (dict(ldx=63), EINVAL), (dict(rows=-1), EINVAL), (dict(n=0), EINVAL), (dict(n=-5), EINVAL), (dict(dtype=3), EINVAL),
+    (dict(codes=P[0] + 100), EINVAL), (dict(scales=P[0] + 511), EINVAL), (dict(x=P[2] - 500), EINVAL),
+    (dict(rows=1 << 62, n=64), EINVAL), (dict(rows=1 << 50, ldx=1 << 40), EINVAL), (dict(rows=0, x=0, codes=0), OK),
+])
+def test_act8(lib, change, want):
+    assert quantize(lib, **change) == want
+    assert dequantize(lib, **change) == want
+
+
+def test_act8_without_a_checkpoint(lib):
+    assert lib.act8_quantize(P[0], 64, None, 4, 64, BF16, None) == EINVAL
+    assert lib.act8_dequantize(None, P[0], 64, 4, 64, BF16, None) == EINVAL
+
+
+NORM = dict(x=P[0], ldx=64, weight=P[1], bias=P[2], y=P[3], ldy=64, mean=P[4], rstd=P[5], codes=P[6], scales=P[7])
+
+
+@pytest.mark.parametrize("change,want", [
+    (dict(x=0), EINVAL), (dict(weight=0), EINVAL), (dict(y=0), EINVAL), (dict(ldx=63), EINVAL), (dict(ldy=1), EINVAL),
+    (dict(x=P[0] + 1), EINVAL), (dict(weight=P[1] + 2), EINVAL), (dict(mean=P[4] + 1), EINVAL), (dict(codes=0), EINVAL),
+    (dict(scales=0), EINVAL), (dict(residual=P[8], ldr=60), EINVAL),
+    (dict(y=P[0] + 2), EINVAL),  # neither x nor apart from it
+    (dict(y=P[0], ldy=128), EINVAL),  # x's place with another stride
+    (dict(residual=P[3] + 64, ldr=64), EINVAL), (dict(mean=P[0] + 64), EINVAL), (dict(rstd=P[4]), EINVAL),
+    (dict(codes=P[3] + 8), EINVAL), (dict(y=P[1]), EINVAL), (dict(scales=P[6] + 255), EINVAL),
+])
+def test_layer_norm_forward(lib, change, want):
+    assert call(lib, "layer_norm_forward", {**NORM, **change}, 4, 64, 1e-5, BF16, None) == want
+
+
+def test_layer_norm_forward_sizes(lib):
+    go = lambda rows=4, n=64, eps=1e-5, dtype=BF16: call(lib, "layer_norm_forward", NORM, rows, n, eps, dtype, None)  # noqa: E731
+    assert go(rows=0) == OK and go(rows=-1) == EINVAL and go(n=0) == EINVAL and go(dtype=7) == EINVAL
+    assert go(n=16385) == EUNSUP
+    assert go(eps=-1e-9) == EINVAL and go(eps=math.nan) == EINVAL and go(eps=math.inf) == EINVAL
+    assert lib.layer_norm_forward(None, 4, 64, 1e-5, BF16, None) == EINVAL
+
+
+GRAD = dict(dy=P[0], ldg=64, x=P[1], ldx=64, weight=P[2], mean=P[3], rstd=P[4], dx=P[5], ldd=64, dweight=P[6], dbias=P[7],
+            workspace=P[8], workspace_bytes=1 << 20)
+
+
+@pytest.mark.parametrize("change,want", [
+    (dict(dy=0), EINVAL), (dict(weight=0), EINVAL), (dict(mean=0), EINVAL), (dict(rstd=0), EINVAL), (dict(dx=0), EINVAL),
+    (dict(dweight=0), EINVAL), (dict(dbias=0), EINVAL), (dict(x=0), EINVAL),  # neither x nor a checkpoint
+    (dict(x=0, codes=P[9]), EINVAL), (dict(x=0, codes=P[9], scales=P[10], residual=P[11], ldr=64), EINVAL),
+    (dict(workspace=0), EINVAL), (dict(workspace_bytes=16), EINVAL), (dict(workspace=P[8] + 8), EINVAL),
+    (dict(dx=P[0] + 2), EINVAL), (dict(dx=P[0], ldd=72), EINVAL), (dict(dx=P[1]), EINVAL), (dict(dweight=P[0] + 4), EINVAL),
+    (dict(dbias=P[6] + 128), EINVAL), (dict(workspace=P[5]), EINVAL), (dict(workspace=P[0] + 16), EINVAL),
+    (dict(ldg=10), EINVAL), (dict(ldd=63), EINVAL), (dict(mean=P[3] + 2), EINVAL),
+])
+def test_layer_norm_backward(lib, change, want):
+    assert call(lib, "layer_norm_backward", {**GRAD, **change}, 400, 64, BF16, None) == want
+
+
+def test_layer_norm_backward_sizes(lib):
+    go = lambda rows=4, n=64, dtype=BF16: call(lib, "layer_norm_backward", GRAD, rows, n, dtype, None)  # noqa: E731
+    assert go(rows=-1) == EINVAL and go(n=0) == EINVAL and go(dtype=9) == EINVAL and go(n=16385) == EUNSUP
+    assert lib.layer_norm_backward(None, 4, 64, BF16, None) == EINVAL
+    need = lib.layer_norm_backward_workspace
+    assert need(-1, 64) == EINVAL and need(4, 0) == EINVAL and need(4, 16385) == EUNSUP
+    assert 0 < need(1, 64) <= need(100000, 64) and need(1 << 40, 16384) <= 64 << 20
+
+
+LINEAR = dict(x=P[0], ldx=64, w=P[1], ldw=64, bias=P[2], y=P[4], ldy=96, codes=P[5], scales=P[6], workspace=P[7],
+              workspace_bytes=1 << 29)
+
+
+@pytest.mark.parametrize("change,want", [
+    (dict(x=0), EINVAL), (dict(w=0), EINVAL), (dict(y=0), EINVAL), (dict(ldx=63), EINVAL), (dict(ldw=1), EINVAL),
+    (dict(ldy=95), EINVAL), (dict(x=P[0] + 1), EINVAL), (dict(bias=P[2] + 1), EINVAL), (dict(codes=0), EINVAL),
+    (dict(scales=0), EINVAL), (dict(residual=P[3], ldr=80), EINVAL), (dict(y=P[0]), EINVAL), (dict(y=P[1] + 96), EINVAL),
+    (dict(residual=P[4] + 2, ldr=96), EINVAL), (dict(residual=P[4], ldr=100), EINVAL), (dict(codes=P[4]), EINVAL),
+    (dict(y=P[2]), EINVAL), (dict(ldx=(1 << 21) + 1), EUNSUP), (dict(ldw=(1 << 21) + 8), EUNSUP),
+    (dict(workspace=0), EINVAL), (dict(workspace_bytes=256), EINVAL), (dict(workspace=P[7] + 4), EINVAL),
+    (dict(workspace=P[4]), EINVAL),
+])
+def test_linear_forward(lib, change, want):
+    tokens, d_in, d_out = 96, 64, 96
+    if any(k.startswith("workspace") for k in change):  # a size whose k is split
+        tokens, d_in = 96, 65536
+        change = dict(ldx=65536, ldw=65536, **change)
+        assert lib.linear_forward_workspace(d_in, d_out, tokens, BF16) > 256
+    assert call(lib, "linear_forward", {**LINEAR, **change}, d_in, d_out, tokens, 2, BF16, None) == want
+
+
+@pytest.mark.parametrize("d_in,d_out,tokens,act,dtype,want", [
+    (0, 96, 4, 0, BF16, EINVAL), (64, 0, 4, 0, BF16, EINVAL), (64, 96, -1, 0, BF16, EINVAL), (64, 96, 4, 4, BF16, EINVAL),
+    (64, 96, 4, -1, BF16, EINVAL), (64, 96, 4, 0, 3, EINVAL), ((1 << 20) + 1, 96, 4, 0, BF16, EUNSUP),
+    (64, (1 << 20) + 1, 4, 0, F16, EUNSUP), (64, 96, (1 << 22) + 1, 0, F32, EUNSUP),
+    (64, 1 << 20, 1 << 20, 0, BF16, EUNSUP), (64, 96, 0, 0, BF16, OK),
+])
+def test_linear_sizes(lib, d_in, d_out, tokens, act, dtype, want):
+    assert call(lib, "linear_forward", LINEAR, d_in, d_out, tokens, act, dtype, None) == want
+    # (each gradient that is wanted: none)
+    if want != OK:
+        assert call(lib, "linear_backward", {}, d_in, d_out, tokens, act, dtype, None) == want
+        assert lib.linear_backward_workspace(d_in, d_out, tokens, 1, 1, 1, act, dtype) == want
+    if act == 0:
+        assert lib.linear_forward_workspace(d_in, d_out, tokens, dtype) == want  # (0 bytes where it is OK)
+
+
+BACK = dict(dy=P[0], ldg=96, codes=P[1], scales=P[2], x=P[3], ldx=64, w=P[4], ldw=64, add=P[5], lda=64, dx=P[6], ldd=64,
+            dw=P[7], lddw=64, db=P[8], workspace=P[9], workspace_bytes=1 << 29)
+
+
+@pytest.mark.parametrize("change,want", [
+    (dict(dy=0), EINVAL), (dict(codes=0), EINVAL), (dict(scales=0), EINVAL), (dict(x=0), EINVAL), (dict(w=0), EINVAL),
+    (dict(ldg=95), EINVAL), (dict(ldx=60), EINVAL), (dict(ldw=63), EINVAL), (dict(lda=2), EINVAL), (dict(ldd=63), EINVAL),
+    (dict(lddw=63), EINVAL), (dict(dy=P[0] + 1), EINVAL), (dict(db=P[8] + 1), EINVAL), (dict(workspace=0), EINVAL),
+    (dict(workspace_bytes=1000), EINVAL), (dict(workspace=P[9] + 2), EINVAL), (dict(dx=P[0]), EINVAL),
+    (dict(dx=P[5] + 2), EINVAL), (dict(dx=P[5], ldd=80), EINVAL), (dict(dw=P[4]), EINVAL), (dict(db=P[7] + 64), EINVAL),
+    (dict(dw=P[6]), EINVAL), (dict(workspace=P[3]), EINVAL), (dict(db=P[5]), EINVAL), (dict(ldg=(1 << 21) + 1), EUNSUP),
+    (dict(ldx=(1 << 21) + 1), EUNSUP), (dict(ldw=(1 << 21) + 1), EUNSUP),
+])
+def test_linear_backward(lib, change, want):
+    assert call(lib, "linear_backward", {**BACK, **change}, 64, 96, 160, 2, BF16, None) == want
+
+
+def test_linear_backward_of_nothing(lib):
+    assert call(lib, "linear_backward", dict(dy=P[0], ldg=96), 64, 96, 160, 0, BF16, None) == OK
+    assert lib.linear_backward(None, 64, 96, 160, 0, BF16, None) == EINVAL
+
+
+def test_slices_side_by_side_do_not_overlap(lib):
+    # columns 0..63 and 64..127 of one buffer: refused only for the workspace that the call lacks
+    fields = {**GRAD, "dy": P[0], "ldg": 128, "dx": P[0] + 128, "ldd": 128, "workspace": 0}
+    assert call(lib, "layer_norm_backward", fields, 400, 64, BF16, None) == EINVAL
+    assert call(lib, "layer_norm_backward", {**fields, "workspace": P[8] + 8}, 400, 64, BF16, None) == EINVAL
+
+
+def test_the_binding_refuses_host_tensors_and_names():
+    x, w = torch.zeros(4, 64), torch.ones(64)
+    c = api.checkpoint_like(x)
+    for bad in (lambda: api.act8_quantize(x, *c), lambda: api.act8_dequantize(*c, x),
+                lambda: api.layer_norm_forward(x, w, w, x), lambda: api.layer_norm_backward(x, x, w, w, w, x, w, w),
+                lambda: api.linear_forward(x, x, x), lambda: api.linear_backward(x, x, x, dx=x)):
+        with pytest.raises(ValueError, match="device tensor"):
+            bad()
+    with pytest.raises(ValueError, match="two-dimensional"):
+        api.layer_norm_forward(w, w, w, w)
+    with pytest.raises(ValueError, match="activation"):
+        api.linear_forward_workspace(64, 64, 64, torch.bfloat16) or api._activation("tanh")
+
+
+def test_a_checkpoint_has_a_byte_a_value_and_one_for_32():
+    codes, scales = api.checkpoint_like(torch.zeros(5, 70))
+    assert codes.shape == (5, 70) and codes.dtype == torch.int8
+    assert scales.shape == (5, 3) and scales.dtype == torch.uint8
+
+
+def test_workspace_sizes():
+    assert api.linear_forward_workspace(4096, 4096, 64, torch.bfloat16) == 0
+    full = api.linear_backward_workspace(4096, 4096, 4096, torch.bfloat16, "gelu")
+    assert full >= 4096 * 4096 * 2  # dz
+    assert api.linear_backward_workspace(4096, 4096, 4096, torch.bfloat16, "none", db=False) < full
+    with pytest.raises(api.RdfftError):
+        api.layer_norm_backward_workspace(4, 20000)
+    with pytest.raises(ValueError):
+        api.linear_backward_workspace(64, 64, 64, torch.bfloat16, "softplus")
+
+
+@pytest.mark.parametrize("args,kw,err", [
+    ((256, 512, 48), {}, ValueError), ((256, 500, 64), {}, ValueError), ((256, 512, 16384), {}, ValueError),
+    ((256, 512, 64), dict(activation="tanh"), ValueError), ((256, 512, 64), dict(dtype=torch.float64), TypeError),
+])
+def test_feed_forward_arguments(args, kw, err):
+    with pytest.raises(err):
+        AdaptedFeedForward(*args, device="cpu", **kw)
+    net = AdaptedFeedForward(256, 512, 64, device="cpu")
+    assert net.c.shape == (4, 8, 64) and not net.c.any() and {n for n, _ in net.named_parameters()} == {"c", "weight", "bias"}
+    with pytest.raises(ValueError):
+        net(torch.zeros(3, 255))
+    with pytest.raises(TypeError):
+        net(torch.zeros(3, 256))

@@ -124,6 +124,26 @@ def test_in_place():
     assert torch.equal(dy, dx)
 
 
+def test_slices_side_by_side_and_refusals():
+    both = hidden(40, 1000, 4, "bf16")
+    dy, dx = both[:, :500], both[:, 500:]
+    x, w = hidden(40, 500, 5, "bf16"), torch.ones(500, device="cuda")
+    mean, rstd = torch.zeros(40, device="cuda"), torch.ones(40, device="cuda")
+    want = api.layer_norm_backward(dy.clone(), x, w, mean, rstd, torch.empty_like(x), torch.empty_like(w), torch.empty_like(w))[0]
+    dw, db = torch.empty_like(w), torch.empty_like(w)
+    assert torch.equal(api.layer_norm_backward(dy, x, w, mean, rstd, dx, dw, db)[0], want)
+    back = lambda **k: api.layer_norm_backward(*[k.get(n, v) for n, v in (  # noqa: E731
+        ("dy", dy), ("x", x), ("w", w), ("mean", mean), ("rstd", rstd), ("dx", dx), ("dw", dw), ("db", db))])
+    for bad, err in ((dict(x=x.float()), TypeError), (dict(w=w.bfloat16()), TypeError), (dict(w=w[:499]), ValueError),
+                     (dict(dx=dx[:39]), ValueError), (dict(mean=mean[:39]), ValueError), (dict(dw=w.cpu()), ValueError),
+                     (dict(dx=torch.empty(500, 40, dtype=x.dtype, device="cuda").t()), ValueError),
+                     (dict(dx=x), api.RdfftError), (dict(x=(x, x)), TypeError), (dict(dy=dy.double()), TypeError)):
+        with pytest.raises(err):
+            back(**bad)
+    with pytest.raises(ValueError):
+        api.layer_norm_backward(dy, x, w, mean, rstd, dx, dw, db, workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))
+
+
 def test_constant_rows_and_large_means():
     # variance zero: y is the bias; a mean a thousand times the deviation loses only what float32 inputs have lost
     x = torch.full((3, 700), 2.5, device="cuda")

@@ -169,6 +169,26 @@ def test_in_place():
     assert torch.equal(dx, want)
 
 
+def test_refusals():
+    x, w, b, r, dy, a = tensors(40, 96, 160, "bf16", 3)
+    y = torch.empty_like(r)
+    held = api.checkpoint_like(r)
+    for args, kw, err in (((x, w.half(), y), {}, TypeError), ((x, w[:, :95], y), {}, ValueError), ((x, w, y[:39]), {}, ValueError),
+                          ((x, w.cpu(), y), {}, ValueError), ((x, w, y), dict(bias=b.float()), TypeError),
+                          ((x, w, y), dict(bias=b[1:]), ValueError), ((x, w, y), dict(activation="tanh"), ValueError),
+                          ((x, w, y), dict(residual=r[:, 1:]), ValueError), ((x, w, y), dict(checkpoint=(held[1], held[0])), TypeError),
+                          ((x, w, y), dict(checkpoint=(held[0], held[1][:, :4])), ValueError), ((x, w, x[:, :160]), {}, ValueError),
+                          ((x, w, w[:40, :1].expand(40, 160)), {}, ValueError), ((x.double(), w, y), {}, TypeError)):
+        with pytest.raises(err):
+            api.linear_forward(*args, **kw)
+    for kw, err in ((dict(dx=a, activation="gelu"), ValueError), (dict(dx=a[:, :95]), ValueError), (dict(dw=w.float()), TypeError),
+                    (dict(dx=a, dw=w[:, :95]), ValueError), (dict(db=b[:5]), ValueError), (dict(dx=dy[:, :96]), api.RdfftError)):
+        with pytest.raises(err):
+            api.linear_backward(dy, x, w, **kw)
+    with pytest.raises(ValueError):
+        api.linear_backward(dy, None, w, dw=torch.empty_like(w))
+
+
 def test_no_tokens():
     x, w, b, r, dy, a = tensors(0, 96, 160, "bf16", 3)
     api.linear_forward(x, w, torch.empty_like(r), bias=b)
