@@ -90,7 +90,7 @@ struct GemmArgs {
   int tiles_m, tiles_n;
 };
 // the instances for one storage type; null where one is not built.  Last index: 1 with loads straight to LDS
-enum LinearTile { kTile64, kTile128, kTile128x256, kTile256, kLinearTiles };
+enum LinearTile { kTile32x64, kTile64, kTile128, kTile128x256, kTile256, kLinearTiles };
 enum LinearOperands { kForward, kGradX, kGradW, kLinearOperands };
 using LinearFn = hipError_t (*)(const GemmArgs&, hipStream_t);
 constexpr int64_t kFewTokens = 64;

@@ -137,34 +137,37 @@ static int64_t slope_parts(int64_t rows, int64_t n) {
 // ----------------------------------------------------------------------------------
 // plans
 
-// What a tile costs, in us, from products of 768 to 8192: a stage (128 bytes of k) where a CU has one workgroup
-// of them, a stage of each where it has more (`together` fit), and what comes before and after.  The largest tile
-// reaches 1390 to 1420 TFLOP/s (16-bit) where its tiles fill the chip in whole rounds; the smaller ones
-// 1270, 1200 and 780, but leave fewer CUs idle: 4096 x 768 x 768 (12 stages) takes 10 us in tiles of 128 or 64 and 15 and 23
-// in the larger two, 2045 x 4096 x 4096 58 us in 128 x 256, 61, 81 and 92 in 128, 256 and 64.
+// What a tile costs, in us, from products of 128 to 8192: a stage (128 bytes of k) where a CU has one workgroup
+// of them, a stage of each where it has more (`together` fit), and what comes before and after.  16-bit values: the largest
+// tile reaches 1390 to 1420 TFLOP/s where its tiles fill the chip in whole rounds; the smaller ones 1270, 1200 and 780, but
+// leave fewer CUs idle: 4096 x 768 x 768 (12 stages) takes 10 us in tiles of 128 or 64 and 15 and 23 in the larger two,
+// 2045 x 4096 x 4096 58 us in 128 x 256, 61, 81 and 92 in 128, 256 and 64; 128 x 4096 x 4096 16 us in 32 x 64 and 64,
+// 38 in 128.  float32: the matrix cores bound every tile alike (142 TFLOP/s); 300 x 768 x 768 10 us in 32 x 64, 16 in 64.
 struct TileCost {
   int bm, bn, together;
   double alone, each, ends;
 };
-constexpr TileCost kCost16[kLinearTiles] = {
-    {64, 64, 4, 0.25, 0.175, 3.6}, {128, 128, 2, 0.50, 0.445, 4.0}, {128, 256, 1, 0.82, 0.82, 4.8}, {256, 256, 1, 1.30, 1.30, 13.0}};
-constexpr TileCost kCost32 = {64, 64, 4, 0.62, 0.45, 3.6};
+constexpr TileCost kCost16[kLinearTiles] = {{32, 64, 4, 0.19, 0.14, 3.4},   {64, 64, 3, 0.235, 0.175, 3.6},
+                                            {128, 128, 2, 0.50, 0.445, 4.0}, {128, 256, 1, 0.82, 0.82, 4.8},
+                                            {256, 256, 1, 1.30, 1.30, 13.0}};
+constexpr TileCost kCost32[] = {{32, 64, 4, 0.285, 0.256, 3.6}, {64, 64, 3, 0.53, 0.50, 4.0}};
 
 struct Plan {
   LinearTile tile;
   int64_t splits, k_split;
 };
 
-// The tile and the number of k ranges that cost least.  The join of s ranges costs a launch (3 us) and 8 s bytes a
+// The tile and the number of k ranges that cost least.  The join of s ranges costs a launch (4 us) and 8 s bytes a
 // result, at 4 TB/s.
-static Plan plan_of(int64_t m, int64_t n, int64_t k, int storage, bool direct) {
+static Plan plan_of(int64_t m, int64_t n, int64_t k, LinearOperands kind, int storage, bool direct) {
   const bool f32 = storage == kStorageF32;
   const int64_t bk = kStageBytes / (f32 ? 4 : 2), stages = std::max<int64_t>(1, (k + bk - 1) / bk);
   Plan best{kTile64, 1, stages * bk};
   double least = 0;
   for (int t = 0; t < kLinearTiles; ++t) {
-    if (t != kTile64 && (f32 || (!direct && t != kTile128))) continue;
-    const TileCost& c = f32 ? kCost32 : kCost16[t];
+    if (direct ? f32 && t > kTile64 : t == kTile32x64 || t == kTile256 || (f32 && t > kTile64)) continue;  // (not built)
+    if (t == kTile32x64 && kind == kGradW) continue;
+    const TileCost& c = f32 ? kCost32[t] : kCost16[t];
     const int64_t tiles = ((m + c.bm - 1) / c.bm) * ((n + c.bn - 1) / c.bn);
     for (int64_t want = 1; want <= 16; ++want) {
       const int64_t each = (stages + want - 1) / want, splits = (stages + each - 1) / each;
@@ -173,7 +176,7 @@ static Plan plan_of(int64_t m, int64_t n, int64_t k, int storage, bool direct) {
       const int64_t per_cu = std::max<int64_t>(1, (tiles * splits + kCUs - 1) / kCUs);
       const double stage = per_cu == 1 ? c.alone : c.each * (double)per_cu;
       double cost = (double)each * stage + c.ends * (double)((per_cu + c.together - 1) / c.together);
-      if (splits > 1) cost += 3.0 + 8.0 * (double)splits * (double)m * (double)n / 4e6;
+      if (splits > 1) cost += 4.0 + 8.0 * (double)splits * (double)m * (double)n / 4e6;
       if (least == 0 || cost < least) {
         least = cost;
         best = {(LinearTile)t, splits, each * bk};
@@ -183,10 +186,10 @@ static Plan plan_of(int64_t m, int64_t n, int64_t k, int storage, bool direct) {
   return best;
 }
 // (whether rows are aligned is not known here: the larger of both plans' needs)
-static int64_t split_bytes(int64_t m, int64_t n, int64_t k, int storage) {
+static int64_t split_bytes(int64_t m, int64_t n, int64_t k, LinearOperands kind, int storage) {
   int64_t most = 0;
   for (const bool direct : {false, true}) {
-    const Plan p = plan_of(m, n, k, storage, direct);
+    const Plan p = plan_of(m, n, k, kind, storage, direct);
     if (p.splits > 1) most = std::max(most, p.splits * m * n * 4);
   }
   return most;
@@ -196,7 +199,7 @@ static int64_t round_up(int64_t bytes) { return (bytes + 255) & ~(int64_t)255; }
 static int storage_bytes(int storage) { return storage == kStorageF32 ? 4 : 2; }
 
 int64_t linear_forward_workspace(const LinearSizes& s) {
-  return s.tokens <= kFewTokens ? 0 : split_bytes(s.tokens, s.d_out, s.d_in, s.storage);
+  return s.tokens <= kFewTokens ? 0 : split_bytes(s.tokens, s.d_out, s.d_in, kForward, s.storage);
 }
 
 // dz, then the partial sums of whichever pass runs (they follow each other on the stream)
@@ -206,8 +209,8 @@ static int64_t slope_bytes(const LinearSizes& s) {
 int64_t linear_backward_workspace(const LinearSizes& s, bool dx, bool dw, bool db) {
   int64_t parts = 0;
   if (db) parts = std::max(parts, slope_parts(s.tokens, s.d_out) * s.d_out * 4);
-  if (dx) parts = std::max(parts, split_bytes(s.tokens, s.d_in, s.d_out, s.storage));
-  if (dw) parts = std::max(parts, split_bytes(s.d_out, s.d_in, s.tokens, s.storage));
+  if (dx) parts = std::max(parts, split_bytes(s.tokens, s.d_in, s.d_out, kGradX, s.storage));
+  if (dw) parts = std::max(parts, split_bytes(s.d_out, s.d_in, s.tokens, kGradW, s.storage));
   return slope_bytes(s) + parts;
 }
 
@@ -229,7 +232,7 @@ static hipError_t product(GemmArgs& g, LinearOperands kind, int storage, void* w
     const bool wide = g.ck.codes != nullptr || g.n >= 32 * kCUs;
     return t.few[g.m <= 16 ? 0 : g.m <= 32 ? 1 : 2][wide][direct](g, stream);
   }
-  const Plan p = plan_of(g.m, g.n, g.k, storage, direct);
+  const Plan p = plan_of(g.m, g.n, g.k, kind, storage, direct);
   g.splits = (int)p.splits;
   g.k_split = p.k_split;
   g.partial = p.splits > 1 ? static_cast<float*>(workspace) : nullptr;

@@ -177,6 +177,25 @@ __device__ __forceinline__ void reads_wait() {
   asm volatile("" ::: "memory");
 }
 
+__device__ __forceinline__ void wave_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// 16 bytes without the first `bytes` (0 ... 15), the rest moved up
+__device__ __forceinline__ u32x4 drop_bytes(u32x4 v, int bytes) {
+  uint64_t lo = (uint64_t)v[1] << 32 | v[0], hi = (uint64_t)v[3] << 32 | v[2];
+  if (bytes >= 8) {
+    lo = hi;
+    hi = 0;
+  }
+  const int bits = (bytes & 7) * 8;
+  lo = lo >> bits | hi << 1 << (63 - bits);
+  hi >>= bits;
+  return u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+}
+
 // R rows (m or n) of one operand's stage.  ACROSS: memory rows run along m.  DMA: straight to
 // LDS, for which a memory row starts at a multiple of 16 bytes and holds whole chunks.
 template <class E, int R, int WAVES, bool ACROSS, bool DMA>
@@ -187,13 +206,16 @@ struct Operand {
   static constexpr int BYTES = R * kStageBytes;
   static constexpr int LINES = BYTES / 1024 / WAVES;   // 64 chunks each, a wave's share
   static_assert(LINES * WAVES * 1024 == BYTES && 64 % CPR == 0);
+  static_assert(!ACROSS || CPR >= (S == 2 ? 8 : 16), "the swizzle stays in the row");
 
   const T* base;    // row 0 and k 0 of this workgroup's tile
   int64_t ld;
   int rows, depth;  // rows of the tile that exist, k that is left
+  int before;       // values of a memory row in front of the tile, or of the k that is left
   int wave, lane;
   uint32_t offset[DMA ? LINES : 1];
-  u32x4 held[DMA ? 1 : LINES];
+  u32x4 held[2][DMA ? 1 : LINES];  // two stages on their way through registers,
+  int held_along[2], held_lines[2];  // and what of them exists where that is not all of it
 
   __device__ __forceinline__ static int swizzle(int k) { return S == 2 ? (k & 3) << 1 : (k >> 2 & 3) << 2; }
   // LDS row and chunk of this lane's part of line j
@@ -208,6 +230,7 @@ struct Operand {
     base = origin + (ACROSS ? k0 * ld + r0 : r0 * ld + k0);
     rows = (int)(r_end - r0 < R ? r_end - r0 : R);
     depth = (int)(k_end - k0);
+    before = ACROSS ? (int)(r0 < kVec ? r0 : kVec) : (int)(k0 < kVec ? k0 : kVec);
     wave = wave_;
     lane = lane_;
     if constexpr (DMA) {
@@ -220,9 +243,9 @@ struct Operand {
     }
   }
 
-  // starts the loads of the next stage (to the LDS region `lds` for DMA) and steps on.  WHOLE: the stage
-  // is known to lie in front of the end of k.
-  template <bool WHOLE = false>
+  // starts the loads of the next stage (to the LDS region `lds` for DMA, else to held[SLOT]) and steps on.
+  // WHOLE: the stage is known to lie in front of the end of k.
+  template <bool WHOLE = false, int SLOT = 0>
   __device__ __forceinline__ void fetch(uint32_t lds) {
     if constexpr (DMA) {
       const char* const p = reinterpret_cast<const char*>(base);
@@ -237,13 +260,24 @@ struct Operand {
         }
       }
     } else {
-      // (a stage in the interior is loaded without branches)
-      if (rows == R && depth >= BK) {
+      // Whole chunks without branches: a chunk that the end of its memory row cuts is loaded so as to end there, then
+      // shifted into place.  k beyond its end is zero; a row of the tile beyond the last is of no account (its
+      // results are not stored) and repeats what is near.
+      const int along = ACROSS ? rows : min(depth, BK), lines = ACROSS ? min(depth, BK) : rows;
+      const auto chunk = [](const T* p) {
+        const Bytes16 v = *reinterpret_cast<const Bytes16*>(p);
+        return u32x4{v.w[0], v.w[1], v.w[2], v.w[3]};
+      };
+      bool mend = false;
+      if (along == (ACROSS ? R : BK) && lines == (ACROSS ? BK : R)) {
 #pragma unroll
-        for (int j = 0; j < LINES; ++j) {
-          const Bytes16 v = *reinterpret_cast<const Bytes16*>(base + row_of(j) * ld + chunk_of(j) * EPC);
-          held[j] = u32x4{v.w[0], v.w[1], v.w[2], v.w[3]};
-        }
+        for (int j = 0; j < LINES; ++j) held[SLOT][j] = chunk(base + row_of(j) * ld + chunk_of(j) * EPC);
+      } else if (along + before >= EPC) {
+        const int last = along - EPC;
+#pragma unroll
+        for (int j = 0; j < LINES; ++j)
+          held[SLOT][j] = chunk(base + min(row_of(j), lines - 1) * ld + min(chunk_of(j) * EPC, last));
+        mend = true;
       } else {
 #pragma unroll
         for (int j = 0; j < LINES; ++j) {
@@ -264,19 +298,34 @@ struct Operand {
                 }
             }
           }
-          held[j] = h;
+          held[SLOT][j] = h;
         }
       }
+      held_along[SLOT] = mend ? along : kVec << 20;
+      held_lines[SLOT] = lines;
     }
     base += ACROSS ? BK * ld : BK;
     depth -= BK;
+    if constexpr (!ACROSS && !DMA) before = kVec;
   }
-  // puts fetched registers into LDS
-  __device__ __forceinline__ void commit(char* lds) const {
+  // puts held[SLOT] into LDS
+  template <int SLOT>
+  __device__ __forceinline__ void commit(char* lds) {
     if constexpr (!DMA) {
+      const int along = held_along[SLOT], last = along - EPC;
+      if (along <= (ACROSS ? R : BK)) {
+#pragma unroll
+        for (int j = 0; j < LINES; ++j) {
+          const int i = chunk_of(j) * EPC;
+          const u32x4 h = drop_bytes(held[SLOT][j], i > last && i < along ? (i - last) * S : 0);
+          const bool out = ACROSS ? row_of(j) >= held_lines[SLOT] : i >= along;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) held[SLOT][j][e] = out ? 0 : h[e];
+        }
+      }
 #pragma unroll
       for (int j = 0; j < LINES; ++j)
-        *reinterpret_cast<u32x4*>(lds + (wave * LINES + j) * 1024 + lane * 16) = held[j];
+        *reinterpret_cast<u32x4*>(lds + (wave * LINES + j) * 1024 + lane * 16) = held[SLOT][j];
     }
   }
 };
@@ -539,27 +588,48 @@ __global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_
       multiply(h1);
     }
   } else {
+    // The same with two stages on their way through registers: stage t + 1 goes to LDS between the halves of stage t,
+    // into the region that every wave has left at the last barrier, and stage t + 3 sets out.
     static_assert(DMA || STAGES == 2);
-    if (steps > 0) {
-      a.fetch(0);
-      b.fetch(0);
-    }
-    for (int t = 0; t < steps; ++t) {
-      char* const la = linear_lds + (t & 1) * STAGE;
-      a.commit(la);
-      b.commit(la + OpA::BYTES);
-      // (the other region's last reads lie before the barrier that follows)
-      stage_wait<0>();
+    const auto fetch = [&](auto slot) {
+      a.template fetch<false, decltype(slot)::value>(0);
+      b.template fetch<false, decltype(slot)::value>(0);
+    };
+    const auto commit = [&](auto slot) {
+      constexpr int S = decltype(slot)::value;
+      a.template commit<S>(linear_lds + S * STAGE);
+      b.template commit<S>(linear_lds + S * STAGE + OpA::BYTES);
+    };
+    using std::integral_constant;
+    Half h0, h1;
+    const auto step = [&](int t, auto cur) {
+      constexpr int C = decltype(cur)::value;
+      constexpr integral_constant<int, C ^ 1> other{};
+      read(h1, linear_lds + C * STAGE, 1);
+      multiply(h0);
       if (t + 1 < steps) {
-        a.fetch(0);
-        b.fetch(0);
+        commit(other);
+        if (t + 3 < steps) fetch(other);
+        reads_wait();
+        wave_barrier();
+        read(h0, linear_lds + (C ^ 1) * STAGE, 0);
       }
-      Half h;
-#pragma unroll
-      for (int kk = 0; kk < 2; ++kk) {
-        read(h, la, kk);
-        multiply(h);
-      }
+      multiply(h1);
+    };
+    constexpr integral_constant<int, 0> even{};
+    constexpr integral_constant<int, 1> odd{};
+    if (steps > 0) {
+      fetch(even);
+      if (steps > 1) fetch(odd);
+      commit(even);
+      if (steps > 2) fetch(even);
+      reads_wait();
+      wave_barrier();
+      read(h0, linear_lds, 0);
+    }
+    for (int t = 0; t < steps; t += 2) {
+      step(t, even);
+      if (t + 1 < steps) step(t + 1, odd);
     }
   }
   stage_wait<0>();
@@ -567,7 +637,7 @@ __global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_
   // Each wave turns its results through LDS of its own (no wave reads stages any more), PART blocks of 16 rows at a
   // time, into runs of eight along n: the lanes of a row then read and write whole cache lines.  16 bytes c of a row lie
   // at (c / 2, odd ones in the second half) xor row: neither side meets in a bank.
-  constexpr int PART = FM < 4 ? FM : 4, CH = TN / 4, RUNS = TN / kVec, ROWS = 64 / RUNS, PASSES = 16 * PART / ROWS;
+  constexpr int PART = FM >= 4 && WAVES * 4 * 16 * TN * 4 <= STAGES * STAGE ? 4 : FM >= 2 ? 2 : 1, CH = TN / 4, RUNS = TN / kVec, ROWS = 64 / RUNS, PASSES = 16 * PART / ROWS;
   static_assert(WAVES * PART * 16 * TN * 4 <= STAGES * STAGE && FM % PART == 0);
   char* const turn = linear_lds + wave * (PART * 16 * TN * 4);
   const auto slot = [](int row, int c) { return (row * CH + (((c >> 1) | (c & 1) * (CH / 2)) ^ (row & (CH - 1)))) * 16; };
@@ -784,10 +854,12 @@ LinearTable make_linear_table() {
   const auto operands = [&](auto ax, auto bx, LinearOperands o) {
     constexpr bool AX = decltype(ax)::value, BX = decltype(bx)::value;
     t.fn[kTile64][o][0] = linear_launch<E, 64, 64, 2, 2, 2, AX, BX, false>;
-    t.fn[kTile64][o][1] = linear_launch<E, 64, 64, 2, 2, 2, AX, BX, true>;
+    t.fn[kTile64][o][1] = linear_launch<E, 64, 64, 2, 2, 3, AX, BX, true>;
+    if constexpr (!AX) t.fn[kTile32x64][o][1] = linear_launch<E, 32, 64, 2, 2, 3, AX, BX, true>;
     // (float32 products are bound by the matrix cores in the smallest tile already: 142 to 144 TFLOP/s)
     if constexpr (E::kId != kStorageF32) {
       t.fn[kTile128][o][0] = linear_launch<E, 128, 128, 2, 4, 2, AX, BX, false>;
+      t.fn[kTile128x256][o][0] = linear_launch<E, 128, 256, 2, 4, 2, AX, BX, false>;
       t.fn[kTile128][o][1] = linear_launch<E, 128, 128, 2, 4, 2, AX, BX, true>;
       t.fn[kTile128x256][o][1] = linear_launch<E, 128, 256, 2, 4, 3, AX, BX, true>;
       t.fn[kTile256][o][1] = linear_launch<E, 256, 256, 2, 4, 2, AX, BX, true>;
