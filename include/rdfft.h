@@ -300,7 +300,8 @@ typedef struct {
   void *workspace;
   int64_t workspace_bytes;
 } layer_norm_backward_t;
-RDFFT_API int64_t layer_norm_backward_workspace(int64_t rows, int64_t n); /* bytes, or a negative rdfft_status_t */
+/* bytes (0: none is needed), or a negative rdfft_status_t */
+RDFFT_API int64_t layer_norm_backward_workspace(int64_t rows, int64_t n);
 RDFFT_API int layer_norm_backward(const layer_norm_backward_t *a, int64_t rows, int64_t n, rdfft_dtype_t dtype,
                                   rdfft_stream_t stream);
 

@@ -174,7 +174,9 @@ int layer_norm_forward(const layer_norm_forward_t* a, int64_t rows, int64_t n, f
 
 int64_t layer_norm_backward_workspace(int64_t rows, int64_t n) {
   const int st = norm_sizes(rows, n, RDFFT_F32);
-  return st != RDFFT_OK ? st : rdfft::norm_partials(rows, n) * 2 * n * 4;
+  if (st != RDFFT_OK) return st;
+  const int64_t parts = rdfft::norm_partials(rows, n);
+  return parts == 1 ? 0 : parts * 2 * n * 4;
 }
 
 int layer_norm_backward(const layer_norm_backward_t* a, int64_t rows, int64_t n, rdfft_dtype_t dtype,

@@ -55,7 +55,7 @@ struct NormGradArgs {
   void* dx;
   int64_t ldd;
   float *dweight, *dbias;
-  float* partials;  // norm_partials(rows, n) * 2n floats
+  float* partials;  // norm_partials(rows, n) * 2n floats; unused where that is one
   int64_t rows, n;
   int storage;
 };

@@ -50,14 +50,14 @@ static hipError_t join(GemmArgs g, hipStream_t stream) {
 // ----------------------------------------------------------------------------------
 // dz = dy act'(z), z from its checkpoint, rounded once to the storage type (it is a matrix operand),
 // and the column sums of the unrounded dz.  A workgroup takes a strip of 512 columns, its four
-// waves every fourth row of its range; partials[blockIdx.y][n] receive the sums.
+// waves every fourth row of its range; partials[blockIdx.y][n] receive the sums, or db where there is one range.
 constexpr int kSlopeWG = 256, kSlopeWaves = 4, kSlopeStrip = 64 * kVec, kSlopeAhead = 4;
 constexpr int64_t kSlopeMaxParts = 256;
 
 template <class E, bool EXACT>
 __global__ void __launch_bounds__(kSlopeWG)
     linear_slope_kernel(const typename E::T* __restrict__ dy, int64_t ldg, Checkpoint ck, typename E::T* __restrict__ dz,
-                        float* __restrict__ partials, int rows, int per, int n, int act) {
+                        float* __restrict__ partials, typename E::T* __restrict__ db, int rows, int per, int n, int act) {
   __shared__ float sums[kSlopeWaves][kSlopeStrip];
   const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
   const int i = blockIdx.x * kSlopeStrip + lane * kVec;
@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(kSlopeWG)
       row(r, g, code, byte);
     }
   }
-  if (partials == nullptr) return;
+  if (partials == nullptr && db == nullptr) return;
 #pragma unroll
   for (int k = 0; k < kVec; ++k) sums[wave][k * 64 + lane] = s[k];
   __syncthreads();
@@ -124,7 +124,8 @@ __global__ void __launch_bounds__(kSlopeWG)
     float v = sums[0][at];
 #pragma unroll
     for (int w = 1; w < kSlopeWaves; ++w) v += sums[w][at];
-    partials[(int64_t)blockIdx.y * n + col] = v;
+    if (db != nullptr) E::put(db + col, v);
+    else partials[(int64_t)blockIdx.y * n + col] = v;
   }
 }
 
@@ -208,7 +209,7 @@ static int64_t slope_bytes(const LinearSizes& s) {
 }
 int64_t linear_backward_workspace(const LinearSizes& s, bool dx, bool dw, bool db) {
   int64_t parts = 0;
-  if (db) parts = std::max(parts, slope_parts(s.tokens, s.d_out) * s.d_out * 4);
+  if (db && slope_parts(s.tokens, s.d_out) > 1) parts = std::max(parts, slope_parts(s.tokens, s.d_out) * s.d_out * 4);
   if (dx) parts = std::max(parts, split_bytes(s.tokens, s.d_in, s.d_out, kGradX, s.storage));
   if (dw) parts = std::max(parts, split_bytes(s.d_out, s.d_in, s.tokens, kGradW, s.storage));
   return slope_bytes(s) + parts;
@@ -269,18 +270,20 @@ hipError_t launch_linear_backward(const LinearBackward& a, hipStream_t stream) {
   hipError_t e = hipSuccess;
   if (a.s.act != kActNone || a.db != nullptr) {
     const int64_t count = slope_parts(T, n), per = (T + count - 1) / count;
-    float* const partials = a.db == nullptr ? nullptr : reinterpret_cast<float*>(parts);
+    float* const partials = a.db == nullptr || count == 1 ? nullptr : reinterpret_cast<float*>(parts);
+    void* const db = count == 1 ? a.db : nullptr;
     e = with_elem(storage, [&](auto elem) {
       using E = decltype(elem);
       const auto go = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)((n + kSlopeStrip - 1) / kSlopeStrip), (unsigned)count), dim3(kSlopeWG),
                            0, stream, static_cast<const typename E::T*>(a.dy), a.ldg, a.ck,
-                           static_cast<typename E::T*>(a.workspace), partials, (int)T, (int)per, (int)n, a.s.act);
+                           static_cast<typename E::T*>(a.workspace), partials, static_cast<typename E::T*>(db), (int)T,
+                           (int)per, (int)n, a.s.act);
         return hipGetLastError();
       };
       return n % kVec == 0 ? go(linear_slope_kernel<E, true>) : go(linear_slope_kernel<E, false>);
     });
-    if (e == hipSuccess && a.db != nullptr)
+    if (e == hipSuccess && partials != nullptr)
       e = launch_column_finish(partials, count, n, n, a.db, nullptr, storage, stream);
     if (e != hipSuccess) return e;
     if (a.s.act != kActNone) {

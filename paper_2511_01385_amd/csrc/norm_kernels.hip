@@ -425,7 +425,8 @@ hipError_t launch_layer_norm_forward(const NormArgs& a, hipStream_t stream, int 
 }
 
 // Workgroups of the backward, each leaving one row of partial sums: one per CU of the largest device
-// at most.  More would fill the chip no better (16 waves each) and cost 8n bytes of traffic apiece, twice.
+// at most.  More would fill the chip no better (16 waves each) and cost 8n bytes of traffic apiece, twice.  Rows that
+// one workgroup goes through in two turns are left to it, whose sums are the result: that saves the second launch.
 constexpr int64_t kNormMaxPartials = 256;
 int64_t norm_partials(int64_t rows, int64_t n) {
   int64_t groups = 1;
@@ -433,7 +434,7 @@ int64_t norm_partials(int64_t rows, int64_t n) {
     groups = kNormBwdWG / decltype(tpr)::value;
     return hipSuccess;
   });
-  return std::max<int64_t>(1, std::min((rows + groups - 1) / groups, kNormMaxPartials));
+  return rows <= 2 * groups ? 1 : std::min((rows + groups - 1) / groups, kNormMaxPartials);
 }
 
 template <class E, int TPR, int C, bool CK, bool EXACT>
