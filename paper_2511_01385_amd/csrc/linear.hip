@@ -166,8 +166,9 @@ static Plan plan_of(int64_t m, int64_t n, int64_t k, LinearOperands kind, int st
   Plan best{kTile64, 1, stages * bk};
   double least = 0;
   for (int t = 0; t < kLinearTiles; ++t) {
-    if (direct ? f32 && t > kTile64 : t == kTile32x64 || t == kTile256 || (f32 && t > kTile64)) continue;  // (not built)
-    if (t == kTile32x64 && kind == kGradW) continue;
+    // what is not built
+    if ((f32 && t > kTile64) || (!direct && (t == kTile32x64 || t == kTile256))) continue;
+    if (kind == kGradW && (t == kTile32x64 || (!direct && t == kTile128x256))) continue;
     const TileCost& c = f32 ? kCost32[t] : kCost16[t];
     const int64_t tiles = ((m + c.bm - 1) / c.bm) * ((n + c.bn - 1) / c.bn);
     for (int64_t want = 1; want <= 16; ++want) {

@@ -16,9 +16,11 @@
 // LDS layouts (units of 16 bytes, `pos` of a row holding chunk `pos ^ swizzle`):
 //   along k:   [BM rows][8 chunks], swizzle row & 7: the 16 rows of a fragment, read at one chunk,
 //              fall on all banks evenly;
-//   across k:  [k rows][BM * S / 16 chunks], swizzle (k & 3) * 2 for 16-bit values, whose
-//              fragments are read transposed, four k rows of 16 values (32 bytes) at a time, and
-//              (k / 4 & 3) * 4 for floats, read one by one in runs of 16 at four k rows.
+//   across k:  [k rows][BM * S / 16 chunks].  16-bit fragments are read transposed, four k rows of 16
+//              values (32 bytes) at a time, k and k + 8 together: swizzle (k & 3) * 2 + (k / 8 & 1) * 8
+//              spreads them over all banks ((k & 3 ^ k / 8 & 1) * 2 in rows of 128 bytes; without the
+//              k / 8 a third to a half of the LDS cycles of dx and dW were conflicts).  Floats are read
+//              one by one in runs of 16 at four k rows: (k / 4 & 3) * 4.
 //
 // The matrix instructions take n as their row and m as their column, so that a lane's four
 // results are consecutive in n, the direction in which D, the bias, the residual and the 8-bit
@@ -196,6 +198,13 @@ __device__ __forceinline__ u32x4 drop_bytes(u32x4 v, int bytes) {
   return u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
 }
 
+// what a chunk's place in memory row k of a stage across k is xored with
+template <int S, int CPR>
+__device__ __forceinline__ int across_swizzle(int k) {
+  if (S == 4) return (k >> 2 & 3) << 2;
+  return CPR >= 16 ? (k & 3) << 1 | (k >> 3 & 1) << 3 : ((k & 3) ^ (k >> 3 & 1)) << 1;
+}
+
 // R rows (m or n) of one operand's stage.  ACROSS: memory rows run along m.  DMA: straight to
 // LDS, for which a memory row starts at a multiple of 16 bytes and holds whole chunks.
 template <class E, int R, int WAVES, bool ACROSS, bool DMA>
@@ -217,11 +226,10 @@ struct Operand {
   u32x4 held[2][DMA ? 1 : LINES];  // two stages on their way through registers,
   int held_along[2], held_lines[2];  // and what of them exists where that is not all of it
 
-  __device__ __forceinline__ static int swizzle(int k) { return S == 2 ? (k & 3) << 1 : (k >> 2 & 3) << 2; }
   // LDS row and chunk of this lane's part of line j
   __device__ __forceinline__ int row_of(int j) const { return (wave * LINES + j) * (64 / CPR) + lane / CPR; }
   __device__ __forceinline__ int chunk_of(int j) const {
-    return (lane % CPR) ^ (ACROSS ? swizzle(row_of(j)) : row_of(j) & 7);
+    return (lane % CPR) ^ (ACROSS ? across_swizzle<S, CPR>(row_of(j)) : row_of(j) & 7);
   }
 
   __device__ __forceinline__ void init(const T* origin, int64_t ld_, int64_t r0, int64_t r_end, int64_t k0, int64_t k_end,
@@ -243,13 +251,20 @@ struct Operand {
     }
   }
 
+  // line j of a stage in front of the end of k, straight to LDS; step() after the last
+  __device__ __forceinline__ void fetch_line(int j, uint32_t lds) const {
+    load_to_lds(reinterpret_cast<const char*>(base), offset[j], lds + (uint32_t)(wave * LINES + j) * 1024u);
+  }
+  __device__ __forceinline__ void step() {
+    base += ACROSS ? BK * ld : BK;
+    depth -= BK;
+  }
   // starts the loads of the next stage (to the LDS region `lds` for DMA, else to held[SLOT]) and steps on.
-  // WHOLE: the stage is known to lie in front of the end of k.
-  template <bool WHOLE = false, int SLOT = 0>
+  template <int SLOT = 0>
   __device__ __forceinline__ void fetch(uint32_t lds) {
     if constexpr (DMA) {
       const char* const p = reinterpret_cast<const char*>(base);
-      if (WHOLE || depth >= BK) {
+      if (depth >= BK) {
 #pragma unroll
         for (int j = 0; j < LINES; ++j) load_to_lds(p, offset[j], lds + (uint32_t)(wave * LINES + j) * 1024u);
       } else {
@@ -304,8 +319,7 @@ struct Operand {
       held_along[SLOT] = mend ? along : kVec << 20;
       held_lines[SLOT] = lines;
     }
-    base += ACROSS ? BK * ld : BK;
-    depth -= BK;
+    step();
     if constexpr (!ACROSS && !DMA) before = kVec;
   }
   // puts held[SLOT] into LDS
@@ -342,10 +356,10 @@ struct Fragments {
       for (int kk = 0; kk < 2; ++kk)
         at[kk] = (uint32_t)((row0 + j) * kStageBytes + ((kk * 4 + g) ^ (j & 7)) * 16);
     } else if constexpr (S == 2) {
-      // (row0 is a multiple of 32: its chunks leave the swizzled bits alone but for the lowest f's)
+      // (all k that a lane reads have its group's bit 3 and its own bits 0 and 1)
 #pragma unroll
       for (int f = 0; f < 4; ++f) {
-        const int chunk = (row0 / 8 + f * 2 + ((j & 3) >> 1)) ^ ((j >> 2) << 1);
+        const int chunk = (row0 / 8 + f * 2 + ((j & 3) >> 1)) ^ across_swizzle<S, ROWB / 16>(g * 8 + (j >> 2));
         at[f] = (uint32_t)((g * 8 + (j >> 2)) * ROWB + chunk * 16 + (j & 1) * 8);
       }
     } else {
@@ -360,8 +374,8 @@ struct Fragments {
     if constexpr (!ACROSS) {
       return *reinterpret_cast<const u32x4*>(lds + at[kk] + f * 16 * kStageBytes);
     } else if constexpr (S == 2) {
-      // four groups of 16 rows are 128 bytes: f / 4 steps over the swizzle
-      const char* const p = lds + at[f & 3] + (f >> 2) * 128 + kk * 32 * ROWB;
+      // the second four groups of 16 rows are 128 bytes on, a bit of its own in the place (row0 is a multiple of 128 there)
+      const char* const p = lds + (at[f & 3] ^ ((f >> 2) * 128)) + kk * 32 * ROWB;
       typedef __attribute__((address_space(3))) s16x4 Lds;
       const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)p));
       const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(p + 4 * ROWB)));
@@ -548,14 +562,38 @@ __global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_
     // between a stage's two halves: every wave has read all of the stage by then, so that its
     // region can be loaded anew, and the next stage's first half is read under the second's products.
     constexpr int EACH = OpA::LINES + OpB::LINES;
-    const auto fetch = [&](int slot, auto whole) {
-      a.template fetch<decltype(whole)::value>(lds0 + (uint32_t)slot * STAGE);
-      b.template fetch<decltype(whole)::value>(lds0 + (uint32_t)slot * STAGE + OpA::BYTES);
+    const auto fetch = [&](int slot) {
+      a.fetch(lds0 + (uint32_t)slot * STAGE);
+      b.fetch(lds0 + (uint32_t)slot * STAGE + OpA::BYTES);
+    };
+    // One half's products with the other's reads and a stage's loads between them, a row of fragments at a time:
+    // loads that set out together wait for each other and hold up the products behind them.
+    const auto weave = [&](const Half& h, Half& to, const char* from, int slot) {
+      constexpr int TOTAL = FM + FN;
+      const uint32_t la = lds0 + (uint32_t)slot * STAGE, lb = la + OpA::BYTES;
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+#pragma unroll
+        for (int e = i * EACH / FM; e < (i + 1) * EACH / FM; ++e) {
+          if (e < OpA::LINES) a.fetch_line(e, la);
+          else b.fetch_line(e - OpA::LINES, lb);
+        }
+#pragma unroll
+        for (int e = i * TOTAL / FM; e < (i + 1) * TOTAL / FM; ++e) {
+          if (e < FN) to.b[e] = fb.read(from + OpA::BYTES, e, 0);
+          else to.a[e - FN] = fa.read(from, e - FN, 0);
+        }
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = mfma_chunk<E>(h.b[j], h.a[i], acc[i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      a.step();
+      b.step();
     };
     Half h0, h1;
 #pragma unroll
     for (int q = 0; q < STAGES; ++q)
-      if (q < steps) fetch(q, std::false_type{});
+      if (q < steps) fetch(q);
     if (steps > 0) {
       if (steps >= STAGES) stage_wait<(STAGES - 1) * EACH>();
       else stage_wait<0>();
@@ -568,11 +606,23 @@ __global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_
       multiply(h0);
       interleave();
       stage_wait<(STAGES - 2) * EACH>();
-      fetch(cur, std::true_type{});
-      cur = next(cur);
-      read(h0, linear_lds + cur * STAGE, 0);
-      multiply(h1);
-      interleave();
+      if constexpr (E::kId != kStorageF32) {
+        weave(h1, h0, linear_lds + next(cur) * STAGE, cur);
+        cur = next(cur);
+      } else {
+        // (four products a pair of fragments: the loads are out of their way)
+        const uint32_t la = lds0 + (uint32_t)cur * STAGE;
+#pragma unroll
+        for (int e = 0; e < OpA::LINES; ++e) a.fetch_line(e, la);
+#pragma unroll
+        for (int e = 0; e < OpB::LINES; ++e) b.fetch_line(e, la + OpA::BYTES);
+        a.step();
+        b.step();
+        cur = next(cur);
+        read(h0, linear_lds + cur * STAGE, 0);
+        multiply(h1);
+        interleave();
+      }
     }
     for (; t < steps; ++t) {
       read(h1, linear_lds + cur * STAGE, 1);
@@ -581,7 +631,7 @@ __global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_
         // this stage is read; the next has landed when those after it are all that is left
         if (STAGES > 2 && t + STAGES - 1 < steps) stage_wait<(STAGES - 2) * EACH>();
         else stage_wait<0>();
-        if (t + STAGES < steps) fetch(cur, std::false_type{});
+        if (t + STAGES < steps) fetch(cur);
         cur = next(cur);
         read(h0, linear_lds + cur * STAGE, 0);
       }
@@ -592,8 +642,8 @@ __global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_
     // into the region that every wave has left at the last barrier, and stage t + 3 sets out.
     static_assert(DMA || STAGES == 2);
     const auto fetch = [&](auto slot) {
-      a.template fetch<false, decltype(slot)::value>(0);
-      b.template fetch<false, decltype(slot)::value>(0);
+      a.template fetch<decltype(slot)::value>(0);
+      b.template fetch<decltype(slot)::value>(0);
     };
     const auto commit = [&](auto slot) {
       constexpr int S = decltype(slot)::value;
@@ -859,7 +909,8 @@ LinearTable make_linear_table() {
     // (float32 products are bound by the matrix cores in the smallest tile already: 142 to 144 TFLOP/s)
     if constexpr (E::kId != kStorageF32) {
       t.fn[kTile128][o][0] = linear_launch<E, 128, 128, 2, 4, 2, AX, BX, false>;
-      t.fn[kTile128x256][o][0] = linear_launch<E, 128, 256, 2, 4, 2, AX, BX, false>;
+      // (both operands across k need more than the 256 registers there are)
+      if constexpr (!AX) t.fn[kTile128x256][o][0] = linear_launch<E, 128, 256, 2, 4, 2, AX, BX, false>;
       t.fn[kTile128][o][1] = linear_launch<E, 128, 128, 2, 4, 2, AX, BX, true>;
       t.fn[kTile128x256][o][1] = linear_launch<E, 128, 256, 2, 4, 3, AX, BX, true>;
       t.fn[kTile256][o][1] = linear_launch<E, 256, 256, 2, 4, 2, AX, BX, true>;
