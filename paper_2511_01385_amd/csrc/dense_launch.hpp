@@ -89,7 +89,8 @@ struct GemmArgs {
   int64_t k_split;
   int tiles_m, tiles_n;
 };
-// the instances for one storage type; null where one is not built.  Last index: 1 with loads straight to LDS
+// the instances for one storage type; null where one is not built.  Last index: 1 where
+// both operands' memory rows hold whole chunks of 16 bytes, at addresses that can be loaded straight to LDS
 enum LinearTile { kTile32x64, kTile64, kTile128, kTile128x256, kTile256, kLinearTiles };
 enum LinearOperands { kForward, kGradX, kGradW, kLinearOperands };
 using LinearFn = hipError_t (*)(const GemmArgs&, hipStream_t);

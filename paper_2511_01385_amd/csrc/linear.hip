@@ -167,7 +167,7 @@ static Plan plan_of(int64_t m, int64_t n, int64_t k, LinearOperands kind, int st
   double least = 0;
   for (int t = 0; t < kLinearTiles; ++t) {
     // what is not built
-    if ((f32 && t > kTile64) || (!direct && (t == kTile32x64 || t == kTile256))) continue;
+    if (f32 ? t > kTile64 : !direct && (t == kTile32x64 || t == kTile256)) continue;
     if (kind == kGradW && (t == kTile32x64 || (!direct && t == kTile128x256))) continue;
     const TileCost& c = f32 ? kCost32[t] : kCost16[t];
     const int64_t tiles = ((m + c.bm - 1) / c.bm) * ((n + c.bn - 1) / c.bn);
@@ -216,10 +216,11 @@ int64_t linear_backward_workspace(const LinearSizes& s, bool dx, bool dw, bool d
   return slope_bytes(s) + parts;
 }
 
-// Whether an operand's memory rows of `len` values start at multiples of 16 bytes and hold whole chunks.
+// Whether an operand's memory rows of `len` values hold whole chunks of 16 bytes and, of 16-bit values, start at
+// multiples of 16 bytes (floats may start anywhere).
 static bool whole_chunks(const void* p, int64_t ld, int64_t len, int storage) {
-  const int64_t s = storage_bytes(storage);
-  return (reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * s) | (uintptr_t)(len * s)) % 16 == 0;
+  if (storage == kStorageF32) return len % 4 == 0;
+  return (reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * 2) | (uintptr_t)(len * 2)) % 16 == 0;
 }
 
 static hipError_t product(GemmArgs& g, LinearOperands kind, int storage, void* workspace, hipStream_t stream) {

@@ -11,7 +11,7 @@
 // A workgroup computes a BM x BN tile of D; a stage of 128 bytes of k (64 16-bit values, 32
 // floats) of both operands lies in LDS, two stages in turn.  The stage after the one being
 // multiplied is under way in the meantime: by loads that go straight to LDS (16 bytes a lane), or
-// through registers where a row of an operand does not start at a multiple of 16 bytes.
+// through registers where a row of a 16-bit operand does not start at a multiple of 16 bytes.
 //
 // LDS layouts (units of 16 bytes, `pos` of a row holding chunk `pos ^ swizzle`):
 //   along k:   [BM rows][8 chunks], swizzle row & 7: the 16 rows of a fragment, read at one chunk,
@@ -136,13 +136,14 @@ __device__ __forceinline__ void times_slope8(int act, const float* z, float* g) 
 
 constexpr int kStageBytes = 128;  // of k, per row and stage
 
-// Loads that go straight to LDS: 64 lanes of 16 bytes from `base` + their offset to consecutive LDS
+// Loads that go straight to LDS: 64 lanes of 16 bytes (or four) from `base` + their offset to consecutive LDS
 // bytes from `lds`.  A lane whose offset is kNowhere stores zeros.  They are written as
 // assembly because the compiler, which cannot tell the two stages apart, would wait for them before
 // each LDS read; stage_wait() is the wait.  (No register receives anything.)
 constexpr uint32_t kNowhere = 0x80000000u;
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
+template <int BYTES = 16>
 __device__ __forceinline__ void load_to_lds(const char* base, uint32_t offset, uint32_t lds) {
   // (base and lds are the same in all lanes, which the compiler does not always see)
   const uint64_t p = reinterpret_cast<uint64_t>(base);
@@ -151,8 +152,12 @@ __device__ __forceinline__ void load_to_lds(const char* base, uint32_t offset, u
   lds = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds);
   const __amdgpu_buffer_rsrc_t r =
       __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<char*>(u), 0, (int)(kNowhere - 1), 0x00020000);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(r)
-               : "memory", "m0");
+  if constexpr (BYTES == 16)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(r)
+                 : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(r)
+                 : "memory", "m0");
 }
 #pragma clang diagnostic pop
 // all but the last LEFT of this wave's loads to LDS done, its LDS reads done, every wave here
@@ -205,11 +210,15 @@ __device__ __forceinline__ int across_swizzle(int k) {
   return CPR >= 16 ? (k & 3) << 1 | (k >> 3 & 1) << 3 : ((k & 3) ^ (k >> 3 & 1)) << 1;
 }
 
-// R rows (m or n) of one operand's stage.  ACROSS: memory rows run along m.  DMA: straight to
-// LDS, for which a memory row starts at a multiple of 16 bytes and holds whole chunks.
-template <class E, int R, int WAVES, bool ACROSS, bool DMA>
+// R rows (m or n) of one operand's stage.  ACROSS: memory rows run along m.  kDirect: straight to LDS, for which
+// memory rows hold whole chunks and, of 16-bit values, start at multiples of 16 bytes (these loads take any address that
+// is a multiple of four).  kDirectCut, floats only: the same where chunks may be cut, by the end of k or by the
+// operand's last row across k; such a stage is loaded value by value.
+enum LoadPath { kByRegisters, kDirect, kDirectCut };
+template <class E, int R, int WAVES, bool ACROSS, LoadPath PATH>
 struct Operand {
   using T = typename E::T;
+  static constexpr bool DMA = PATH != kByRegisters;
   static constexpr int S = sizeof(T), EPC = 16 / S, BK = kStageBytes / S;
   static constexpr int CPR = ACROSS ? R * S / 16 : 8;  // chunks of an LDS row
   static constexpr int BYTES = R * kStageBytes;
@@ -228,6 +237,8 @@ struct Operand {
 
   // LDS row and chunk of this lane's part of line j
   __device__ __forceinline__ int row_of(int j) const { return (wave * LINES + j) * (64 / CPR) + lane / CPR; }
+  // whether every stage has chunks that the operand's last row (across k) cuts
+  __device__ __forceinline__ bool cut() const { return PATH == kDirectCut && ACROSS && rows < R && rows % EPC != 0; }
   __device__ __forceinline__ int chunk_of(int j) const {
     return (lane % CPR) ^ (ACROSS ? across_swizzle<S, CPR>(row_of(j)) : row_of(j) & 7);
   }
@@ -264,7 +275,16 @@ struct Operand {
   __device__ __forceinline__ void fetch(uint32_t lds) {
     if constexpr (DMA) {
       const char* const p = reinterpret_cast<const char*>(base);
-      if (depth >= BK) {
+      if (PATH == kDirectCut && (cut() || (!ACROSS && depth < BK && depth % EPC != 0))) {
+#pragma unroll
+        for (int q = 0; q < LINES * 4; ++q) {  // 64 values each
+          const int place = q * 16 + lane / 4, line = wave * LINES * (64 / CPR) + place / CPR;
+          const int c = place % CPR ^ (ACROSS ? across_swizzle<S, CPR>(line) : line & 7);
+          const int i = c * EPC + lane % 4, r = ACROSS ? i : line, k = ACROSS ? line : i;
+          const uint32_t at = (uint32_t)line * (uint32_t)(ld * S) + (uint32_t)i * 4u;
+          load_to_lds<4>(p, r < rows && k < depth ? at : kNowhere, lds + (uint32_t)(wave * LINES) * 1024u + (uint32_t)q * 256u);
+        }
+      } else if (depth >= BK) {
 #pragma unroll
         for (int j = 0; j < LINES; ++j) load_to_lds(p, offset[j], lds + (uint32_t)(wave * LINES + j) * 1024u);
       } else {
@@ -495,15 +515,16 @@ __device__ __forceinline__ TileAt tile_of(int id, int tiles_m, int tiles_n, int 
   return {first + t % high, t / high, split};
 }
 
-template <class E, int BM, int BN, int WM, int WN, int STAGES, bool AX, bool BX, bool DMA>
+template <class E, int BM, int BN, int WM, int WN, int STAGES, bool AX, bool BX, LoadPath PATH>
 __global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2)))  // 256 registers, no second file
     linear_kernel(GemmArgs g) {
   using T = typename E::T;
   constexpr int WAVES = WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
   constexpr int BK = kStageBytes / (int)sizeof(T);
   static_assert(FN % 2 == 0, "a wave holds whole blocks of 32 values");
-  using OpA = Operand<E, BM, WAVES, AX, DMA>;
-  using OpB = Operand<E, BN, WAVES, BX, DMA>;
+  constexpr bool DMA = PATH != kByRegisters;
+  using OpA = Operand<E, BM, WAVES, AX, PATH>;
+  using OpB = Operand<E, BN, WAVES, BX, PATH>;
   constexpr int STAGE = OpA::BYTES + OpB::BYTES;
   extern __shared__ __attribute__((aligned(1024))) char linear_lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
@@ -561,7 +582,7 @@ __global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_
     // STAGES - 1 stages are under way ahead of the one being multiplied.  The barrier sits
     // between a stage's two halves: every wave has read all of the stage by then, so that its
     // region can be loaded anew, and the next stage's first half is read under the second's products.
-    constexpr int EACH = OpA::LINES + OpB::LINES;
+    constexpr int EACH = OpA::LINES + OpB::LINES;  // (a stage that is loaded value by value has more: its waits are longer)
     const auto fetch = [&](int slot) {
       a.fetch(lds0 + (uint32_t)slot * STAGE);
       b.fetch(lds0 + (uint32_t)slot * STAGE + OpA::BYTES);
@@ -601,7 +622,8 @@ __global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_
     }
     int cur = 0, t = 0;
     const auto next = [](int slot) { return slot + 1 == STAGES ? 0 : slot + 1; };
-    for (; t + STAGES < steps - 1; ++t) {  // (the stage that is fetched is not the last)
+    const int steady = a.cut() || b.cut() ? 0 : steps - 1 - STAGES;
+    for (; t < steady; ++t) {  // (the stage that is fetched is not the last)
       read(h1, linear_lds + cur * STAGE, 1);
       multiply(h0);
       interleave();
@@ -729,10 +751,10 @@ __global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_
   }
 }
 
-template <class E, int BM, int BN, int WM, int WN, int STAGES, bool AX, bool BX, bool DMA>
+template <class E, int BM, int BN, int WM, int WN, int STAGES, bool AX, bool BX, LoadPath PATH>
 hipError_t linear_launch(const GemmArgs& g, hipStream_t stream) {
   constexpr int lds = STAGES * (BM + BN) * kStageBytes;
-  const auto kernel = linear_kernel<E, BM, BN, WM, WN, STAGES, AX, BX, DMA>;
+  const auto kernel = linear_kernel<E, BM, BN, WM, WN, STAGES, AX, BX, PATH>;
   static const hipError_t ready = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                                       hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (ready != hipSuccess) return ready;
@@ -749,9 +771,10 @@ hipError_t linear_launch(const GemmArgs& g, hipStream_t stream) {
 // of its own, STAGES stages of 128 bytes of k a row, without a barrier: whole cache lines, many of them in
 // flight, and no registers held for them.  Without (rows that start anywhere) the fragments come from
 // memory, half a line a row and instruction.  The waves' sums meet in LDS.
-template <class E, int MT, int NT, int WAVES, int STAGES, bool DMA>
+template <class E, int MT, int NT, int WAVES, int STAGES, LoadPath PATH>
 __global__ void __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(2))) linear_few_kernel(GemmArgs g) {
   using T = typename E::T;
+  constexpr bool DMA = PATH != kByRegisters;
   constexpr int BK = kStageBytes / (int)sizeof(T), STAGE = 16 * (MT + NT) * kStageBytes;
   constexpr int PRIVATE = DMA ? STAGES * STAGE : NT * MT * 1024;
   static_assert(PRIVATE >= NT * MT * 1024);
@@ -774,8 +797,8 @@ __global__ void __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu
   const int64_t k0 = min(wave * per, g.k), k1 = min(k0 + per, g.k);
 
   if constexpr (DMA) {
-    Operand<E, 16 * NT, 1, false, true> w;
-    Operand<E, 16 * MT, 1, false, true> x;
+    Operand<E, 16 * NT, 1, false, PATH> w;
+    Operand<E, 16 * MT, 1, false, PATH> x;
     w.init(static_cast<const T*>(g.b), g.ldb, n0, g.n, k0, k1, 0, lane);
     x.init(static_cast<const T*>(g.a), g.lda, 0, g.m, k0, k1, 0, lane);
     Fragments<E, 16, false> f;
@@ -887,10 +910,10 @@ __global__ void __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu
   finish_group<E>(g, m, n0 + q * kVec, bias, z);
 }
 
-template <class E, int MT, int NT, int WAVES, int STAGES, bool DMA>
+template <class E, int MT, int NT, int WAVES, int STAGES, LoadPath PATH>
 hipError_t few_launch(const GemmArgs& g, hipStream_t stream) {
-  constexpr int lds = WAVES * (DMA ? STAGES * 16 * (MT + NT) * kStageBytes : NT * MT * 1024);
-  const auto kernel = linear_few_kernel<E, MT, NT, WAVES, STAGES, DMA>;
+  constexpr int lds = WAVES * (PATH != kByRegisters ? STAGES * 16 * (MT + NT) * kStageBytes : NT * MT * 1024);
+  const auto kernel = linear_few_kernel<E, MT, NT, WAVES, STAGES, PATH>;
   static const hipError_t ready = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                                       hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (ready != hipSuccess) return ready;
@@ -901,36 +924,42 @@ hipError_t few_launch(const GemmArgs& g, hipStream_t stream) {
 template <class E>
 LinearTable make_linear_table() {
   LinearTable t{};
+  constexpr bool F32 = E::kId == kStorageF32;
+  // the loads of whole chunks, and those of anything else
+  constexpr LoadPath W = kDirect, ANY = F32 ? kDirectCut : kByRegisters;
   const auto operands = [&](auto ax, auto bx, LinearOperands o) {
     constexpr bool AX = decltype(ax)::value, BX = decltype(bx)::value;
-    t.fn[kTile64][o][0] = linear_launch<E, 64, 64, 2, 2, 2, AX, BX, false>;
-    t.fn[kTile64][o][1] = linear_launch<E, 64, 64, 2, 2, 3, AX, BX, true>;
-    if constexpr (!AX) t.fn[kTile32x64][o][1] = linear_launch<E, 32, 64, 2, 2, 3, AX, BX, true>;
-    // (float32 products are bound by the matrix cores in the smallest tile already: 142 to 144 TFLOP/s)
-    if constexpr (E::kId != kStorageF32) {
-      t.fn[kTile128][o][0] = linear_launch<E, 128, 128, 2, 4, 2, AX, BX, false>;
+    t.fn[kTile64][o][0] = linear_launch<E, 64, 64, 2, 2, F32 ? 3 : 2, AX, BX, ANY>;
+    t.fn[kTile64][o][1] = linear_launch<E, 64, 64, 2, 2, 3, AX, BX, W>;
+    if constexpr (!AX) {
+      t.fn[kTile32x64][o][1] = linear_launch<E, 32, 64, 2, 2, 3, AX, BX, W>;
+      if constexpr (F32) t.fn[kTile32x64][o][0] = linear_launch<E, 32, 64, 2, 2, 3, AX, BX, ANY>;
+    }
+    // (float32 products are bound by the matrix cores in the smallest tiles already: 142 to 144 TFLOP/s)
+    if constexpr (!F32) {
+      t.fn[kTile128][o][0] = linear_launch<E, 128, 128, 2, 4, 2, AX, BX, ANY>;
       // (both operands across k need more than the 256 registers there are)
-      if constexpr (!AX) t.fn[kTile128x256][o][0] = linear_launch<E, 128, 256, 2, 4, 2, AX, BX, false>;
-      t.fn[kTile128][o][1] = linear_launch<E, 128, 128, 2, 4, 2, AX, BX, true>;
-      t.fn[kTile128x256][o][1] = linear_launch<E, 128, 256, 2, 4, 3, AX, BX, true>;
-      t.fn[kTile256][o][1] = linear_launch<E, 256, 256, 2, 4, 2, AX, BX, true>;
+      if constexpr (!AX) t.fn[kTile128x256][o][0] = linear_launch<E, 128, 256, 2, 4, 2, AX, BX, ANY>;
+      t.fn[kTile128][o][1] = linear_launch<E, 128, 128, 2, 4, 2, AX, BX, W>;
+      t.fn[kTile128x256][o][1] = linear_launch<E, 128, 256, 2, 4, 3, AX, BX, W>;
+      t.fn[kTile256][o][1] = linear_launch<E, 256, 256, 2, 4, 2, AX, BX, W>;
     }
   };
   operands(std::false_type{}, std::false_type{}, kForward);
   operands(std::false_type{}, std::true_type{}, kGradX);
   operands(std::true_type{}, std::true_type{}, kGradW);
-  t.few[0][0][1] = few_launch<E, 1, 1, 8, 4, true>;
-  t.few[0][1][1] = few_launch<E, 1, 2, 4, 6, true>;
-  t.few[1][0][1] = few_launch<E, 2, 1, 4, 6, true>;
-  t.few[1][1][1] = few_launch<E, 2, 2, 4, 4, true>;
-  t.few[2][0][1] = few_launch<E, 4, 1, 4, 4, true>;
-  t.few[2][1][1] = few_launch<E, 4, 2, 4, 3, true>;
-  t.few[0][0][0] = few_launch<E, 1, 1, 8, 0, false>;
-  t.few[0][1][0] = few_launch<E, 1, 2, 8, 0, false>;
-  t.few[1][0][0] = few_launch<E, 2, 1, 8, 0, false>;
-  t.few[1][1][0] = few_launch<E, 2, 2, 8, 0, false>;
-  t.few[2][0][0] = few_launch<E, 4, 1, 8, 0, false>;
-  t.few[2][1][0] = few_launch<E, 4, 2, 8, 0, false>;
+  t.few[0][0][1] = few_launch<E, 1, 1, 8, 4, W>;
+  t.few[0][1][1] = few_launch<E, 1, 2, 4, 6, W>;
+  t.few[1][0][1] = few_launch<E, 2, 1, 4, 6, W>;
+  t.few[1][1][1] = few_launch<E, 2, 2, 4, 4, W>;
+  t.few[2][0][1] = few_launch<E, 4, 1, 4, 4, W>;
+  t.few[2][1][1] = few_launch<E, 4, 2, 4, 3, W>;
+  t.few[0][0][0] = few_launch<E, 1, 1, 8, F32 ? 4 : 0, ANY>;
+  t.few[0][1][0] = few_launch<E, 1, 2, F32 ? 4 : 8, F32 ? 6 : 0, ANY>;
+  t.few[1][0][0] = few_launch<E, 2, 1, F32 ? 4 : 8, F32 ? 6 : 0, ANY>;
+  t.few[1][1][0] = few_launch<E, 2, 2, F32 ? 4 : 8, F32 ? 4 : 0, ANY>;
+  t.few[2][0][0] = few_launch<E, 4, 1, F32 ? 4 : 8, F32 ? 4 : 0, ANY>;
+  t.few[2][1][0] = few_launch<E, 4, 2, F32 ? 4 : 8, F32 ? 3 : 0, ANY>;
   return t;
 }
 
