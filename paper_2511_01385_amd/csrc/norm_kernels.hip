@@ -13,6 +13,11 @@
 // the backward the sums of dw and db over its rows.  The groups of a workgroup are added in LDS
 // in a fixed order and each workgroup leaves one row of partial sums (2n floats); a second launch adds
 // those.  No atomics: results do not depend on the order of execution.
+//
+// 16384 x 4096 bf16 with a residual and a checkpoint: forward 88 us (472 MB, 5.4 TB/s), backward 69 us (337 MB,
+// 4.9 TB/s) and 4 us for the join; 4096 x 768: 7.4, 8.1 and 1.8 us, two or three trips to memory one after another.  One
+// wave per row up to 1024 values (no barrier), a workgroup beyond; rows of more than 8192 values run at about 60 %
+// of those rates in the backward, whose threads then hold two groups each and spill.
 #include <hip/hip_runtime.h>
 
 #include "dense_device.hpp"
