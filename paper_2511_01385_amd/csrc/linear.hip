@@ -48,8 +48,8 @@ static hipError_t join(GemmArgs g, hipStream_t stream) {
 }
 
 // ----------------------------------------------------------------------------------
-// dz = dy act'(z), z from its checkpoint, rounded once to the storage type (it is a matrix operand),
-// and the column sums of the unrounded dz.  A workgroup takes a strip of 512 columns, its four
+// dz = dy act'(z), z from its checkpoint, rounded once to the storage type (it is a matrix operand), in rows of
+// slope_pitch values so that it is loaded like an aligned operand whatever d_out, and the column sums of the unrounded dz.  A workgroup takes a strip of 512 columns, its four
 // waves every fourth row of its range; partials[blockIdx.y][n] receive the sums, or db where there is one range.
 // 8192 x 8192 bf16: 72 us (346 MB, 4.8 TB/s; one row at a time in a wave 88), 4096 x 768: 8 us (16).
 constexpr int kSlopeWG = 256, kSlopeWaves = 4, kSlopeStrip = 64 * kVec, kSlopeAhead = 4;
@@ -58,7 +58,8 @@ constexpr int64_t kSlopeMaxParts = 256;
 template <class E, bool EXACT>
 __global__ void __launch_bounds__(kSlopeWG)
     linear_slope_kernel(const typename E::T* __restrict__ dy, int64_t ldg, Checkpoint ck, typename E::T* __restrict__ dz,
-                        float* __restrict__ partials, typename E::T* __restrict__ db, int rows, int per, int n, int act) {
+                        int64_t ldz, float* __restrict__ partials, typename E::T* __restrict__ db, int rows, int per, int n,
+                        int act) {
   __shared__ float sums[kSlopeWaves][kSlopeStrip];
   const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
   const int i = blockIdx.x * kSlopeStrip + lane * kVec;
@@ -71,8 +72,7 @@ __global__ void __launch_bounds__(kSlopeWG)
         float z[kVec];
         ck_decode(code, ck_scale(byte), z);
         times_slope8(act, z, g);
-        if constexpr (EXACT) E::store(dz + (int64_t)r * n + i, g);
-        else write_group<E>(dz + (int64_t)r * n, i, n, g);
+        E::store(dz + r * ldz + i, g);  // (rows are padded to whole groups, with zeros)
       }
 #pragma unroll
       for (int k = 0; k < kVec; ++k) s[k] += g[k];
@@ -129,6 +129,8 @@ __global__ void __launch_bounds__(kSlopeWG)
     else partials[(int64_t)blockIdx.y * n + col] = v;
   }
 }
+
+static int64_t slope_pitch(int64_t n) { return (n + kVec - 1) / kVec * kVec; }
 
 // row ranges that fill the chip's wave slots (eight workgroups a CU), of sixteen rows at least
 static int64_t slope_parts(int64_t rows, int64_t n) {
@@ -207,7 +209,7 @@ int64_t linear_forward_workspace(const LinearSizes& s) {
 
 // dz, then the partial sums of whichever pass runs (they follow each other on the stream)
 static int64_t slope_bytes(const LinearSizes& s) {
-  return s.act == kActNone ? 0 : round_up(s.tokens * s.d_out * storage_bytes(s.storage));
+  return s.act == kActNone ? 0 : round_up(s.tokens * slope_pitch(s.d_out) * storage_bytes(s.storage));
 }
 int64_t linear_backward_workspace(const LinearSizes& s, bool dx, bool dw, bool db) {
   int64_t parts = 0;
@@ -224,10 +226,12 @@ static bool whole_chunks(const void* p, int64_t ld, int64_t len, int storage) {
   return (reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * 2) | (uintptr_t)(len * 2)) % 16 == 0;
 }
 
-static hipError_t product(GemmArgs& g, LinearOperands kind, int storage, void* workspace, hipStream_t stream) {
+// a_len: values in a memory row of A that may be loaded (those past its end are zeros)
+static hipError_t product(GemmArgs& g, int64_t a_len, LinearOperands kind, int storage, void* workspace,
+                          hipStream_t stream) {
   static const LinearTable tables[] = {linear_table_f32(), linear_table_bf16(), linear_table_f16()};
   const LinearTable& t = tables[storage];
-  const bool direct = whole_chunks(g.a, g.lda, kind == kGradW ? g.m : g.k, storage) &&
+  const bool direct = whole_chunks(g.a, g.lda, a_len, storage) &&
                       whole_chunks(g.b, g.ldb, kind == kForward ? g.k : g.n, storage);
   g.splits = 1;
   if (kind == kForward && g.m <= kFewTokens) {
@@ -261,7 +265,7 @@ hipError_t launch_linear_forward(const LinearForward& a, hipStream_t stream) {
   g.ldr = a.ldr;
   g.ck = a.ck;
   g.act = a.s.act;
-  return product(g, kForward, a.s.storage, a.workspace, stream);
+  return product(g, g.k, kForward, a.s.storage, a.workspace, stream);
 }
 
 hipError_t launch_linear_backward(const LinearBackward& a, hipStream_t stream) {
@@ -269,7 +273,7 @@ hipError_t launch_linear_backward(const LinearBackward& a, hipStream_t stream) {
   const int storage = a.s.storage;
   char* const parts = static_cast<char*>(a.workspace) + slope_bytes(a.s);
   const void* dz = a.dy;
-  int64_t ldz = a.ldg;
+  int64_t ldz = a.ldg, dz_len = n;
   hipError_t e = hipSuccess;
   if (a.s.act != kActNone || a.db != nullptr) {
     const int64_t count = slope_parts(T, n), per = (T + count - 1) / count;
@@ -280,8 +284,8 @@ hipError_t launch_linear_backward(const LinearBackward& a, hipStream_t stream) {
       const auto go = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)((n + kSlopeStrip - 1) / kSlopeStrip), (unsigned)count), dim3(kSlopeWG),
                            0, stream, static_cast<const typename E::T*>(a.dy), a.ldg, a.ck,
-                           static_cast<typename E::T*>(a.workspace), partials, static_cast<typename E::T*>(db), (int)T,
-                           (int)per, (int)n, a.s.act);
+                           static_cast<typename E::T*>(a.workspace), slope_pitch(n), partials,
+                           static_cast<typename E::T*>(db), (int)T, (int)per, (int)n, a.s.act);
         return hipGetLastError();
       };
       return n % kVec == 0 ? go(linear_slope_kernel<E, true>) : go(linear_slope_kernel<E, false>);
@@ -291,7 +295,7 @@ hipError_t launch_linear_backward(const LinearBackward& a, hipStream_t stream) {
     if (e != hipSuccess) return e;
     if (a.s.act != kActNone) {
       dz = a.workspace;
-      ldz = n;
+      ldz = dz_len = slope_pitch(n);
     }
   }
   if (a.dx != nullptr && T > 0) {
@@ -307,7 +311,7 @@ hipError_t launch_linear_backward(const LinearBackward& a, hipStream_t stream) {
     g.ldd = a.ldd;
     g.residual = a.add;
     g.ldr = a.lda;
-    e = product(g, kGradX, storage, parts, stream);
+    e = product(g, dz_len, kGradX, storage, parts, stream);
     if (e != hipSuccess) return e;
   }
   if (a.dw != nullptr) {
@@ -321,7 +325,7 @@ hipError_t launch_linear_backward(const LinearBackward& a, hipStream_t stream) {
     g.k = T;
     g.d = a.dw;
     g.ldd = a.lddw;
-    e = product(g, kGradW, storage, parts, stream);
+    e = product(g, dz_len, kGradW, storage, parts, stream);
   }
   return e;
 }

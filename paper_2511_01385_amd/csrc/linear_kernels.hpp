@@ -9,8 +9,8 @@
 // are runs of m (a[k * lda + m]).
 //
 // A workgroup computes a BM x BN tile of D; a stage of 128 bytes of k (64 16-bit values, 32
-// floats) of both operands lies in LDS, two stages in turn.  The stage after the one being
-// multiplied is under way in the meantime: by loads that go straight to LDS (16 bytes a lane), or
+// floats) of both operands lies in LDS, two or three stages in turn.  The stages after the one being
+// multiplied are under way in the meantime: by loads that go straight to LDS (16 bytes a lane), or
 // through registers where a row of a 16-bit operand does not start at a multiple of 16 bytes.
 //
 // LDS layouts (units of 16 bytes, `pos` of a row holding chunk `pos ^ swizzle`):
@@ -27,10 +27,11 @@
 // blocks run.  k is spread over a fragment's four lane groups in runs of one chunk, for both
 // operands alike.  Sums are float32 throughout.
 //
-// What bounds it: 8192 x 4096 x 8192 (bf16, normal values) takes 403 us, 1360 TFLOP/s, next to 1300 to 1470 of the
-// library's bare products on the same card; the matrix cores are busy 74 % of the CUs' cycles, at a clock that
-// such work takes down to about 1.9 GHz.  The forward of 8192 tokens, 4096 -> 8192, takes 387 us without anything in its epilogue
-// (library 375), 410 with gelu, 440 with the checkpoint and 466 with both: the epilogues of a round of tiles coincide.
+// What bounds it: 8192 x 4096 x 8192 (bf16, normal values) takes 395 us, 1390 TFLOP/s, next to 1300 to
+// 1470 of the library's bare products on the same card; the matrix cores are busy 74 % of the CUs'
+// cycles, at a clock that such work takes down to about 1.9 GHz.  The forward of 8192 tokens, 4096 ->
+// 8192, takes 387 us without anything in its epilogue (library 375), 410 with gelu, 440 with the
+// checkpoint and 466 with both: the epilogues of a round of tiles coincide.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -141,10 +142,10 @@ __device__ __forceinline__ void times_slope8(int act, const float* z, float* g) 
 
 constexpr int kStageBytes = 128;  // of k, per row and stage
 
-// Loads that go straight to LDS: 64 lanes of 16 bytes (or four) from `base` + their offset to consecutive LDS
-// bytes from `lds`.  A lane whose offset is kNowhere stores zeros.  They are written as
-// assembly because the compiler, which cannot tell the two stages apart, would wait for them before
-// each LDS read; stage_wait() is the wait.  (No register receives anything.)
+// Loads that go straight to LDS: 64 lanes of 16 bytes (or four) from `base` + their offset to consecutive
+// LDS bytes from `lds`.  A lane whose offset is kNowhere stores zeros.  They are written as assembly
+// because the compiler, which cannot tell the stages apart, would wait for them before each LDS
+// read; stage_wait() and loads_wait() are the waits.  (No register receives anything.)
 constexpr uint32_t kNowhere = 0x80000000u;
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
@@ -712,7 +713,8 @@ __global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_
   // Each wave turns its results through LDS of its own (no wave reads stages any more), PART blocks of 16 rows at a
   // time, into runs of eight along n: the lanes of a row then read and write whole cache lines.  16 bytes c of a row lie
   // at (c / 2, odd ones in the second half) xor row: neither side meets in a bank.
-  constexpr int PART = FM >= 4 && WAVES * 4 * 16 * TN * 4 <= STAGES * STAGE ? 4 : FM >= 2 ? 2 : 1, CH = TN / 4, RUNS = TN / kVec, ROWS = 64 / RUNS, PASSES = 16 * PART / ROWS;
+  constexpr int PART = FM >= 4 && WAVES * 4 * 16 * TN * 4 <= STAGES * STAGE ? 4 : FM >= 2 ? 2 : 1;
+  constexpr int CH = TN / 4, RUNS = TN / kVec, ROWS = 64 / RUNS, PASSES = 16 * PART / ROWS;
   static_assert(WAVES * PART * 16 * TN * 4 <= STAGES * STAGE && FM % PART == 0);
   char* const turn = linear_lds + wave * (PART * 16 * TN * 4);
   const auto slot = [](int row, int c) { return (row * CH + (((c >> 1) | (c & 1) * (CH / 2)) ^ (row & (CH - 1)))) * 16; };
@@ -773,8 +775,8 @@ hipError_t linear_launch(const GemmArgs& g, hipStream_t stream) {
 // W's rows, each of its waves a range of k.  With direct loads a wave streams its part of both operands through LDS
 // of its own, STAGES stages of 128 bytes of k a row, without a barrier: whole cache lines, many of them in
 // flight, and no registers held for them.  Without (rows that start anywhere) the fragments come from
-// memory, half a line a row and instruction.  The waves' sums meet in LDS.  One token of 4096 x 4096: 4.8 us (33.6 MB that the
-// Infinity Cache holds: 7 TB/s), 6.8 without; 61 tokens, 1024 -> 4096: 4.3 and 6.9.
+// memory, half a line a row and instruction.  The waves' sums meet in LDS.  One token of 4096 x 4096: 4.8 us
+// (33.6 MB that the Infinity Cache holds: 7 TB/s), 6.8 without; 61 tokens, 1024 -> 4096: 4.3 and 6.9.
 template <class E, int MT, int NT, int WAVES, int STAGES, LoadPath PATH>
 __global__ void __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(2))) linear_few_kernel(GemmArgs g) {
   using T = typename E::T;
