@@ -48,9 +48,10 @@ static hipError_t join(GemmArgs g, hipStream_t stream) {
 }
 
 // ----------------------------------------------------------------------------------
-// dz = dy act'(z), z from its checkpoint, rounded once to the storage type (it is a matrix operand), in rows of
-// slope_pitch values so that it is loaded like an aligned operand whatever d_out, and the column sums of the unrounded dz.  A workgroup takes a strip of 512 columns, its four
-// waves every fourth row of its range; partials[blockIdx.y][n] receive the sums, or db where there is one range.
+// dz = dy act'(z), z from its checkpoint, rounded once to the storage type (it is a matrix operand), in rows
+// of slope_pitch values, so that it is loaded like an aligned operand whatever d_out; and the column sums
+// of the unrounded dz.  A workgroup takes a strip of 512 columns, its four waves every fourth row of its
+// range; partials[blockIdx.y][n] receive the sums, or db where there is one range.
 // 8192 x 8192 bf16: 72 us (346 MB, 4.8 TB/s; one row at a time in a wave 88), 4096 x 768: 8 us (16).
 constexpr int kSlopeWG = 256, kSlopeWaves = 4, kSlopeStrip = 64 * kVec, kSlopeAhead = 4;
 constexpr int64_t kSlopeMaxParts = 256;
