@@ -124,5 +124,23 @@ def load() -> ctypes.CDLL:
     return lib
 
 
+_binding = None
+
+
+def binding():
+    """The native module that takes torch tensors (csrc/binding.cpp); it calls the same library."""
+    global _binding
+    if _binding is None:
+        load()
+        import torch  # noqa: F401  (whose libraries the module needs)
+
+        try:
+            from . import _binding as module
+        except ImportError as e:
+            raise ImportError(f"the _binding module is not built ({e}); run paper_2511_01385_amd.build.build() first") from e
+        _binding = module
+    return _binding
+
+
 def status_string(status: int) -> str:
     return load().rdfft_status_string(status).decode()

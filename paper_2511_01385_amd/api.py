@@ -244,6 +244,9 @@ def bca_backward_batched(xs, c_spectras, gys, dxs, dcs):
 # The operators around the adapter.  Tensors of the storage type are two-dimensional with
 # consecutive elements in a row; a row stride of their own (a slice of wider rows) is fine.  A checkpoint is the
 # pair (codes, scales): int8 (rows, n) and uint8 (rows, ceil(n / 32)).
+#
+# Each call goes through the native module, which takes the tensors as they are (a call's checks take 0.1 to 0.3 us
+# there and 2 to 5 here); where that finds a tensor that is not what the call needs, what follows says so.
 
 CHECKPOINT_BLOCK = 32
 ACTIVATIONS = {"none": _lib.RDFFT_ACT_NONE, "relu": _lib.RDFFT_ACT_RELU, "gelu": _lib.RDFFT_ACT_GELU,
@@ -346,10 +349,15 @@ def checkpoint_like(x: torch.Tensor) -> tuple[torch.Tensor, torch.Tensor]:
 
 def act8_quantize(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor):
     """The 8-bit checkpoint of x (rows, n): int8 codes, and one scale byte for 32 values of a row."""
-    p, ld, shape, dtype, code, device, stream = _first(x, "x")
-    rows, n = shape
-    held = _lib.pack["act8"](*_held((codes, scales), device, rows, n))
-    status = _lib.load().act8_quantize(p, ld, held, rows, n, code, stream)
+    status = None
+    if x.is_cuda:
+        device = _current_device()
+        status = _lib.binding().act8_quantize(x, codes, scales, device, _raw_stream(device))
+    if status is None:
+        p, ld, shape, dtype, code, device, stream = _first(x, "x")
+        rows, n = shape
+        held = _lib.pack["act8"](*_held((codes, scales), device, rows, n))
+        status = _lib.load().act8_quantize(p, ld, held, rows, n, code, stream)
     if status:
         _check(status, "act8_quantize")
     return codes, scales
@@ -357,16 +365,22 @@ def act8_quantize(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor):
 
 def act8_dequantize(codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor) -> torch.Tensor:
     """What a checkpoint stands for, in ``out``'s type (exact in float32 and bfloat16)."""
-    p, ld, shape, dtype, code, device, stream = _first(out, "out")
-    rows, n = shape
-    held = _lib.pack["act8"](*_held((codes, scales), device, rows, n))
-    status = _lib.load().act8_dequantize(held, p, ld, rows, n, code, stream)
+    status = None
+    if out.is_cuda:
+        device = _current_device()
+        status = _lib.binding().act8_dequantize(codes, scales, out, device, _raw_stream(device))
+    if status is None:
+        p, ld, shape, dtype, code, device, stream = _first(out, "out")
+        rows, n = shape
+        held = _lib.pack["act8"](*_held((codes, scales), device, rows, n))
+        status = _lib.load().act8_dequantize(held, p, ld, rows, n, code, stream)
     if status:
         _check(status, "act8_dequantize")
     return out
 
 
 _F32 = torch.float32
+_NONE = (None, None)
 
 
 def layer_norm_forward(x, weight, bias, y, *, residual=None, mean=None, rstd=None, checkpoint=None, eps=1e-5):
@@ -375,18 +389,25 @@ def layer_norm_forward(x, weight, bias, y, *, residual=None, mean=None, rstd=Non
     ``mean`` and ``rstd`` (rows,) and ``checkpoint``, of the norm's input, are written if given.
     ``y`` may be ``x`` or ``residual``.
     """
-    p, ld, shape, dtype, code, device, stream = _first(x, "x")
-    rows, n = shape
-    a = _lib.pack["layer_norm_forward"](
-        p, ld,
-        *((0, 0) if residual is None else _rows(residual, "residual", dtype, device, shape)),
-        _vector(weight, "weight", _F32, device, n),
-        0 if bias is None else _vector(bias, "bias", _F32, device, n),
-        *_rows(y, "y", dtype, device, shape),
-        0 if mean is None else _vector(mean, "mean", _F32, device, rows),
-        0 if rstd is None else _vector(rstd, "rstd", _F32, device, rows),
-        *((0, 0) if checkpoint is None else _held(checkpoint, device, rows, n)))
-    status = _lib.load().layer_norm_forward(a, rows, n, eps, code, stream)
+    status = None
+    if x.is_cuda:
+        device = _current_device()
+        codes, scales = checkpoint or _NONE
+        status = _lib.binding().layer_norm_forward(x, residual, weight, bias, y, mean, rstd, codes, scales, eps, device,
+                                                   _raw_stream(device))
+    if status is None:
+        p, ld, shape, dtype, code, device, stream = _first(x, "x")
+        rows, n = shape
+        a = _lib.pack["layer_norm_forward"](
+            p, ld,
+            *((0, 0) if residual is None else _rows(residual, "residual", dtype, device, shape)),
+            _vector(weight, "weight", _F32, device, n),
+            0 if bias is None else _vector(bias, "bias", _F32, device, n),
+            *_rows(y, "y", dtype, device, shape),
+            0 if mean is None else _vector(mean, "mean", _F32, device, rows),
+            0 if rstd is None else _vector(rstd, "rstd", _F32, device, rows),
+            *((0, 0) if checkpoint is None else _held(checkpoint, device, rows, n)))
+        status = _lib.load().layer_norm_forward(a, rows, n, eps, code, stream)
     if status:
         _check(status, "layer_norm_forward")
     return y
@@ -398,23 +419,30 @@ def layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, *, residu
     ``x`` is the forward's x, or the checkpoint (codes, scales) of the norm's input; ``dx`` may be ``dy``.
     ``workspace``: ``layer_norm_backward_workspace(rows, n)`` bytes, allocated if not given.
     """
-    p, ld, shape, dtype, code, device, stream = _first(dy, "dy")
-    rows, n = shape
-    if isinstance(x, torch.Tensor):
-        inputs = (*_rows(x, "x", dtype, device, shape),
-                  *((0, 0) if residual is None else _rows(residual, "residual", dtype, device, shape)), 0, 0)
-    else:
-        if residual is not None:
-            raise ValueError("a checkpoint is of the norm's input, residual included")
-        inputs = (0, 0, 0, 0, *_held(x, device, rows, n))
-    keep, scratch, size = _scratch(_need("layer_norm_backward_workspace", rows, n), workspace, device,
-                                   "layer_norm_backward")
-    a = _lib.pack["layer_norm_backward"](
-        p, ld, *inputs, _vector(weight, "weight", _F32, device, n),
-        _vector(mean, "mean", _F32, device, rows), _vector(rstd, "rstd", _F32, device, rows),
-        *_rows(dx, "dx", dtype, device, shape), _vector(dweight, "dweight", _F32, device, n),
-        _vector(dbias, "dbias", _F32, device, n), scratch, size)
-    status = _lib.load().layer_norm_backward(a, rows, n, code, stream)
+    status = None
+    values = isinstance(x, torch.Tensor)
+    if not values and residual is not None:
+        raise ValueError("a checkpoint is of the norm's input, residual included")
+    if dy.is_cuda:
+        device = _current_device()
+        codes, scales = _NONE if values else x
+        status = _lib.binding().layer_norm_backward(dy, x if values else None, residual, codes, scales, weight, mean, rstd,
+                                                    dx, dweight, dbias, workspace, device, _raw_stream(device))
+    if status is None:
+        p, ld, shape, dtype, code, device, stream = _first(dy, "dy")
+        rows, n = shape
+        if values:
+            inputs = (*_rows(x, "x", dtype, device, shape),
+                      *((0, 0) if residual is None else _rows(residual, "residual", dtype, device, shape)), 0, 0)
+        else:
+            inputs = (0, 0, 0, 0, *_held(x, device, rows, n))
+        keep, scratch, size = _scratch(_need("layer_norm_backward_workspace", rows, n), workspace, device,
+                                       "layer_norm_backward")
+        a = _lib.pack["layer_norm_backward"](
+            p, ld, *inputs, _vector(weight, "weight", _F32, device, n), _vector(mean, "mean", _F32, device, rows),
+            _vector(rstd, "rstd", _F32, device, rows), *_rows(dx, "dx", dtype, device, shape),
+            _vector(dweight, "dweight", _F32, device, n), _vector(dbias, "dbias", _F32, device, n), scratch, size)
+        status = _lib.load().layer_norm_backward(a, rows, n, code, stream)
     if status:
         _check(status, "layer_norm_backward")
     return dx, dweight, dbias
@@ -438,20 +466,28 @@ def linear_forward(x, w, y, *, bias=None, activation="none", residual=None, chec
     ``checkpoint``, of the pre-activation, is written if given.  ``y`` may be ``residual``.
     ``workspace``: ``linear_forward_workspace(...)`` bytes, allocated if not given.
     """
-    p, ld, shape, dtype, code, device, stream = _first(x, "x")
-    tokens, d_in = shape
-    d_out = w.shape[0]
-    act = _activation(activation)
-    out = (tokens, d_out)
-    keep, scratch, size = _scratch(_need("linear_forward_workspace", d_in, d_out, tokens, code), workspace, device,
-                                   "linear_forward")
-    a = _lib.pack["linear_forward"](
-        p, ld, *_rows(w, "w", dtype, device, (d_out, d_in)),
-        0 if bias is None else _vector(bias, "bias", dtype, device, d_out),
-        *((0, 0) if residual is None else _rows(residual, "residual", dtype, device, out)),
-        *_rows(y, "y", dtype, device, out),
-        *((0, 0) if checkpoint is None else _held(checkpoint, device, tokens, d_out)), scratch, size)
-    status = _lib.load().linear_forward(a, d_in, d_out, tokens, act, code, stream)
+    status = None
+    act = ACTIVATIONS.get(activation)
+    if x.is_cuda and act is not None:
+        device = _current_device()
+        codes, scales = checkpoint or _NONE
+        status = _lib.binding().linear_forward(x, w, bias, residual, y, codes, scales, act, workspace, device,
+                                               _raw_stream(device))
+    if status is None:
+        p, ld, shape, dtype, code, device, stream = _first(x, "x")
+        tokens, d_in = shape
+        d_out = w.shape[0]
+        act = _activation(activation)
+        out = (tokens, d_out)
+        keep, scratch, size = _scratch(_need("linear_forward_workspace", d_in, d_out, tokens, code), workspace, device,
+                                       "linear_forward")
+        a = _lib.pack["linear_forward"](
+            p, ld, *_rows(w, "w", dtype, device, (d_out, d_in)),
+            0 if bias is None else _vector(bias, "bias", dtype, device, d_out),
+            *((0, 0) if residual is None else _rows(residual, "residual", dtype, device, out)),
+            *_rows(y, "y", dtype, device, out),
+            *((0, 0) if checkpoint is None else _held(checkpoint, device, tokens, d_out)), scratch, size)
+        status = _lib.load().linear_forward(a, d_in, d_out, tokens, act, code, stream)
     if status:
         _check(status, "linear_forward")
     return y
@@ -469,38 +505,46 @@ def linear_backward(dy, x, w, *, dx=None, dw=None, db=None, activation="none", c
     z is what ``checkpoint`` stands for (not needed without an activation).  ``x`` may be None without dw, ``w``
     without dx; ``dx`` may be ``add``.  ``workspace``: ``linear_backward_workspace(...)`` bytes, allocated if not given.
     """
-    p, ld, shape, dtype, code, device, stream = _first(dy, "dy")
-    tokens, d_out = shape
-    act = _activation(activation)
-    d_in = 1  # (db alone)
-    if dx is not None:
-        if w is None:
-            raise ValueError("dx needs w")
-        d_in = dx.shape[-1]
-    if dw is not None:
-        if x is None:
-            raise ValueError("dw needs x")
-        if dx is not None and dw.shape[-1] != d_in:
-            raise ValueError(f"dx and dw have {d_in} and {dw.shape[-1]} columns")
-        d_in = dw.shape[-1]
-    held = (0, 0)
-    if act != _lib.RDFFT_ACT_NONE:
-        if checkpoint is None:
-            raise ValueError(f"the gradient through {activation} needs the checkpoint of the pre-activation")
-        held = _held(checkpoint, device, tokens, d_out)
-    none = (0, 0)
-    keep, scratch, size = _scratch(
-        _need("linear_backward_workspace", d_in, d_out, tokens, dx is not None, dw is not None, db is not None, act, code),
-        workspace, device, "linear_backward")
-    a = _lib.pack["linear_backward"](
-        p, ld, *held,
-        *(none if dw is None else _rows(x, "x", dtype, device, (tokens, d_in))),
-        *(none if dx is None else _rows(w, "w", dtype, device, (d_out, d_in))),
-        *(none if dx is None or add is None else _rows(add, "add", dtype, device, (tokens, d_in))),
-        *(none if dx is None else _rows(dx, "dx", dtype, device, (tokens, d_in))),
-        *(none if dw is None else _rows(dw, "dw", dtype, device, (d_out, d_in))),
-        0 if db is None else _vector(db, "db", dtype, device, d_out), scratch, size)
-    status = _lib.load().linear_backward(a, d_in, d_out, tokens, act, code, stream)
+    status = None
+    act = ACTIVATIONS.get(activation)
+    if dy.is_cuda and act is not None:
+        device = _current_device()
+        codes, scales = checkpoint or _NONE
+        status = _lib.binding().linear_backward(dy, x, w, dx, dw, db, add, codes, scales, act, workspace, device,
+                                                _raw_stream(device))
+    if status is None:
+        p, ld, shape, dtype, code, device, stream = _first(dy, "dy")
+        tokens, d_out = shape
+        act = _activation(activation)
+        d_in = 1  # (db alone)
+        if dx is not None:
+            if w is None:
+                raise ValueError("dx needs w")
+            d_in = dx.shape[-1]
+        if dw is not None:
+            if x is None:
+                raise ValueError("dw needs x")
+            if dx is not None and dw.shape[-1] != d_in:
+                raise ValueError(f"dx and dw have {d_in} and {dw.shape[-1]} columns")
+            d_in = dw.shape[-1]
+        held = (0, 0)
+        if act != _lib.RDFFT_ACT_NONE:
+            if checkpoint is None:
+                raise ValueError(f"the gradient through {activation} needs the checkpoint of the pre-activation")
+            held = _held(checkpoint, device, tokens, d_out)
+        none = (0, 0)
+        keep, scratch, size = _scratch(
+            _need("linear_backward_workspace", d_in, d_out, tokens, dx is not None, dw is not None, db is not None, act, code),
+            workspace, device, "linear_backward")
+        a = _lib.pack["linear_backward"](
+            p, ld, *held,
+            *(none if dw is None else _rows(x, "x", dtype, device, (tokens, d_in))),
+            *(none if dx is None else _rows(w, "w", dtype, device, (d_out, d_in))),
+            *(none if dx is None or add is None else _rows(add, "add", dtype, device, (tokens, d_in))),
+            *(none if dx is None else _rows(dx, "dx", dtype, device, (tokens, d_in))),
+            *(none if dw is None else _rows(dw, "dw", dtype, device, (d_out, d_in))),
+            0 if db is None else _vector(db, "db", dtype, device, d_out), scratch, size)
+        status = _lib.load().linear_backward(a, d_in, d_out, tokens, act, code, stream)
     if status:
         _check(status, "linear_backward")
     return dx, dw, db

@@ -1,4 +1,5 @@
-"""Builds ``librdfft.so`` (the HIP kernels and the C ABI) in-tree for gfx950.
+"""Builds ``librdfft.so`` (the HIP kernels and the C ABI) in-tree for gfx950, and ``_binding.so``, the Python module
+that hands torch tensors to it.
 
 Run ``python -m paper_2511_01385_amd.build`` or call :func:`build`.  Objects go to
 ``paper_2511_01385_amd/_build/``; the shared library lands next to this file.
@@ -10,6 +11,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -20,6 +22,8 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "librdfft.so")
 
 SOURCES = ["bca_block_bf16.hip", "bca_block_f16.hip", "bca_block_f32.hip", "bca_store_bf16.hip", "bca_store_f16.hip", "bca_store_f32.hip", "rdfft_kernels.hip", "rdfft_hc_kernels.hip", "bca_kernels.hip", "bca_multipass.hip", "layout_kernels.hip", "mixed_kernels.hip", "act8_kernels.hip", "norm_kernels.hip", "linear_bf16.hip", "linear_f16.hip", "linear_f32.hip", "linear.hip", "capi.cpp", "capi_dense.cpp", "twiddles.cpp"]
+
+BINDING = os.path.join(PKG, "_binding.so")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
@@ -55,6 +59,24 @@ def _compile(src: str) -> str:
     return obj
 
 
+def _build_binding() -> None:
+    """Compiles csrc/binding.cpp against torch's headers and the built library, which it finds next to itself."""
+    import torch
+
+    root = os.path.dirname(torch.__file__)
+    cmd = [
+        os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+        f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+        f"-I{INCLUDE}", f"-I{root}/include", f"-I{root}/include/torch/csrc/api/include",
+        f"-I{sysconfig.get_paths()['include']}", os.path.join(CSRC, "binding.cpp"), "-o", BINDING + ".tmp",
+        LIB, f"-L{root}/lib", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-Wl,-rpath,$ORIGIN",
+    ]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError(f"g++ failed on binding.cpp:\n{res.stderr}")
+    shutil.move(BINDING + ".tmp", BINDING)
+
+
 def build(verbose: bool = True) -> str:
     """Compile every source and link ``librdfft.so``; returns the library path."""
     if not os.path.exists(HIPCC):
@@ -64,11 +86,12 @@ def build(verbose: bool = True) -> str:
     with ThreadPoolExecutor(max_workers=jobs) as ex:
         objs = list(ex.map(_compile, SOURCES))
     tmp = LIB + ".tmp"
-    cmd = [HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *objs]
+    cmd = [HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-Wl,-soname,librdfft.so", "-o", tmp, *objs]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError(f"link failed:\n{res.stderr}")
     shutil.move(tmp, LIB)
+    _build_binding()
     if verbose:
         print(f"built {LIB}", file=sys.stderr)
     return LIB
