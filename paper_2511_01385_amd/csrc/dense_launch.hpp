@@ -94,10 +94,12 @@ struct GemmArgs {
 enum LinearTile { kTile32x64, kTile64, kTile128, kTile128x256, kTile256, kLinearTiles };
 enum LinearOperands { kForward, kGradX, kGradW, kLinearOperands };
 using LinearFn = hipError_t (*)(const GemmArgs&, hipStream_t);
+using LinearGradsFn = hipError_t (*)(const GemmArgs& dw, const GemmArgs& dx, hipStream_t);
 constexpr int64_t kFewTokens = 64;
 struct LinearTable {
   LinearFn fn[kLinearTiles][kLinearOperands][2];
-  LinearFn few[3][2][2];  // the forward of 16, 32, 64 tokens at most, 16 or 32 rows of W to a workgroup
+  LinearGradsFn grads[kLinearTiles];  // dW and dx in one launch, of whole chunks
+  LinearFn few[3][2][2];              // the forward of 16, 32, 64 tokens at most, 16 or 32 rows of W to a workgroup
 };
 LinearTable linear_table_f32();
 LinearTable linear_table_bf16();

@@ -3,6 +3,8 @@
 // product whose k is split and the gradient through the activation with its column sums.
 #include <hip/hip_runtime.h>
 
+#include <cmath>
+
 #include "linear_kernels.hpp"
 
 namespace rdfft {
@@ -160,6 +162,7 @@ constexpr TileCost kCost32[] = {{32, 64, 4, 0.285, 0.256, 3.6}, {64, 64, 3, 0.53
 struct Plan {
   LinearTile tile;
   int64_t splits, k_split;
+  double cost;
 };
 
 // The tile and the number of k ranges that cost least.  The join of s ranges costs a launch (4 us) and 8 s bytes a
@@ -167,8 +170,7 @@ struct Plan {
 static Plan plan_of(int64_t m, int64_t n, int64_t k, LinearOperands kind, int storage, bool direct) {
   const bool f32 = storage == kStorageF32;
   const int64_t bk = kStageBytes / (f32 ? 4 : 2), stages = std::max<int64_t>(1, (k + bk - 1) / bk);
-  Plan best{kTile64, 1, stages * bk};
-  double least = 0;
+  Plan best{kTile64, 1, stages * bk, 0};
   for (int t = 0; t < kLinearTiles; ++t) {
     // what is not built
     if (f32 ? t > kTile64 : !direct && (t == kTile32x64 || t == kTile256)) continue;
@@ -183,10 +185,7 @@ static Plan plan_of(int64_t m, int64_t n, int64_t k, LinearOperands kind, int st
       const double stage = per_cu == 1 ? c.alone : c.each * (double)per_cu;
       double cost = (double)each * stage + c.ends * (double)((per_cu + c.together - 1) / c.together);
       if (splits > 1) cost += 4.0 + 8.0 * (double)splits * (double)m * (double)n / 4e6;
-      if (least == 0 || cost < least) {
-        least = cost;
-        best = {(LinearTile)t, splits, each * bk};
-      }
+      if (best.cost == 0 || cost < best.cost) best = {(LinearTile)t, splits, each * bk, cost};
     }
   }
   return best;
@@ -227,13 +226,20 @@ static bool whole_chunks(const void* p, int64_t ld, int64_t len, int storage) {
   return (reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * 2) | (uintptr_t)(len * 2)) % 16 == 0;
 }
 
+static const LinearTable& table_of(int storage) {
+  static const LinearTable tables[] = {linear_table_f32(), linear_table_bf16(), linear_table_f16()};
+  return tables[storage];
+}
+
 // a_len: values in a memory row of A that may be loaded (those past its end are zeros)
+static bool whole_operands(const GemmArgs& g, int64_t a_len, LinearOperands kind, int storage) {
+  return whole_chunks(g.a, g.lda, a_len, storage) && whole_chunks(g.b, g.ldb, kind == kForward ? g.k : g.n, storage);
+}
+
 static hipError_t product(GemmArgs& g, int64_t a_len, LinearOperands kind, int storage, void* workspace,
                           hipStream_t stream) {
-  static const LinearTable tables[] = {linear_table_f32(), linear_table_bf16(), linear_table_f16()};
-  const LinearTable& t = tables[storage];
-  const bool direct = whole_chunks(g.a, g.lda, a_len, storage) &&
-                      whole_chunks(g.b, g.ldb, kind == kForward ? g.k : g.n, storage);
+  const LinearTable& t = table_of(storage);
+  const bool direct = whole_operands(g, a_len, kind, storage);
   g.splits = 1;
   if (kind == kForward && g.m <= kFewTokens) {
     // 32 rows of W to a workgroup where that still fills the chip (x is read half as often: 64 tokens of 8192 x 8192
@@ -248,6 +254,43 @@ static hipError_t product(GemmArgs& g, int64_t a_len, LinearOperands kind, int s
   const hipError_t e = t.fn[p.tile][kind][direct](g, stream);
   if (e != hipSuccess || g.partial == nullptr) return e;
   return with_elem(storage, [&](auto elem) { return join<decltype(elem)>(g, stream); });
+}
+
+// Which tile dW and dx share in one launch, or kLinearTiles where two launches cost less.  The product with the longer k
+// goes first.  Where it has a workgroup for every CU the rounds are simply full; where it has fewer, its CUs deal
+// part of their time to the other's tiles until those run out, and finish alone.  This tells the time to
+// about 8 % (dx and dW of 512 to 16384 tokens of 128 to 5120, bf16 and float32), so it has to be that much less.
+// One launch and two, us (tokens x d_in x d_out): 1021 x 1024 x 768 float32 42 and 49; bf16 512 x 768 x 768 12.6 and 16.6, 2045 x
+// 2048 x 2048 42 and 57, 4096 x 768 x 2560 53 and 70.  Two stay: bf16 4096 x 768 x 768 (54 and 51), 2048 x 4096 x 4096 (136 and 128), 8192 x 768 x 768
+// (65 and 46, its dW's k split).
+static LinearTile together_of(const GemmArgs& dw, const GemmArgs& dx, int storage) {
+  const bool f32 = storage == kStorageF32;
+  const int64_t bk = kStageBytes / (f32 ? 4 : 2);
+  LinearTile best = kLinearTiles;
+  double least = 0.92 * (plan_of(dw.m, dw.n, dw.k, kGradW, storage, true).cost +
+                         plan_of(dx.m, dx.n, dx.k, kGradX, storage, true).cost);
+  const GemmArgs& first = dw.k >= dx.k ? dw : dx;
+  const GemmArgs& second = dw.k >= dx.k ? dx : dw;
+  const double cus = (double)kCUs, k1 = (double)((first.k + bk - 1) / bk), k2 = (double)((second.k + bk - 1) / bk);
+  for (const LinearTile t : {kTile64, kTile128}) {
+    if (table_of(storage).grads[t] == nullptr) continue;
+    const TileCost& c = f32 ? kCost32[t] : kCost16[t];
+    const auto tiles = [&](const GemmArgs& g) { return (double)((g.m + c.bm - 1) / c.bm * ((g.n + c.bn - 1) / c.bn)); };
+    const double n1 = tiles(first), n2 = tiles(second), per_cu = std::ceil((n1 + n2) / cus);
+    const double full = (n1 * k1 + n2 * k2) / cus * c.each;
+    double cost = std::max(full, k1 * c.alone);
+    if (n1 < cus && per_cu > 1) {
+      const double share = 1 / std::min((double)c.together, per_cu);  // of such a CU that the longer k has
+      const double until = n2 * k2 / cus * c.each / (1 - n1 / cus * share);
+      cost = std::max(full, until + std::max(0.0, k1 - until * share / c.each) * c.alone);
+    }
+    cost += c.ends * std::ceil(per_cu / c.together);
+    if (cost < least) {
+      least = cost;
+      best = t;
+    }
+  }
+  return best;
 }
 
 hipError_t launch_linear_forward(const LinearForward& a, hipStream_t stream) {
@@ -299,35 +342,39 @@ hipError_t launch_linear_backward(const LinearBackward& a, hipStream_t stream) {
       ldz = dz_len = slope_pitch(n);
     }
   }
-  if (a.dx != nullptr && T > 0) {
-    GemmArgs g{};
-    g.a = dz;
-    g.lda = ldz;
-    g.b = a.w;
-    g.ldb = a.ldw;
-    g.m = T;
-    g.n = a.s.d_in;
-    g.k = n;
-    g.d = a.dx;
-    g.ldd = a.ldd;
-    g.residual = a.add;
-    g.ldr = a.lda;
-    e = product(g, dz_len, kGradX, storage, parts, stream);
-    if (e != hipSuccess) return e;
+  GemmArgs x{}, w{};
+  const bool dx = a.dx != nullptr && T > 0, dw = a.dw != nullptr;
+  x.a = dz;
+  x.lda = ldz;
+  x.b = a.w;
+  x.ldb = a.ldw;
+  x.m = T;
+  x.n = a.s.d_in;
+  x.k = n;
+  x.d = a.dx;
+  x.ldd = a.ldd;
+  x.residual = a.add;
+  x.ldr = a.lda;
+  w.a = dz;
+  w.lda = ldz;
+  w.b = a.x;
+  w.ldb = a.ldx;
+  w.m = n;
+  w.n = a.s.d_in;
+  w.k = T;
+  w.d = a.dw;
+  w.ldd = a.lddw;
+  if (dx && dw && whole_operands(x, dz_len, kGradX, storage) && whole_operands(w, dz_len, kGradW, storage)) {
+    const LinearTile t = together_of(w, x, storage);
+    if (t != kLinearTiles) {
+      x.splits = w.splits = 1;
+      x.k_split = x.k;
+      w.k_split = w.k;
+      return table_of(storage).grads[t](w, x, stream);
+    }
   }
-  if (a.dw != nullptr) {
-    GemmArgs g{};
-    g.a = dz;
-    g.lda = ldz;
-    g.b = a.x;
-    g.ldb = a.ldx;
-    g.m = n;
-    g.n = a.s.d_in;
-    g.k = T;
-    g.d = a.dw;
-    g.ldd = a.lddw;
-    e = product(g, dz_len, kGradW, storage, parts, stream);
-  }
+  if (dx) e = product(x, dz_len, kGradX, storage, parts, stream);
+  if (e == hipSuccess && dw) e = product(w, dz_len, kGradW, storage, parts, stream);
   return e;
 }
 

@@ -520,8 +520,7 @@ __device__ __forceinline__ TileAt tile_of(int id, int tiles_m, int tiles_n, int 
 }
 
 template <class E, int BM, int BN, int WM, int WN, int STAGES, bool AX, bool BX, LoadPath PATH>
-__global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2)))  // 256 registers, no second file
-    linear_kernel(GemmArgs g) {
+__device__ __forceinline__ void linear_tile(GemmArgs g, int id) {
   using T = typename E::T;
   constexpr int WAVES = WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
   constexpr int BK = kStageBytes / (int)sizeof(T);
@@ -533,7 +532,7 @@ __global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_
   extern __shared__ __attribute__((aligned(1024))) char linear_lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
   const int wm = wave / WN, wn = wave % WN;
-  const TileAt at = tile_of((int)blockIdx.x, g.tiles_m, g.tiles_n, g.splits);
+  const TileAt at = tile_of(id, g.tiles_m, g.tiles_n, g.splits);
   const int64_t m0 = (int64_t)at.tm * BM, n0 = (int64_t)at.tn * BN;
   const int64_t k0 = (int64_t)at.split * g.k_split, k1 = min(k0 + g.k_split, g.k);
 
@@ -757,6 +756,12 @@ __global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_
 }
 
 template <class E, int BM, int BN, int WM, int WN, int STAGES, bool AX, bool BX, LoadPath PATH>
+__global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2)))  // 256 registers, no second file
+    linear_kernel(GemmArgs g) {
+  linear_tile<E, BM, BN, WM, WN, STAGES, AX, BX, PATH>(g, (int)blockIdx.x);
+}
+
+template <class E, int BM, int BN, int WM, int WN, int STAGES, bool AX, bool BX, LoadPath PATH>
 hipError_t linear_launch(const GemmArgs& g, hipStream_t stream) {
   constexpr int lds = STAGES * (BM + BN) * kStageBytes;
   const auto kernel = linear_kernel<E, BM, BN, WM, WN, STAGES, AX, BX, PATH>;
@@ -767,6 +772,35 @@ hipError_t linear_launch(const GemmArgs& g, hipStream_t stream) {
   t.tiles_m = (int)((g.m + BM - 1) / BM);
   t.tiles_n = (int)((g.n + BN - 1) / BN);
   hipLaunchKernelGGL(kernel, dim3((unsigned)(t.tiles_m * t.tiles_n * t.splits)), dim3(WM * WN * 64), lds, stream, t);
+  return hipGetLastError();
+}
+
+// dW and dx in one launch, neither with its k split: the first workgroups take the tiles of the one with the longer k.
+// Where each alone leaves CUs idle they fill each other's rounds.
+template <class E, int BM, int BN, int WM, int WN, int STAGES, LoadPath PATH>
+__global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2)))
+    linear_grads_kernel(GemmArgs dw, GemmArgs dx) {
+  const bool dw_first = dw.k >= dx.k;
+  const int id = (int)blockIdx.x, first = dw_first ? dw.tiles_m * dw.tiles_n : dx.tiles_m * dx.tiles_n;
+  const int at = id < first ? id : id - first;
+  if ((id < first) == dw_first) linear_tile<E, BM, BN, WM, WN, STAGES, true, true, PATH>(dw, at);
+  else linear_tile<E, BM, BN, WM, WN, STAGES, false, true, PATH>(dx, at);
+}
+
+template <class E, int BM, int BN, int WM, int WN, int STAGES, LoadPath PATH>
+hipError_t grads_launch(const GemmArgs& dw, const GemmArgs& dx, hipStream_t stream) {
+  constexpr int lds = STAGES * (BM + BN) * kStageBytes;
+  const auto kernel = linear_grads_kernel<E, BM, BN, WM, WN, STAGES, PATH>;
+  static const hipError_t ready = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                                      hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (ready != hipSuccess) return ready;
+  GemmArgs t[2] = {dw, dx};
+  for (GemmArgs& g : t) {
+    g.tiles_m = (int)((g.m + BM - 1) / BM);
+    g.tiles_n = (int)((g.n + BN - 1) / BN);
+  }
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(t[0].tiles_m * t[0].tiles_n + t[1].tiles_m * t[1].tiles_n)),
+                     dim3(WM * WN * 64), lds, stream, t[0], t[1]);
   return hipGetLastError();
 }
 
@@ -951,6 +985,8 @@ LinearTable make_linear_table() {
   operands(std::false_type{}, std::false_type{}, kForward);
   operands(std::false_type{}, std::true_type{}, kGradX);
   operands(std::true_type{}, std::true_type{}, kGradW);
+  t.grads[kTile64] = grads_launch<E, 64, 64, 2, 2, 3, W>;
+  if constexpr (!F32) t.grads[kTile128] = grads_launch<E, 128, 128, 2, 4, 2, W>;
   t.few[0][0][1] = few_launch<E, 1, 1, 8, 4, W>;
   t.few[0][1][1] = few_launch<E, 1, 2, 4, 6, W>;
   t.few[1][0][1] = few_launch<E, 2, 1, 4, 6, W>;
