@@ -235,6 +235,8 @@ RDFFT_API int bca_backward_batched(int count, const void *const *x, const void *
  * rint(x / 2^e) (half to even) and stands for code * 2^e; the block's scale is the byte e + 127.
  * A block with an infinity or a NaN has scale byte 255, codes 0, and stands for NaN throughout.
  * The error of a value is at most 2^(e-1), 1/126 of the block's largest |x| (down to 2^-121).
+ * Where |x| is within 1 % of the largest number M of its type, code * 2^e can be the power of two past M: +-64 * 2^10
+ * made into float16, +-64 * 2^122 into any other type.  It stands for +-M, so finite values come back finite.
  */
 typedef struct {
   int8_t *codes;
@@ -242,7 +244,7 @@ typedef struct {
 } act8_t;
 
 /* act8_quantize / act8_dequantize -- rows x n values into their checkpoint, and back (the values
- * that it stands for, rounded to dtype).  n >= 1; rows == 0 is a no-op. */
+ * that it stands for, rounded to dtype: a checkpoint of larger numbers than float16 has becomes infinities there).  n >= 1; rows == 0 is a no-op. */
 RDFFT_API int act8_quantize(const void *x, int64_t ldx, const act8_t *to, int64_t rows, int64_t n, rdfft_dtype_t dtype,
                             rdfft_stream_t stream);
 RDFFT_API int act8_dequantize(const act8_t *from, void *out, int64_t ldo, int64_t rows, int64_t n, rdfft_dtype_t dtype,

@@ -51,7 +51,7 @@ __global__ void __launch_bounds__(kActWG) act8_dequantize_kernel(const int8_t* _
   for (int64_t i = ((int64_t)blockIdx.x * lanes + lane) * kVec; i < n; i += step) {
     const Bytes8 c = i + kVec <= n ? *reinterpret_cast<const Bytes8*>(codes + i) : tail_codes(codes, i, n);
     float v[kVec];
-    ck_decode(c, ck_scale(scales[i / kCkBlock]), v);
+    ck_decode<E>(c, ck_scale(scales[i / kCkBlock]), v);
     write_group<E>(out, i, n, v);
   }
 }

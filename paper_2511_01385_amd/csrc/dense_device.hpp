@@ -6,6 +6,8 @@
 // rint(x / 2^e) in int8, the block's scale as the byte e + 127.  Scaling by a power of two is exact, so
 // the code of a value depends on nothing but the value and its block, and code * 2^e fits in
 // bfloat16.  A block with an infinity or a NaN has scale byte 255 and stands for NaN throughout.
+// Code 64 of a block whose largest |x| is within 1 % of the type's largest number would stand for the power of two past
+// that number: it stands for the number itself (ck_decode), so what was finite comes back finite.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -33,6 +35,8 @@ struct __attribute__((packed, aligned(1))) Bytes8 {
 struct ElemF32 {
   using T = float;
   static constexpr int kId = 0;
+  // the largest finite number, the step of a block that reaches it, and 64 such steps, as floats
+  static constexpr float kMost = 0x1.fffffep127f, kLastStep = 0x1p122f, kPast = __builtin_inff();
   struct Raw {
     Bytes16 a, b;
   };
@@ -64,6 +68,9 @@ template <int ID, float2 (*WIDEN)(uint32_t), uint32_t (*NARROW)(float2)>
 struct Elem16 {
   using T = uint16_t;
   static constexpr int kId = ID;
+  static constexpr bool kHalf = ID == 2;
+  static constexpr float kMost = kHalf ? 65504.f : 0x1.fep127f, kLastStep = kHalf ? 0x1p10f : 0x1p122f,
+                         kPast = kHalf ? 65536.f : __builtin_inff();
   using Raw = Bytes16;
   __device__ __forceinline__ static Raw load(const T* p) { return *reinterpret_cast<const Bytes16*>(p); }
   __device__ __forceinline__ static void widen(const Raw& r, float* v) {
@@ -203,9 +210,15 @@ __device__ __forceinline__ Bytes8 ck_encode(const float* v, int s) {
     r.w[h] = (c[4 * h] & 0xff) | (c[4 * h + 1] & 0xff) << 8 | (c[4 * h + 2] & 0xff) << 16 | c[4 * h + 3] << 24;
   return r;
 }
+// Eight values, of a checkpoint of E's numbers (float32 for what a kernel computed).
+template <class E>
 __device__ __forceinline__ void ck_decode(const Bytes8& r, float scale, float* v) {
 #pragma unroll
   for (int i = 0; i < kVec; ++i) v[i] = (float)(int8_t)(r.w[i / 4] >> (8 * (i % 4))) * scale;
+  if (scale == E::kLastStep) {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) v[i] = fabsf(v[i]) == E::kPast ? copysignf(E::kMost, v[i]) : v[i];
+  }
 }
 
 // Eight codes of a row, zeros past its end (the load clamped as load_group's).

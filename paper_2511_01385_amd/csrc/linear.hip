@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(kSlopeWG)
     const auto row = [&](int r, float* g, const Bytes8& code, int byte) {
       if (act != kActNone) {
         float z[kVec];
-        ck_decode(code, ck_scale(byte), z);
+        ck_decode<ElemF32>(code, ck_scale(byte), z);
         times_slope8(act, z, g);
         E::store(dz + r * ldz + i, g);  // (rows are padded to whole groups, with zeros)
       }

@@ -216,10 +216,10 @@ struct NormRow {
     for (int c = 0; c < C; ++c) {
       dy[c].widen(static_cast<const T*>(a.dy) + row * a.ldg, at[c], n, g[c]);
       if constexpr (CK && EXACT) {
-        ck_decode(codes[c], ck_scale(scale[c]), u[c]);
+        ck_decode<ElemF32>(codes[c], ck_scale(scale[c]), u[c]);
       } else if constexpr (CK) {
         const int s = at[c] < n ? a.ck.scales[row * blocks + at[c] / kCkBlock] : 0;
-        ck_decode(tail_codes(a.ck.codes + row * n, at[c], n), ck_scale(s), u[c]);
+        ck_decode<ElemF32>(tail_codes(a.ck.codes + row * n, at[c], n), ck_scale(s), u[c]);
       } else {
         x[c].widen(static_cast<const T*>(a.x) + row * a.ldx, at[c], n, u[c]);
         if (a.residual != nullptr) {

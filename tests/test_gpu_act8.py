@@ -110,3 +110,33 @@ def test_no_rows_and_other_streams():
         y = torch.randn(64, 96, device="cuda")
         check(y)
     s.synchronize()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_finite_values_come_back_finite(dtype):
+    """Also those whose code times the step is the power of two past the type's largest number."""
+    most = torch.finfo(TYPES[dtype]).max
+    parts = torch.tensor([1.0, 0.998, 0.9955, 0.99, 0.5], dtype=torch.float64) * most
+    x = torch.zeros(10, 40, dtype=TYPES[dtype], device="cuda")
+    x[:, 3] = torch.cat([parts, -parts]).to(TYPES[dtype]).cuda()
+    x[:, 20] = x[:, 3] / 3
+    assert x.isfinite().all()
+    codes, scales = api.act8_quantize(x, *api.checkpoint_like(x))
+    out = api.act8_dequantize(codes, scales, torch.empty_like(x))
+    assert out.isfinite().all()
+    half = torch.exp2(scales.double() - 128).repeat_interleave(32, dim=1)[:, :40]
+    assert ((out.double() - x.double()).abs() <= half).all()
+    # numbers that float16 does not have are infinities there, not its largest number
+    wide = torch.tensor([[1e6, -66560.0, 65536.0 * 1.5, 1.0]], device="cuda")
+    back = api.act8_dequantize(*api.act8_quantize(wide, *api.checkpoint_like(wide)), torch.empty_like(wide, dtype=torch.float16))
+    assert back[0, :3].isinf().all()
+
+
+@pytest.mark.parametrize("name", ["relu", "gelu", "silu"])
+def test_slope_at_the_largest_numbers(name):
+    eye = torch.eye(32, device="cuda")
+    for value in (3.4e38, -3.4e38):
+        z = torch.full((1, 32), value, device="cuda")
+        held = api.act8_quantize(z, *api.checkpoint_like(z))
+        dx = api.linear_backward(torch.ones_like(z), None, eye, dx=torch.empty_like(z), activation=name, checkpoint=held)[0]
+        assert torch.equal(dx, torch.full_like(dx, float(value > 0)))
