@@ -320,7 +320,8 @@ typedef enum {
  *   y          [tokens][d_out]; may be residual itself (same pointer and stride).
  *   checkpoint of z (of its float32 value), written, for linear_backward; codes null: none.
  * Products of dtype's values are summed in float32 (matrix cores); y is rounded once.
- * d_in, d_out >= 1, at most 2^20, strides at most 2^21, tokens at most 2^22 (more -> RDFFT_EUNSUPPORTED).
+ * d_in, d_out >= 1, at most 2^20, strides at most 2^21 (a single row's is not looked at), tokens at most 2^22 (more
+ * -> RDFFT_EUNSUPPORTED).
  */
 typedef struct {
   const void *x;

@@ -42,7 +42,7 @@ bool overlap(const Rows& a, const Rows& b) {
 bool same(const Rows& a, const Rows& b) { return a.p == b.p && a.pitch == b.pitch; }
 
 // fills `out` from a tensor of elements of `item` bytes; false: null (unless it may be), misaligned, a
-// stride shorter than the row, or sizes beyond 63 bits
+// stride shorter than the row, or sizes beyond 63 bits.  The stride of a single row reaches nothing: it counts as the row.
 bool tensor(const void* p, int64_t rows, int64_t n, int64_t ld, int item, bool may_be_null, Rows* out) {
   if (p == nullptr || rows == 0) {
     *out = Rows{};
@@ -50,13 +50,16 @@ bool tensor(const void* p, int64_t rows, int64_t n, int64_t ld, int item, bool m
   }
   int64_t bytes = 0, all = 0;
   if (ld < n || reinterpret_cast<uintptr_t>(p) % (uintptr_t)item != 0) return false;
-  if (!mul_ok(ld, item, &bytes) || !mul_ok(rows, bytes, &all)) return false;
+  if (!mul_ok(rows == 1 ? n : ld, item, &bytes) || !mul_ok(rows, bytes, &all)) return false;
   *out = Rows{p, rows, n * item, bytes};
   return true;
 }
 bool contiguous(const void* p, int64_t count, int item, bool may_be_null, Rows* out) {
   return tensor(p, count > 0 ? 1 : 0, count, count, item, may_be_null, out);
 }
+
+// a tensor's row stride in elements of `item` bytes
+int64_t stride(const Rows& r, int item) { return r.pitch / item; }
 
 int64_t ck_blocks(int64_t n) { return (n + 31) / 32; }
 bool checkpoint(const act8_t& c, int64_t rows, int64_t n, bool may_be_null, Rows* codes, Rows* scales) {
@@ -227,13 +230,13 @@ int linear_forward(const linear_forward_t* a, int64_t d_in, int64_t d_out, int64
       !tensor(a->y, tokens, d_out, a->ldy, s, false, &y) || !checkpoint(a->checkpoint, tokens, d_out, true, &codes, &scales) ||
       !workspace(a->workspace, a->workspace_bytes, linear_forward_workspace(d_in, d_out, tokens, dtype), &ws))
     return RDFFT_EINVAL;
-  if (a->ldx > kMaxStride || a->ldw > kMaxStride) return RDFFT_EUNSUPPORTED;
+  if (stride(x, s) > kMaxStride || stride(w, s) > kMaxStride) return RDFFT_EUNSUPPORTED;
   if ((overlap(y, r) && !same(y, r)) || !apart({y, codes, scales, ws}, {x, w, b}) || !apart({codes, scales, ws}, {r}))
     return RDFFT_EINVAL;
   st = device(nullptr);
   if (st != RDFFT_OK) return st;
-  const rdfft::LinearForward k{{d_in, d_out, tokens, act, dtype}, a->x, a->ldx, a->w, a->ldw, a->bias, a->residual,
-                               a->ldr, a->y, a->ldy, {a->checkpoint.codes, a->checkpoint.scales}, a->workspace};
+  const rdfft::LinearForward k{{d_in, d_out, tokens, act, dtype}, a->x, stride(x, s), a->w, stride(w, s), a->bias,
+                               a->residual, a->ldr, a->y, a->ldy, {a->checkpoint.codes, a->checkpoint.scales}, a->workspace};
   return status(rdfft::launch_linear_forward(k, reinterpret_cast<hipStream_t>(stream)));
 }
 
@@ -265,16 +268,15 @@ int linear_backward(const linear_backward_t* a, int64_t d_in, int64_t d_out, int
   if (!workspace(a->workspace, a->workspace_bytes,
                  linear_backward_workspace(d_in, d_out, tokens, wants_dx, wants_dw, wants_db, act, dtype), &ws))
     return RDFFT_EINVAL;
-  if (a->ldg > kMaxStride || (wants_dw && a->ldx > kMaxStride) || (wants_dx && a->ldw > kMaxStride))
-    return RDFFT_EUNSUPPORTED;
+  if (stride(dy, s) > kMaxStride || stride(x, s) > kMaxStride || stride(w, s) > kMaxStride) return RDFFT_EUNSUPPORTED;
   if ((overlap(dx, add) && !same(dx, add)) || !apart({dx, dw, db, ws}, {dy, codes, scales, x, w}) ||
       !apart({dw, db, ws}, {add}))
     return RDFFT_EINVAL;
   st = device(nullptr);
   if (st != RDFFT_OK) return st;
-  const rdfft::LinearBackward k{{d_in, d_out, tokens, act, dtype}, a->dy, a->ldg,
-                                {a->checkpoint.codes, a->checkpoint.scales}, a->x, a->ldx, a->w, a->ldw, a->add, a->lda,
-                                a->dx, a->ldd, a->dw, a->lddw, a->db, a->workspace};
+  const rdfft::LinearBackward k{{d_in, d_out, tokens, act, dtype}, a->dy, stride(dy, s),
+                                {a->checkpoint.codes, a->checkpoint.scales}, a->x, stride(x, s), a->w, stride(w, s), a->add,
+                                a->lda, a->dx, a->ldd, a->dw, a->lddw, a->db, a->workspace};
   return status(rdfft::launch_linear_backward(k, reinterpret_cast<hipStream_t>(stream)));
 }
 

@@ -212,3 +212,15 @@ def test_feed_forward_arguments(args, kw, err):
         net(torch.zeros(3, 255))
     with pytest.raises(TypeError):
         net(torch.zeros(3, 256))
+
+
+def test_the_stride_of_one_row_is_not_looked_at(lib):
+    # (each call is refused for what lies behind the check of strides: an output over an input)
+    far = 1 << 24
+    assert call(lib, "linear_forward", {**LINEAR, "ldx": far, "y": P[0]}, 64, 96, 2, 0, BF16, None) == EUNSUP
+    assert call(lib, "linear_forward", {**LINEAR, "ldx": far, "y": P[0]}, 64, 96, 1, 0, BF16, None) == EINVAL
+    assert call(lib, "linear_forward", {**LINEAR, "ldw": far, "y": P[1]}, 64, 1, 1, 0, BF16, None) == EINVAL
+    for change in (dict(ldg=far, dx=P[0]), dict(ldx=far, dx=P[3])):
+        assert call(lib, "linear_backward", {**BACK, **change}, 64, 96, 1, 2, BF16, None) == EINVAL
+    # ... but a stride shorter than the row is
+    assert call(lib, "linear_forward", {**LINEAR, "ldx": 63}, 64, 96, 1, 0, BF16, None) == EINVAL

@@ -304,3 +304,23 @@ def test_replayed_from_a_graph():
         step()
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(got, (y, dx, dw, db))), k
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_one_row_of_a_long_stride(dtype):
+    """The last token of a sequence: one row, whose stride (the sequence) reaches nothing."""
+    x, w, b, r, dy, a = tensors(1, 512, 96, dtype, 3)
+
+    def last(t):
+        rows = torch.zeros(1, 5000, t.shape[1], dtype=t.dtype, device="cuda")
+        rows[:, -1, :] = t
+        return rows[:, -1, :]
+
+    assert last(x).stride(0) > 1 << 21
+    want = api.linear_forward(x, w, torch.empty_like(r), bias=b, residual=r)
+    assert torch.equal(api.linear_forward(last(x), w, last(r), bias=b, residual=last(r)), want)
+    y = last(r)
+    assert torch.equal(api.linear_forward(x, w, y, bias=b, residual=y.as_strided((1, 96), (96, 1))), want)
+    dx, dw = api.linear_backward(dy, x, w, dx=torch.empty_like(x), dw=torch.empty_like(w), add=a)[:2]
+    got = api.linear_backward(last(dy), last(x), w, dx=last(a), dw=torch.empty_like(w), add=last(a))
+    assert torch.equal(got[0], dx) and torch.equal(got[1], dw)
