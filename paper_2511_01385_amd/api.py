@@ -300,6 +300,8 @@ def _first(t: torch.Tensor, name: str):
 def _held(checkpoint, device: int, rows: int, n: int) -> tuple[int, int]:
     """Pointers of a (codes, scales) pair for (rows, n) values."""
     codes, scales = checkpoint
+    if codes is None or scales is None:
+        raise ValueError("a checkpoint is the pair (codes, scales), and one of them is None")
     blocks = -(-n // CHECKPOINT_BLOCK)
     if (codes.dtype is torch.int8 and scales.dtype is torch.uint8 and codes.shape == (rows, n)
             and scales.shape == (rows, blocks) and codes.get_device() == device and scales.get_device() == device
@@ -392,7 +394,7 @@ def layer_norm_forward(x, weight, bias, y, *, residual=None, mean=None, rstd=Non
     status = None
     if x.is_cuda:
         device = _current_device()
-        codes, scales = checkpoint or _NONE
+        codes, scales = _NONE if checkpoint is None else checkpoint
         status = _lib.binding().layer_norm_forward(x, residual, weight, bias, y, mean, rstd, codes, scales, eps, device,
                                                    _raw_stream(device))
     if status is None:
@@ -470,7 +472,7 @@ def linear_forward(x, w, y, *, bias=None, activation="none", residual=None, chec
     act = ACTIVATIONS.get(activation)
     if x.is_cuda and act is not None:
         device = _current_device()
-        codes, scales = checkpoint or _NONE
+        codes, scales = _NONE if checkpoint is None else checkpoint
         status = _lib.binding().linear_forward(x, w, bias, residual, y, codes, scales, act, workspace, device,
                                                _raw_stream(device))
     if status is None:
@@ -509,7 +511,7 @@ def linear_backward(dy, x, w, *, dx=None, dw=None, db=None, activation="none", c
     act = ACTIVATIONS.get(activation)
     if dy.is_cuda and act is not None:
         device = _current_device()
-        codes, scales = checkpoint or _NONE
+        codes, scales = _NONE if checkpoint is None else checkpoint
         status = _lib.binding().linear_backward(dy, x, w, dx, dw, db, add, codes, scales, act, workspace, device,
                                                 _raw_stream(device))
     if status is None:

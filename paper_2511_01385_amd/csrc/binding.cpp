@@ -88,7 +88,10 @@ struct Call {
   float* floats(Py_ssize_t i, int64_t n) const { return static_cast<float*>(vector(i, at::kFloat, n)); }
   // codes at i and scales at i + 1
   act8_t held(Py_ssize_t i, int64_t r, int64_t n) const {
-    if (!has(i)) return {nullptr, nullptr};
+    if (!has(i)) {
+      if (has(i + 1)) throw NotPlain{};  // half a checkpoint
+      return {nullptr, nullptr};
+    }
     const at::Tensor &c = tensor(i, at::kChar), &s = tensor(i + 1, at::kByte);
     if (c.dim() != 2 || c.size(0) != r || c.size(1) != n || !c.is_contiguous()) throw NotPlain{};
     if (s.dim() != 2 || s.size(0) != r || s.size(1) != (n + 31) / 32 || !s.is_contiguous()) throw NotPlain{};

@@ -100,3 +100,16 @@ def test_statuses_reach_the_caller():
     x, y = buffer[:256].view(4, 64), buffer[32:].view(4, 64)
     with pytest.raises(api.RdfftError):
         api.layer_norm_forward(x, torch.ones(64, device="cuda"), None, y)
+
+
+def test_half_a_checkpoint_is_refused():
+    x, w, one = made(4, 64, torch.bfloat16, 1), made(64, 64, torch.bfloat16, 2), torch.ones(64, device="cuda")
+    mean = torch.zeros(4, device="cuda")
+    codes, scales = api.checkpoint_like(x)
+    for half in ((None, scales), (codes, None), ()):
+        for call in (lambda: api.layer_norm_forward(x, one, None, torch.empty_like(x), checkpoint=half),
+                     lambda: api.linear_forward(x, w, torch.empty_like(x), checkpoint=half),
+                     lambda: api.linear_backward(x, None, w, dx=torch.empty_like(x), activation="gelu", checkpoint=half),
+                     lambda: api.layer_norm_backward(x, half, one, mean, mean, torch.empty_like(x), one.clone(), one.clone())):
+            with pytest.raises(ValueError):
+                call()
