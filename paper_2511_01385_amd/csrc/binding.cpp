@@ -126,10 +126,7 @@ PyObject* guarded(F&& fn) {
     status = fn();
   } catch (const NotPlain&) {
     Py_RETURN_NONE;
-  } catch (const c10::OutOfMemoryError& e) {
-    PyErr_SetString(PyExc_MemoryError, e.what_without_backtrace());
-    return nullptr;
-  } catch (const std::exception&) {  // a tensor without storage and the like
+  } catch (const std::exception&) {  // a tensor without storage, no memory for the workspace: the long way raises its own
     Py_RETURN_NONE;
   }
   return PyLong_FromLong(status);

@@ -113,3 +113,33 @@ def test_half_a_checkpoint_is_refused():
                      lambda: api.layer_norm_backward(x, half, one, mean, mean, torch.empty_like(x), one.clone(), one.clone())):
             with pytest.raises(ValueError):
                 call()
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_no_memory_for_the_workspace(native, monkeypatch):
+    """Both ways raise torch's own error, and the next call with room is fine."""
+    class HandsBack:
+        def __getattr__(self, name):
+            return lambda *args: None
+
+    if not native:
+        monkeypatch.setattr(_lib, "_binding", HandsBack())
+    tokens, d_out = 8192, 16384
+    dy = torch.ones((tokens, d_out), dtype=torch.bfloat16, device="cuda")
+    held = api.act8_quantize(dy, *api.checkpoint_like(dy))
+    db = torch.empty(d_out, dtype=torch.bfloat16, device="cuda")
+
+    def call():
+        return api.linear_backward(dy, None, None, db=db, activation="relu", checkpoint=held)
+
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    total = torch.cuda.get_device_properties(0).total_memory
+    torch.cuda.set_per_process_memory_fraction((torch.cuda.memory_reserved() + (8 << 20)) / total)
+    try:
+        with pytest.raises(torch.OutOfMemoryError):
+            call()
+    finally:
+        torch.cuda.set_per_process_memory_fraction(1.0)
+    call()
+    assert (db == tokens).all()
