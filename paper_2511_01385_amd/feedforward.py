@@ -17,6 +17,7 @@ from __future__ import annotations
 import math
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import api
 
@@ -48,6 +49,7 @@ class _FeedForward(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable  # (the library's calls are not recorded: second derivatives are refused, not left out)
     def backward(ctx, dy):
         w1, w2, spectra, weight, mean, rstd, u_codes, u_scales, h_codes, h_scales, *z8 = ctx.saved_tensors
         dy = dy.contiguous()

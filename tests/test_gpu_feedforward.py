@@ -127,3 +127,14 @@ def test_adapter_with_8_bit_activations(dtype, d_in, d_out, p):
     assert torch.equal(y8, y)
     assert torch.equal(dx8, dx)  # (dx does not depend on x)
     assert rel(dc8, dc.double()) < 2e-2
+
+
+def test_second_derivatives_are_refused():
+    net = AdaptedFeedForward(256, 512, 64)
+    x = torch.randn(10, 256, device="cuda").bfloat16().requires_grad_(True)
+    y = net(x)
+    plain = torch.autograd.grad(y.float().square().sum(), x, retain_graph=True)[0]
+    dx = torch.autograd.grad(y.float().square().sum(), x, create_graph=True)[0]
+    assert torch.equal(dx, plain)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        (y.float().sum() + dx.float().square().sum()).backward()
