@@ -9,7 +9,8 @@ the second one's residual (written over it), the sum with x inside the norm.
 
 Memory: between forward and backward a token keeps the pre-activation and h (d_ff values each) and the norm's
 input (d_model values), all as 8-bit checkpoints: 33/32 bytes a value, instead of x, the pre-activation, h and the
-norm's input in the storage type.  Gradients are taken at the checkpointed values.
+norm's input in the storage type.  Gradients are taken at the checkpointed values.  Where no gradient can be asked for
+(``torch.no_grad()``, or nothing that requires one) no checkpoint is made.
 """
 
 from __future__ import annotations
@@ -24,11 +25,12 @@ from . import api
 
 class _FeedForward(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w1, b1, w2, b2, c, weight, bias, activation, eps):
+    def forward(ctx, x, w1, b1, w2, b2, c, weight, bias, activation, eps, keep):
+        # keep: whether there may be a backward, whose checkpoints are made only then
         tokens, d_model = x.shape
         d_ff = w1.shape[0]
         h = torch.empty((tokens, d_ff), dtype=x.dtype, device=x.device)
-        z8 = None if activation == "none" else api.checkpoint_like(h)
+        z8 = api.checkpoint_like(h) if keep and activation != "none" else None
         api.linear_forward(x, w1, h, bias=b1, activation=activation, checkpoint=z8)
         q, kb, p = c.shape
         spectra = c.detach().to(x.dtype).contiguous()
@@ -38,9 +40,11 @@ class _FeedForward(torch.autograd.Function):
         o = torch.empty_like(x)
         api.bca_forward(h, spectra, o)
         api.linear_forward(h, w2, o, bias=b2, residual=o)
+        y = torch.empty_like(x)
+        if not keep:
+            return api.layer_norm_forward(o, weight.detach(), bias.detach(), y, residual=x, eps=eps)
         mean, rstd = (torch.empty(tokens, dtype=torch.float32, device=x.device) for _ in range(2))
         u8 = api.checkpoint_like(x)
-        y = torch.empty_like(x)
         api.layer_norm_forward(o, weight.detach(), bias.detach(), y, residual=x, mean=mean, rstd=rstd, checkpoint=u8,
                                eps=eps)
         h8 = api.act8_quantize(h, *api.checkpoint_like(h))
@@ -67,7 +71,7 @@ class _FeedForward(torch.autograd.Function):
             # x also reached the norm directly
             dx = torch.empty_like(du)
             api.linear_backward(dh, None, w1, dx=dx, activation=ctx.activation, checkpoint=tuple(z8) or None, add=du)
-        return dx, None, None, None, None, dc, dweight, dbias, None, None
+        return dx, None, None, None, None, dc, dweight, dbias, None, None, None
 
 
 class AdaptedFeedForward(torch.nn.Module):
@@ -109,8 +113,10 @@ class AdaptedFeedForward(torch.nn.Module):
         if x.dtype != self.dtype:
             raise TypeError(f"input is {x.dtype}, the layer stores {self.dtype}")
         x2d = x.reshape(-1, self.d_model).contiguous()
+        trained = (x2d, self.c, self.weight, self.bias)
+        keep = torch.is_grad_enabled() and any(t.requires_grad for t in trained)
         y = _FeedForward.apply(x2d, self.w1, self.b1, self.w2, self.b2, self.c, self.weight, self.bias, self.activation,
-                               self.eps)
+                               self.eps, keep)
         return y.reshape(x.shape)
 
     def extra_repr(self) -> str:

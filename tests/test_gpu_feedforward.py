@@ -11,6 +11,7 @@ operands (at most 0.2 % each) add up to less than 2.5 %.  Bounds on rel-L2: 3e-2
 import pytest
 import torch
 
+from paper_2511_01385_amd import api
 from paper_2511_01385_amd.feedforward import AdaptedFeedForward
 from paper_2511_01385_amd.layer import BlockCirculantLinear
 from tests.test_gpu_act8 import reference
@@ -138,3 +139,28 @@ def test_second_derivatives_are_refused():
     assert torch.equal(dx, plain)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         (y.float().sum() + dx.float().square().sum()).backward()
+
+
+@pytest.mark.parametrize("how", ["no_grad", "inference_mode", "frozen"])
+def test_no_checkpoints_without_a_backward(how, monkeypatch):
+    net = AdaptedFeedForward(256, 512, 64)
+    with torch.no_grad():
+        net.c.normal_(std=0.01)
+    x = torch.randn(100, 256, device="cuda").bfloat16()
+    want = net(x).detach()
+
+    def closed(*args, **kwargs):
+        raise AssertionError("a checkpoint was made")
+
+    monkeypatch.setattr(api, "checkpoint_like", closed)
+    monkeypatch.setattr(api, "act8_quantize", closed)
+    if how == "frozen":
+        net.requires_grad_(False)
+        y = net(x)
+    else:
+        with getattr(torch, how)():
+            y = net(x)
+    assert not y.requires_grad and torch.equal(y, want)
+    net.requires_grad_(True)
+    with pytest.raises(AssertionError, match="checkpoint"):
+        net(x)
