@@ -109,7 +109,9 @@ class BlockCirculantLinear(torch.nn.Module):
             raise TypeError(f"input is {x.dtype}, the layer stores {self.dtype}")
         lead = x.shape[:-1]
         x2d = x.reshape(-1, self.d_in).contiguous()
-        y = _BcaFunction.apply(x2d, self.c, self.dtype, self.clobber_grad, self.checkpoint8)
+        # (a checkpoint is made only where there may be a backward)
+        checkpoint8 = self.checkpoint8 and torch.is_grad_enabled() and (x2d.requires_grad or self.c.requires_grad)
+        y = _BcaFunction.apply(x2d, self.c, self.dtype, self.clobber_grad, checkpoint8)
         return y.reshape(*lead, self.d_out)
 
     def extra_repr(self) -> str:

@@ -164,3 +164,27 @@ def test_no_checkpoints_without_a_backward(how, monkeypatch):
     net.requires_grad_(True)
     with pytest.raises(AssertionError, match="checkpoint"):
         net(x)
+
+
+@pytest.mark.parametrize("how", ["no_grad", "inference_mode", "frozen"])
+def test_no_checkpoint_of_the_adapter_without_a_backward(how, monkeypatch):
+    net = BlockCirculantLinear(256, 512, 64, checkpoint8=True)
+    x = torch.randn(100, 256, device="cuda").bfloat16()
+    want = net(x).detach()
+
+    def closed(*args, **kwargs):
+        raise AssertionError("a checkpoint was made")
+
+    monkeypatch.setattr(api, "checkpoint_like", closed)
+    monkeypatch.setattr(api, "act8_quantize", closed)
+    if how == "frozen":
+        net.requires_grad_(False)
+        y = net(x)
+    else:
+        with getattr(torch, how)():
+            y = net(x)
+    assert not y.requires_grad and torch.equal(y, want)
+    for parameter, value in ((True, False), (False, True)):
+        net.requires_grad_(parameter)
+        with pytest.raises(AssertionError, match="checkpoint"):
+            net(x.detach().requires_grad_(value))
