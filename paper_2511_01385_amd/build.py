@@ -59,22 +59,28 @@ def _compile(src: str) -> str:
     return obj
 
 
-def _build_binding() -> None:
-    """Compiles csrc/binding.cpp against torch's headers and the built library, which it finds next to itself."""
-    import torch
+def _build_binding() -> bool:
+    """Compiles csrc/binding.cpp (plain C++) against torch's headers and the built library, which it finds next to itself.
 
+    By hipcc too: no other compiler is needed.  Without torch there is nothing to bind (False): C callers have their library.
+    """
+    try:
+        import torch
+    except ImportError:
+        return False
     root = os.path.dirname(torch.__file__)
     cmd = [
-        os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+        HIPCC, "-x", "c++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
         f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
         f"-I{INCLUDE}", f"-I{root}/include", f"-I{root}/include/torch/csrc/api/include",
         f"-I{sysconfig.get_paths()['include']}", os.path.join(CSRC, "binding.cpp"), "-o", BINDING + ".tmp",
-        LIB, f"-L{root}/lib", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-Wl,-rpath,$ORIGIN",
+        "-x", "none", LIB, f"-L{root}/lib", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-Wl,-rpath,$ORIGIN",
     ]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
-        raise RuntimeError(f"g++ failed on binding.cpp:\n{res.stderr}")
+        raise RuntimeError(f"hipcc failed on binding.cpp:\n{res.stderr}")
     shutil.move(BINDING + ".tmp", BINDING)
+    return True
 
 
 def build(verbose: bool = True) -> str:
@@ -91,9 +97,9 @@ def build(verbose: bool = True) -> str:
     if res.returncode != 0:
         raise RuntimeError(f"link failed:\n{res.stderr}")
     shutil.move(tmp, LIB)
-    _build_binding()
+    bound = _build_binding()
     if verbose:
-        print(f"built {LIB}", file=sys.stderr)
+        print(f"built {LIB}" + ("" if bound else " (without its Python module: there is no torch)"), file=sys.stderr)
     return LIB
 
 
