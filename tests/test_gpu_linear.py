@@ -324,3 +324,62 @@ def test_one_row_of_a_long_stride(dtype):
     dx, dw = api.linear_backward(dy, x, w, dx=torch.empty_like(x), dw=torch.empty_like(w), add=a)[:2]
     got = api.linear_backward(last(dy), last(x), w, dx=last(a), dw=torch.empty_like(w), add=last(a))
     assert torch.equal(got[0], dx) and torch.equal(got[1], dw)
+
+
+# Sizes (tokens, d_in, d_out) for the kernels that those above leave out; what the plan takes for them is named.
+WHOLE = [
+    (806, 5328, 16),      # y: 64 x 64, k split
+    (4179, 4456, 78),     # y: 128 x 128, k split
+    (12440, 712, 296),    # y: 128 x 256
+    (68, 6728, 11220),    # y: 128 x 256, k split
+    (133, 10720, 12632),  # y: 256 x 256, k split
+    (1176, 16, 3448),     # dx: 64 x 64, k split
+    (12840, 72, 16),      # dx: 64 x 64
+    (12931, 208, 16),     # dx: 128 x 128
+    (74, 2704, 7608),     # dx: 128 x 128, k split
+    (5554, 152, 4800),    # dx: 128 x 256, k split
+    (3103, 3848, 688),    # dx: 256 x 256
+    (165, 10928, 8512),   # dx: 256 x 256, k split
+    (7470, 2808, 72),     # dW: 128 x 128, k split
+    (4884, 136, 5488),    # dW: 128 x 256, k split
+    (691, 7600, 1600),    # dW: 256 x 256
+    (7823, 136, 11440),   # dW: 256 x 256, k split
+]
+CUT = [
+    (74, 1353, 16),       # y: 64 x 64, k split
+    (4651, 17, 656),      # y: 128 x 128
+    (2093, 10314, 72),    # y: 128 x 128, k split
+    (308, 773, 11703),    # y: 128 x 256
+    (65, 6309, 12344),    # y: 128 x 256, k split
+    (69, 17, 1559),       # dx: 64 x 64, k split
+    (584, 4925, 16),      # dx: 128 x 128
+    (2314, 67, 8312),     # dx: 128 x 128, k split
+    (11405, 273, 721),    # dx: 128 x 256
+    (6498, 131, 4920),    # dx: 128 x 256, k split
+    (1264, 17, 24),       # dW: 64 x 64, k split
+    (71, 402, 7099),      # dW: 128 x 128
+    (6403, 3332, 81),     # dW: 128 x 128, k split
+    (61, 1001, 999), (40, 333, 8200), (33, 77, 8195),  # few tokens
+]
+FLOAT = [
+    (8549, 1256, 16),     # y: 64 x 64, k split
+    (9695, 16, 1280),     # dx: 64 x 64, k split
+    (107, 531, 16),       # y: 32 x 64, cut, k split
+    (11915, 17, 144),     # y: 64 x 64, cut
+    (8782, 959, 16),      # y: 64 x 64, cut, k split
+    (70, 19, 591),        # dx: 32 x 64, cut, k split
+    (11699, 137, 18),     # dx: 64 x 64, cut
+    (8523, 17, 1232),     # dx: 64 x 64, cut, k split
+    (385, 19, 16),        # dW: 64 x 64, cut, k split
+    (61, 1001, 999), (40, 333, 8200), (33, 77, 8195),  # few tokens, cut
+]
+
+
+@pytest.mark.parametrize("dtype,tokens,d_in,d_out", [(t, *s) for t in ("bf16", "f16") for s in WHOLE + CUT]
+                         + [("f32", *s) for s in FLOAT])
+def test_every_tile(dtype, tokens, d_in, d_out):
+    forward(tokens, d_in, d_out, dtype, seed=tokens)
+    forward(tokens, d_in, d_out, dtype, "gelu", checkpoint=True, seed=tokens + 1)
+    for which in ("x", "w"):  # (apart: each with a plan of its own)
+        backward(tokens, d_in, d_out, dtype, which=which, seed=tokens + 2)
+        backward(tokens, d_in, d_out, dtype, "silu", which=which, add=False, seed=tokens + 3)
