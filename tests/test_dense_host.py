@@ -224,3 +224,17 @@ def test_the_stride_of_one_row_is_not_looked_at(lib):
         assert call(lib, "linear_backward", {**BACK, **change}, 64, 96, 1, 2, BF16, None) == EINVAL
     # ... but a stride shorter than the row is
     assert call(lib, "linear_forward", {**LINEAR, "ldx": 63}, 64, 96, 1, 0, BF16, None) == EINVAL
+
+
+@pytest.mark.skipif(torch.cuda.device_count() > 0, reason="what passes the checks would run, on addresses that are made up")
+def test_slices_side_by_side_pass_the_checks(lib):
+    """Without a GPU a call that every check lets through ends at the device, not as an invalid argument."""
+    fields = {**GRAD, "dy": P[0], "ldg": 128, "ldd": 128, "workspace": 0}
+    for start, want in ((128, _lib.RDFFT_EDEVICE), (126, EINVAL), (130, EINVAL), (64, EINVAL)):  # (rows of 128 bytes in 256)
+        assert call(lib, "layer_norm_backward", {**fields, "dx": P[0] + start}, 4, 64, BF16, None) == want, start
+    assert lib.layer_norm_backward_workspace(4, 64) == 0
+    # a norm's y beside its x, a product's y beside its residual, and both in place
+    for y, want in ((P[0] + 128, _lib.RDFFT_EDEVICE), (P[0], _lib.RDFFT_EDEVICE), (P[0] + 120, EINVAL)):
+        assert call(lib, "layer_norm_forward", {**NORM, "ldx": 128, "ldy": 128, "y": y}, 4, 64, 1e-5, BF16, None) == want
+        fields = {**LINEAR, "residual": P[0], "ldr": 128, "ldy": 128, "y": y, "x": P[8], "codes": 0, "scales": 0}
+        assert call(lib, "linear_forward", fields, 64, 64, 4, 0, BF16, None) == want
