@@ -105,23 +105,7 @@ hipError_t with_elem(int storage, F&& fn) {
   }
 }
 
-// Values i0 ... i0+7 of a row of n, zeros past its end.  The load of a whole group is issued
-// whatever i0 (clamped into the row), without a branch around it; n >= 8 for that.
-template <class E>
-__device__ __forceinline__ typename E::Raw load_group(const typename E::T* row, int64_t i0, int64_t n) {
-  return E::load(row + (i0 + kVec <= n ? i0 : 0));
-}
-template <class E>
-__device__ __forceinline__ void widen_group(const typename E::Raw& r, const typename E::T* row, int64_t i0, int64_t n,
-                                            float* v) {
-  if (i0 + kVec <= n) {
-    E::widen(r, v);
-  } else {
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) v[i] = i0 + i < n ? E::get(row + i0 + i) : 0.f;
-  }
-}
-// both at once, for rows of any length
+// Values i0 ... i0+7 of a row of n of any length, zeros past its end.
 template <class E>
 __device__ __forceinline__ void read_group(const typename E::T* row, int64_t i0, int64_t n, float* v) {
   if (i0 + kVec <= n) {
@@ -221,10 +205,7 @@ __device__ __forceinline__ void ck_decode(const Bytes8& r, float scale, float* v
   }
 }
 
-// Eight codes of a row, zeros past its end (the load clamped as load_group's).
-__device__ __forceinline__ Bytes8 load_codes(const int8_t* row, int64_t i0, int64_t n) {
-  return *reinterpret_cast<const Bytes8*>(row + (i0 + kVec <= n ? i0 : 0));
-}
+// Eight codes of a row, zeros past its end.
 __device__ __forceinline__ Bytes8 tail_codes(const int8_t* row, int64_t i0, int64_t n) {
   Bytes8 r = {{0, 0}};
 #pragma unroll
