@@ -244,7 +244,8 @@ typedef struct {
 } act8_t;
 
 /* act8_quantize / act8_dequantize -- rows x n values into their checkpoint, and back (the values
- * that it stands for, rounded to dtype: a checkpoint of larger numbers than float16 has becomes infinities there).  n >= 1; rows == 0 is a no-op. */
+ * that it stands for, rounded to dtype: a checkpoint of larger numbers than float16 has becomes infinities
+ * there).  n >= 1; rows == 0 is a no-op. */
 RDFFT_API int act8_quantize(const void *x, int64_t ldx, const act8_t *to, int64_t rows, int64_t n, rdfft_dtype_t dtype,
                             rdfft_stream_t stream);
 RDFFT_API int act8_dequantize(const act8_t *from, void *out, int64_t ldo, int64_t rows, int64_t n, rdfft_dtype_t dtype,
@@ -346,7 +347,9 @@ RDFFT_API int linear_forward(const linear_forward_t *a, int64_t d_in, int64_t d_
  * linear_backward -- with dz = dy * act'(z), z being what the checkpoint stands for:
  *   dx = dz W (+ add),  dw = dz^T x,  db = sum over tokens of dz.
  * Each of dx, dw, db is computed if its pointer is not null.  (The residual's gradient is dy.)
- *   checkpoint unused (and may be null) for RDFFT_ACT_NONE.
+ *   checkpoint unused (and may be null) for RDFFT_ACT_NONE.  A positive z of less than half its block's step is held as
+ *              zero, where RDFFT_ACT_RELU has slope 0: of normal z 0.6 % of the values, which puts dz 0.11 of its norm
+ *              off the gradient at z itself.  GELU's and SILU's slopes, which have no jump, are off by less than 0.01.
  *   x          needed for dw only, w for dx only.
  *   add        [tokens][d_in] or null: a gradient that reaches x another way; dx may be add itself
  *              (same pointer and stride).

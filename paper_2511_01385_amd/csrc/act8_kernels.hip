@@ -5,8 +5,8 @@
 // maximum is two cross-lane moves and nothing goes through LDS.  Rows that follow each other
 // without a gap and end with a block are one long row, which needs no index arithmetic.
 //
-// 16384 x 4096 bf16 values: quantize 35 us (203 MB, 5.9 TB/s), dequantize 30 us (6.7 TB/s); a copy of 1 GiB runs at
-// 5.2 TB/s.  128 x 256 floats: 2.5 us each, a launch's length.
+// 16384 x 4096 bf16 values: quantize 39 us (203 MB, 5.2 TB/s), dequantize 31 us (6.6 TB/s); a copy of 1 GiB runs at
+// 5.2 TB/s.  128 x 256 floats: 2.9 us each, a launch's length.
 #include <hip/hip_runtime.h>
 
 #include "dense_device.hpp"

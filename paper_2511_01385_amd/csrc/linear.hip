@@ -54,7 +54,7 @@ static hipError_t join(GemmArgs g, hipStream_t stream) {
 // of slope_pitch values, so that it is loaded like an aligned operand whatever d_out; and the column sums
 // of the unrounded dz.  A workgroup takes a strip of 512 columns, its four waves every fourth row of its
 // range; partials[blockIdx.y][n] receive the sums, or db where there is one range.
-// 8192 x 8192 bf16: 72 us (346 MB, 4.8 TB/s; one row at a time in a wave 88), 4096 x 768: 8 us (16).
+// 8192 x 8192 bf16: 72 to 78 us (346 MB, 4.4 to 4.8 TB/s), 4096 x 768: 8.8 us.
 constexpr int kSlopeWG = 256, kSlopeWaves = 4, kSlopeStrip = 64 * kVec, kSlopeAhead = 4;
 constexpr int64_t kSlopeMaxParts = 256;
 
@@ -144,12 +144,13 @@ static int64_t slope_parts(int64_t rows, int64_t n) {
 // ----------------------------------------------------------------------------------
 // plans
 
-// What a tile costs, in us, from products of 128 to 8192: a stage (128 bytes of k) where a CU has one workgroup
+// What a tile costs, in us, fitted to products of 128 to 8192: a stage (128 bytes of k) where a CU has one workgroup
 // of them, a stage of each where it has more (`together` fit), and what comes before and after.  16-bit values: the largest
-// tile reaches 1390 to 1420 TFLOP/s where its tiles fill the chip in whole rounds; the smaller ones 1270, 1200 and 780, but
-// leave fewer CUs idle: 4096 x 768 x 768 (12 stages) takes 10 us in tiles of 128 or 64 and 15 and 23 in the larger two,
-// 2045 x 4096 x 4096 58 us in 128 x 256, 61, 81 and 92 in 128, 256 and 64; 128 x 4096 x 4096 16 us in 32 x 64 and 64,
-// 38 in 128.  float32: the matrix cores bound every tile alike (142 TFLOP/s); 300 x 768 x 768 10 us in 32 x 64, 16 in 64.
+// tile is the fastest where its tiles fill the chip in whole rounds (1390 TFLOP/s); the smaller ones leave fewer CUs idle.
+// Unsplit, in the kernel, averages in turn: 4096 x 768 x 768 (12 stages) 11.6 us in tiles of 128, 12.0 in 64, 15.4 in
+// 32 x 64, 15.6 and 22.9 in the larger two; 2045 x 4096 x 4096 59 us in 128 x 256, 64, 88 and 97 in 128, 256 and 64;
+// 128 x 4096 x 4096 17 us in 32 x 64, 18 in 64, 40 in 128.  float32: 4096 x 4096 x 4096 1013 us in 64, 1055 in 32 x 64;
+// 300 x 768 x 768 11.4 us in 32 x 64, 16.7 in 64.
 struct TileCost {
   int bm, bn, together;
   double alone, each, ends;
@@ -243,7 +244,7 @@ static hipError_t product(GemmArgs& g, int64_t a_len, LinearOperands kind, int s
   g.splits = 1;
   if (kind == kForward && g.m <= kFewTokens) {
     // 32 rows of W to a workgroup where that still fills the chip (x is read half as often: 64 tokens of 8192 x 8192
-    // 22.6 us, else 31.0) or a checkpoint's blocks ask for it; 16 otherwise (one token of 4096 x 4096 4.8 us, else 6.1)
+    // 22.8 us, else 31.3) or a checkpoint's blocks ask for it; 16 otherwise (one token of 4096 x 4096 5.9 us, else 7.2)
     const bool wide = g.ck.codes != nullptr || g.n >= 32 * kCUs;
     return t.few[g.m <= 16 ? 0 : g.m <= 32 ? 1 : 2][wide][direct](g, stream);
   }
@@ -258,11 +259,11 @@ static hipError_t product(GemmArgs& g, int64_t a_len, LinearOperands kind, int s
 
 // Which tile dW and dx share in one launch, or kLinearTiles where two launches cost less.  The product with the longer k
 // goes first.  Where it has a workgroup for every CU the rounds are simply full; where it has fewer, its CUs deal
-// part of their time to the other's tiles until those run out, and finish alone.  This tells the time to
-// about 8 % (dx and dW of 512 to 16384 tokens of 128 to 5120, bf16 and float32), so it has to be that much less.
-// One launch and two, us (tokens x d_in x d_out): 1021 x 1024 x 768 float32 42 and 49; bf16 512 x 768 x 768 12.6 and 16.6, 2045 x
-// 2048 x 2048 42 and 57, 4096 x 768 x 2560 53 and 70.  Two stay: bf16 4096 x 768 x 768 (54 and 51), 2048 x 4096 x 4096 (136 and 128), 8192 x 768 x 768
-// (65 and 46, its dW's k split).
+// part of their time to the other's tiles until those run out, and finish alone.  Its times are good to about 8 % for most
+// sizes, so one launch has to take that much less.
+// One launch and two, us in the kernels (tokens x d_in x d_out): 1021 x 1024 x 768 float32 35.7 and 42.7; bf16 512 x 768 x
+// 768 6.8 and 11.5, 2045 x 2048 x 2048 38.9 and 54.9, 4096 x 768 x 2560 44.1 and 64.7.  Two stay: 2048 x 4096 x 4096 (123
+// and 124), 8192 x 768 x 768 (40.7 and 40.2, its dW's k split), and 4096 x 768 x 768, where the model is wrong (23.5 and 30.2).
 static LinearTile together_of(const GemmArgs& dw, const GemmArgs& dx, int storage) {
   const bool f32 = storage == kStorageF32;
   const int64_t bk = kStageBytes / (f32 ? 4 : 2);

@@ -27,11 +27,12 @@
 // blocks run.  k is spread over a fragment's four lane groups in runs of one chunk, for both
 // operands alike.  Sums are float32 throughout.
 //
-// What bounds it: 8192 x 4096 x 8192 (bf16, normal values) takes 395 us, 1390 TFLOP/s, next to 1300 to
-// 1470 of the library's bare products on the same card; the matrix cores are busy 74 % of the CUs'
-// cycles, at a clock that such work takes down to about 1.9 GHz.  The forward of 8192 tokens, 4096 ->
-// 8192, takes 387 us without anything in its epilogue (library 375), 410 with gelu, 440 with the
-// checkpoint and 466 with both: the epilogues of a round of tiles coincide.
+// What bounds it: dx and dW of 8192 tokens, 4096 -> 8192 (bf16, normal values) take 397 and 405 us, 1390 and
+// 1360 TFLOP/s (the library's bare products 413 and 515); the matrix cores are busy 74 % of the CUs' cycles, at a
+// clock that such work takes down to about 1.9 GHz.  The forward takes 418 us without anything in its epilogue (library
+// 370), 451 with gelu, 444 with the checkpoint, 469 with both and 494 with a residual besides: the epilogues of a round
+// of tiles coincide.  (Averages of 60 launches of each in random order; what ran before moves the clock, and one of
+// these by up to 10 %.)
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -66,7 +67,8 @@ __device__ __forceinline__ f32x4 mfma_chunk(u32x4 a, u32x4 b, f32x4 c) {
 
 // ----------------------------------------------------------------------------------
 // activations.  erf by Abramowitz and Stegun's 7.1.26 (absolute error 1.5e-7), whose exp(-x^2) is
-// also the density in gelu's slope.
+// also the density in gelu's slope.  For float32 storage too: gelu is 9e-8 of its norm off, where a
+// correctly rounded erf leaves 4e-8; relatively it loses most where it is next to nothing (5e-4 at -4).
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float rcp_fast(float x) { return __builtin_amdgcn_rcpf(x); }
@@ -809,8 +811,8 @@ hipError_t grads_launch(const GemmArgs& dw, const GemmArgs& dx, hipStream_t stre
 // W's rows, each of its waves a range of k.  With direct loads a wave streams its part of both operands through LDS
 // of its own, STAGES stages of 128 bytes of k a row, without a barrier: whole cache lines, many of them in
 // flight, and no registers held for them.  Without (rows that start anywhere) the fragments come from
-// memory, half a line a row and instruction.  The waves' sums meet in LDS.  One token of 4096 x 4096: 4.8 us
-// (33.6 MB that the Infinity Cache holds: 7 TB/s), 6.8 without; 61 tokens, 1024 -> 4096: 4.3 and 6.9.
+// memory, half a line a row and instruction.  The waves' sums meet in LDS.  One token of 4096 x 4096, with a residual:
+// 5.9 us (33.6 MB that the Infinity Cache holds: 5.7 TB/s), 7.7 without; 61 tokens, 1024 -> 4096, gelu: 5.3 and 7.7.
 template <class E, int MT, int NT, int WAVES, int STAGES, LoadPath PATH>
 __global__ void __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(2))) linear_few_kernel(GemmArgs g) {
   using T = typename E::T;
@@ -972,7 +974,8 @@ LinearTable make_linear_table() {
       t.fn[kTile32x64][o][1] = linear_launch<E, 32, 64, 2, 2, 3, AX, BX, W>;
       if constexpr (F32) t.fn[kTile32x64][o][0] = linear_launch<E, 32, 64, 2, 2, 3, AX, BX, ANY>;
     }
-    // (float32 products are bound by the matrix cores in the smallest tiles already: 142 to 144 TFLOP/s)
+    // (float32 products are bound by the matrix cores in the smallest tiles already: 4096 x 4096 x 4096 takes 970 to 1010 us
+    // in 64 x 64, 136 to 141 TFLOP/s, the library 960 to 1000)
     if constexpr (!F32) {
       t.fn[kTile128][o][0] = linear_launch<E, 128, 128, 2, 4, 2, AX, BX, ANY>;
       // (both operands across k need more than the 256 registers there are)

@@ -14,10 +14,11 @@
 // in a fixed order and each workgroup leaves one row of partial sums (2n floats); a second launch adds
 // those.  No atomics: results do not depend on the order of execution.
 //
-// 16384 x 4096 bf16 with a residual and a checkpoint: forward 88 us (472 MB, 5.4 TB/s), backward 69 us (337 MB,
-// 4.9 TB/s) and 4 us for the join; 4096 x 768: 7.4, 8.1 and 1.8 us, two or three trips to memory one after another.  One
-// wave per row up to 1024 values (no barrier), a workgroup beyond; rows of more than 8192 values run at about 60 %
-// of those rates in the backward, whose threads then hold two groups each and spill.
+// 16384 x 4096 bf16 with a residual and a checkpoint: forward 91 us (472 MB, 5.2 TB/s), backward 76 us after forwards
+// and 68 after itself (337 MB, 4.4 and 4.9 TB/s) and 5 us for the join; from x and the residual, without a checkpoint, 79 us
+// (403 MB) and 99 (537 MB).  4096 x 768: 7.7, 8.4 and 3.5 us, two or three trips to memory one after another.  One wave per
+// row up to 1024 values (no barrier), a workgroup beyond.  Rows of more than 8192 values run at half the rate in the
+// backward, whose threads then hold two groups each and spill (4096 x 16384: forward 98 us, backward 137).
 #include <hip/hip_runtime.h>
 
 #include "dense_device.hpp"

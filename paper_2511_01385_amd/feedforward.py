@@ -9,8 +9,9 @@ the second one's residual (written over it), the sum with x inside the norm.
 
 Memory: between forward and backward a token keeps the pre-activation and h (d_ff values each) and the norm's
 input (d_model values), all as 8-bit checkpoints: 33/32 bytes a value, instead of x, the pre-activation, h and the
-norm's input in the storage type.  Gradients are taken at the checkpointed values.  Where no gradient can be asked for
-(``torch.no_grad()``, or nothing that requires one) no checkpoint is made.
+norm's input in the storage type.  Gradients are taken at the checkpointed values, in float32 too (with "relu" that
+costs accuracy: see ``api.linear_backward``).  Where no gradient can be asked for (``torch.no_grad()``, or nothing that
+requires one) no checkpoint is made.
 """
 
 from __future__ import annotations
