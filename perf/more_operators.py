@@ -15,7 +15,7 @@ Seven kinds of case:
 
 The 8-bit floating point format: blocks of 128 consecutive values of a row (the last may be short), or tiles of 128 x 128
 of a weight, share a power of two 2^e, the least with max|x| <= 448 * 2^e; each value is x / 2^e rounded to e4m3.
-A row starts at a multiple of 16 bytes.  The int8 checkpoint: blocks of 32, rint(x / 2^e), max|x| <= 127 * 2^e.
+A row of codes starts at a multiple of 16 bytes, one of scales at a multiple of 4.  The int8 checkpoint: blocks of 32, rint(x / 2^e), max|x| <= 127 * 2^e.
 """
 
 from __future__ import annotations
@@ -144,7 +144,8 @@ def _weight(g, d_out, d_in):
 def _empty8(rows, n, tiles=False):
     """Room for rows x n values in 8 bits."""
     codes = torch.empty(rows, -(-n // 16) * 16, dtype=torch.float8_e4m3fn, device="cuda")[:, :n]
-    return codes, torch.empty(-(-rows // BLOCK) if tiles else rows, -(-n // BLOCK), dtype=torch.uint8, device="cuda")
+    blocks, bands = -(-n // BLOCK), -(-rows // BLOCK) if tiles else rows
+    return codes, torch.empty(bands, -(-blocks // 4) * 4, dtype=torch.uint8, device="cuda")[:, :blocks]
 
 
 def _filled8(x, tiles=False):
