@@ -381,6 +381,160 @@ RDFFT_API int64_t linear_backward_workspace(int64_t d_in, int64_t d_out, int64_t
 RDFFT_API int linear_backward(const linear_backward_t *a, int64_t d_in, int64_t d_out, int64_t tokens,
                               rdfft_activation_t act, rdfft_dtype_t dtype, rdfft_stream_t stream);
 
+/* -------------------------------------------------------------------------------------------
+ * The same around a decoder's layer: RMS norm, and the dense product of operands in 8-bit floating point.  The conventions
+ * of the section above hold.
+ */
+
+/*
+ * The 8-bit floating point format.  128 consecutive values of a row (the last block of a row may be short), or the values of
+ * a tile of 128 x 128 (those at the edges may be smaller), share a power of two 2^e, the least one with
+ * max|x| <= 448 * 2^e and e >= -127.  A value is held as x / 2^e rounded to e4m3 (half to even), and stands for
+ * code * 2^e; the block's scale is the byte e + 127.  A block with an infinity or a NaN has scale byte 255 and NaN codes.
+ * An operand of a product has its blocks along the direction that is summed over.
+ *   codes      rows of n codes, `ld` bytes apart (at least n), each starting at a multiple of 16 bytes.
+ *   scales     rows of ceil(n/128) bytes, `lds` apart (at least that), each starting at a multiple of 4 bytes.
+ *              (Strides of a single row are not looked at.)
+ *   block_rows 1: a row of scales for each row of codes; 128: one for 128 rows of codes (tiles).
+ * What follows a row's last value up to the next multiple of 16 codes (4 scales) may be read, but is of no account; it is
+ * never written.
+ */
+typedef struct {
+  uint8_t *codes;
+  int64_t ld;
+  uint8_t *scales;
+  int64_t lds;
+  int64_t block_rows;
+} fp8_t;
+
+/* fp8_quantize -- x [rows][n] into its 8-bit form: `held` [rows][n] and `columns` [n][rows], of x's transpose, with
+ * blocks along x's columns.  Either may be null; both have the same block_rows (of a single row either will do), and
+ * with tiles the same values.
+ * fp8_dequantize -- the values that it stands for, rounded to dtype.  code * 2^e that is the power of two past the
+ * type's largest number M (of values within 1/32 of M) comes back as +-M.
+ * rows == 0 is a no-op; n >= 1, in fp8_quantize at most 2^29 (more -> RDFFT_EUNSUPPORTED). */
+RDFFT_API int fp8_quantize(const void *x, int64_t ldx, const fp8_t *held, const fp8_t *columns, int64_t rows, int64_t n,
+                           rdfft_dtype_t dtype, rdfft_stream_t stream);
+RDFFT_API int fp8_dequantize(const fp8_t *from, void *out, int64_t ldo, int64_t rows, int64_t n, rdfft_dtype_t dtype,
+                             rdfft_stream_t stream);
+
+/*
+ * rms_norm_forward -- per row, u = x (+ residual) rounded to dtype, y = u * rstd * weight with
+ * rstd = (mean(u^2) + eps)^(-1/2).  1 <= n <= 16384 (more -> RDFFT_EUNSUPPORTED).
+ *   residual   may be null.  weight: float32 [n].
+ *   y, y8      the result in dtype and in 8-bit floating point (block_rows 1, from the float32 value); codes null: none.
+ *              Either may be null.
+ *   summed     u, written; may be null.
+ *   y, summed  may be x or residual (same pointer and stride), but not each other.
+ *   rstd       float32 [rows], written; may be null.
+ *   checkpoint of u, written; codes null: none.
+ *   eps        >= 0.
+ */
+typedef struct {
+  const void *x;
+  int64_t ldx;
+  const void *residual;
+  int64_t ldr;
+  const float *weight;
+  void *y;
+  int64_t ldy;
+  void *summed;
+  int64_t lds;
+  float *rstd;
+  act8_t checkpoint;
+  fp8_t y8;
+} rms_norm_forward_t;
+RDFFT_API int rms_norm_forward(const rms_norm_forward_t *a, int64_t rows, int64_t n, float eps, rdfft_dtype_t dtype,
+                               rdfft_stream_t stream);
+
+/*
+ * rms_norm_backward -- with xh = u * rstd, g = dy * weight:
+ *   dx = rstd * (g - xh * mean(g * xh)) (+ add), the gradient of x and of residual,
+ *   dweight = sum over rows of dy * xh  (float32 [n], overwritten; may be null).
+ *   u          the norm's input, or with u null what the checkpoint stands for.
+ *   rstd       as rms_norm_forward left it.
+ *   add        the gradient that reaches the sum another way (the residual stream); may be null.
+ *   dx         may be dy or add itself (same pointer and stride).
+ * rows == 0 writes zeros into dweight.
+ */
+typedef struct {
+  const void *dy;
+  int64_t ldg;
+  const void *u;
+  int64_t ldu;
+  act8_t checkpoint;
+  const float *weight;
+  const float *rstd;
+  const void *add;
+  int64_t lda;
+  void *dx;
+  int64_t ldd;
+  float *dweight;
+  void *workspace;
+  int64_t workspace_bytes;
+} rms_norm_backward_t;
+/* bytes (0: none is needed), or a negative rdfft_status_t */
+RDFFT_API int64_t rms_norm_backward_workspace(int64_t rows, int64_t n);
+RDFFT_API int rms_norm_backward(const rms_norm_backward_t *a, int64_t rows, int64_t n, rdfft_dtype_t dtype,
+                                rdfft_stream_t stream);
+
+/*
+ * linear_fp8_forward -- per token z = W x + bias, y = act(z) + residual, as linear_forward.
+ *   x [tokens][d_in], w [d_out][d_in] in 8-bit floating point, of either block_rows each.
+ *   bias [d_out], residual [tokens][d_out] (null: none) and y [tokens][d_out] in dtype; y may be residual itself.
+ *   checkpoint of z (of its float32 value), written, for linear_fp8_backward; codes null: none.
+ * Sums are float32.  For a 16-bit dtype the 8-bit matrix instructions drop what lies about 16 bits below the largest product
+ * that they add (1.5e-5 of the result's norm for normal values); with RDFFT_F32 every product counts in full, at half the
+ * rate.  Sizes as for linear_forward; strides at most 2^21.
+ */
+typedef struct {
+  fp8_t x;
+  fp8_t w;
+  const void *bias;
+  const void *residual;
+  int64_t ldr;
+  void *y;
+  int64_t ldy;
+  act8_t checkpoint;
+  void *workspace;
+  int64_t workspace_bytes;
+} linear_fp8_forward_t;
+/* bytes (0: none is needed), or a negative rdfft_status_t */
+RDFFT_API int64_t linear_fp8_forward_workspace(int64_t d_in, int64_t d_out, int64_t tokens, rdfft_dtype_t dtype);
+RDFFT_API int linear_fp8_forward(const linear_fp8_forward_t *a, int64_t d_in, int64_t d_out, int64_t tokens,
+                                 rdfft_activation_t act, rdfft_dtype_t dtype, rdfft_stream_t stream);
+
+/*
+ * linear_fp8_backward -- with dz = dy * act'(z), z being what the checkpoint stands for:
+ *   dx = dz W (+ add),  dw = dz^T x,  db = sum over tokens of dz.
+ * dz enters the products in 8-bit floating point, in blocks of 128 along d_out for dx and along the tokens for dw (from
+ * the float32 value); db sums the float32 dz.  Each of dx, dw, db is computed if its pointer is not null.
+ *   x          [d_in][tokens], the columns that fp8_quantize leaves of x; for dw only.
+ *   w          [d_in][d_out], the columns that it leaves of W; for dx only.
+ *   the rest   as for linear_backward.
+ */
+typedef struct {
+  const void *dy;
+  int64_t ldg;
+  act8_t checkpoint;
+  fp8_t x;
+  fp8_t w;
+  const void *add;
+  int64_t lda;
+  void *dx;
+  int64_t ldd;
+  void *dw;
+  int64_t lddw;
+  void *db;
+  void *workspace;
+  int64_t workspace_bytes;
+} linear_fp8_backward_t;
+/* for the gradients that are wanted (nonzero) */
+RDFFT_API int64_t linear_fp8_backward_workspace(int64_t d_in, int64_t d_out, int64_t tokens, int dx, int dw, int db,
+                                                rdfft_dtype_t dtype);
+RDFFT_API int linear_fp8_backward(const linear_fp8_backward_t *a, int64_t d_in, int64_t d_out, int64_t tokens,
+                                  rdfft_activation_t act, rdfft_dtype_t dtype, rdfft_stream_t stream);
+
 /* Uploads the twiddle table to the current device (synchronously) if not done yet.
  * Optional: every entry point does it on first use.  Returns RDFFT_OK or RDFFT_EDEVICE. */
 RDFFT_API int rdfft_init(void);

@@ -49,6 +49,15 @@ EXPORTS = (
     "linear_forward",
     "linear_backward_workspace",
     "linear_backward",
+    "fp8_quantize",
+    "fp8_dequantize",
+    "rms_norm_forward",
+    "rms_norm_backward_workspace",
+    "rms_norm_backward",
+    "linear_fp8_forward_workspace",
+    "linear_fp8_forward",
+    "linear_fp8_backward_workspace",
+    "linear_fp8_backward",
     "rdfft_init",
     "rdfft_table_bytes",
     "rdfft_status_string",
@@ -70,6 +79,13 @@ _FIELDS = {
                            "workspace_bytes",
     "linear_forward": "x ldx w ldw bias residual ldr y ldy codes scales workspace workspace_bytes",
     "linear_backward": "dy ldg codes scales x ldx w ldw add lda dx ldd dw lddw db workspace workspace_bytes",
+    "fp8": "codes ld scales lds block_rows",
+    "rms_norm_forward": "x ldx residual ldr weight y ldy summed lds rstd codes scales codes8 ld8 scales8 lds8 block_rows8",
+    "rms_norm_backward": "dy ldg u ldu codes scales weight rstd add lda dx ldd dweight workspace workspace_bytes",
+    "linear_fp8_forward": "x ldx x_scales ldxs x_block_rows w ldw w_scales ldws w_block_rows bias residual ldr y ldy codes "
+                          "scales workspace workspace_bytes",
+    "linear_fp8_backward": "dy ldg codes scales x ldx x_scales ldxs x_block_rows w ldw w_scales ldws w_block_rows add lda dx "
+                           "ldd dw lddw db workspace workspace_bytes",
 }
 pack = {name: struct.Struct(f"{len(fields.split())}q").pack for name, fields in _FIELDS.items()}
 
@@ -106,13 +122,24 @@ def load() -> ctypes.CDLL:
     lib.layer_norm_backward.argtypes = [vp, i64, i64, i32, vp]
     lib.linear_forward.argtypes = [vp, i64, i64, i64, i32, i32, vp]
     lib.linear_backward.argtypes = [vp, i64, i64, i64, i32, i32, vp]
+    lib.fp8_quantize.argtypes = [vp, i64, vp, vp, i64, i64, i32, vp]
+    lib.fp8_dequantize.argtypes = [vp, vp, i64, i64, i64, i32, vp]
+    lib.rms_norm_forward.argtypes = [vp, i64, i64, f32, i32, vp]
+    lib.rms_norm_backward.argtypes = [vp, i64, i64, i32, vp]
+    lib.linear_fp8_forward.argtypes = [vp, i64, i64, i64, i32, i32, vp]
+    lib.linear_fp8_backward.argtypes = [vp, i64, i64, i64, i32, i32, vp]
     for name in ("act8_quantize", "act8_dequantize", "layer_norm_forward", "layer_norm_backward", "linear_forward",
-                 "linear_backward"):
+                 "linear_backward", "fp8_quantize", "fp8_dequantize", "rms_norm_forward", "rms_norm_backward",
+                 "linear_fp8_forward", "linear_fp8_backward"):
         getattr(lib, name).restype = i32
     lib.layer_norm_backward_workspace.argtypes = [i64, i64]
     lib.linear_forward_workspace.argtypes = [i64, i64, i64, i32]
     lib.linear_backward_workspace.argtypes = [i64, i64, i64, i32, i32, i32, i32, i32]
-    for name in ("layer_norm_backward_workspace", "linear_forward_workspace", "linear_backward_workspace"):
+    lib.rms_norm_backward_workspace.argtypes = [i64, i64]
+    lib.linear_fp8_forward_workspace.argtypes = [i64, i64, i64, i32]
+    lib.linear_fp8_backward_workspace.argtypes = [i64, i64, i64, i32, i32, i32, i32]
+    for name in ("layer_norm_backward_workspace", "linear_forward_workspace", "linear_backward_workspace",
+                 "rms_norm_backward_workspace", "linear_fp8_forward_workspace", "linear_fp8_backward_workspace"):
         getattr(lib, name).restype = i64
     lib.rdfft_init.argtypes = []
     lib.rdfft_init.restype = i32

@@ -559,6 +559,239 @@ def linear_backward_workspace(d_in: int, d_out: int, tokens: int, dtype: torch.d
     return _need("linear_backward_workspace", d_in, d_out, tokens, dx, dw, db, _activation(activation), _CODES[dtype])
 
 
+FP8_BLOCK = 128
+_FP8 = torch.float8_e4m3fn
+
+
+def _held8(held, device: int, rows: int, n: int, what: str) -> tuple[int, int, int, int, int]:
+    """Pointers and row strides of a (codes, scales) pair in 8-bit floating point for (rows, n) values, and its block_rows."""
+    codes, scales = held
+    if codes is None or scales is None:
+        raise ValueError(f"{what} is the pair (codes, scales), and one of them is None")
+    blocks, bands = -(-n // FP8_BLOCK), -(-rows // FP8_BLOCK)
+    if scales.dim() != 2 or scales.shape[1] != blocks or scales.shape[0] not in (rows, bands):
+        raise ValueError(f"the scales of {what} must have shape {(rows, blocks)}, or {(bands, blocks)} in tiles, "
+                         f"got {tuple(scales.shape)}")
+    return (*_rows(codes, f"codes of {what}", _FP8, device, (rows, n)),
+            *_rows(scales, f"scales of {what}", torch.uint8, device, tuple(scales.shape)),
+            1 if scales.shape[0] == rows else FP8_BLOCK)
+
+
+def fp8_like(x: torch.Tensor, *, columns: bool = False, tiles: bool = False) -> tuple[torch.Tensor, torch.Tensor]:
+    """Empty (codes, scales) in 8-bit floating point for a (rows, n) tensor, or for its ``columns`` (its transpose).
+
+    A scale is for 128 consecutive values of a row or, with ``tiles``, for 128 x 128.
+    """
+    rows, n = reversed(x.shape) if columns else x.shape
+    blocks, bands = -(-n // FP8_BLOCK), -(-rows // FP8_BLOCK) if tiles else rows
+    codes = torch.empty((rows, -(-n // 16) * 16), dtype=_FP8, device=x.device)
+    scales = torch.empty((bands, -(-blocks // 4) * 4), dtype=torch.uint8, device=x.device)
+    return codes[:, :n], scales[:, :blocks]
+
+
+def fp8_quantize(x: torch.Tensor, held=None, *, columns=None):
+    """Writes x (rows, n) in 8-bit floating point into ``held`` (codes, scales), and its transpose into ``columns``.
+
+    The shape of the scales says whether a scale is for 128 values of a row or for a tile of 128 x 128.
+    """
+    if held is None and columns is None:
+        raise ValueError("fp8_quantize needs held or columns to write to")
+    status = None
+    if x.is_cuda:
+        device = _current_device()
+        status = _lib.binding().fp8_quantize(x, *(held or _NONE), *(columns or _NONE), device, _raw_stream(device))
+    if status is None:
+        p, ld, shape, dtype, code, device, stream = _first(x, "x")
+        rows, n = shape
+        to = None if held is None else _lib.pack["fp8"](*_held8(held, device, rows, n, "held"))
+        across = None if columns is None else _lib.pack["fp8"](*_held8(columns, device, n, rows, "columns"))
+        status = _lib.load().fp8_quantize(p, ld, to, across, rows, n, code, stream)
+    if status:
+        _check(status, "fp8_quantize")
+    return held, columns
+
+
+def fp8_dequantize(held, out: torch.Tensor) -> torch.Tensor:
+    """What (codes, scales) in 8-bit floating point stand for, in ``out``'s type (exact in float32 and bfloat16)."""
+    status = None
+    if out.is_cuda:
+        device = _current_device()
+        status = _lib.binding().fp8_dequantize(*held, out, device, _raw_stream(device))
+    if status is None:
+        p, ld, shape, dtype, code, device, stream = _first(out, "out")
+        rows, n = shape
+        status = _lib.load().fp8_dequantize(_lib.pack["fp8"](*_held8(held, device, rows, n, "held")), p, ld, rows, n, code,
+                                            stream)
+    if status:
+        _check(status, "fp8_dequantize")
+    return out
+
+
+def rms_norm_forward(x, weight, y=None, *, residual=None, summed=None, rstd=None, checkpoint=None, y8=None, eps=1e-6):
+    """y = u / sqrt(mean(u^2) + eps) * weight per row, u = x (+ residual) rounded to x's type; weight and rstd are float32.
+
+    Written if given: ``y``, ``y8`` (codes, scales), which is y in 8-bit floating point, ``summed``, which is u, ``rstd``
+    (rows,), and ``checkpoint``, of u.  ``y`` and ``summed`` may be ``x`` or ``residual``.
+    """
+    status = None
+    if x.is_cuda:
+        device = _current_device()
+        codes, scales = _NONE if checkpoint is None else checkpoint
+        codes8, scales8 = _NONE if y8 is None else y8
+        status = _lib.binding().rms_norm_forward(x, residual, weight, y, summed, rstd, codes, scales, codes8, scales8, eps,
+                                                 device, _raw_stream(device))
+    if status is None:
+        p, ld, shape, dtype, code, device, stream = _first(x, "x")
+        rows, n = shape
+        none = (0, 0)
+        a = _lib.pack["rms_norm_forward"](
+            p, ld,
+            *(none if residual is None else _rows(residual, "residual", dtype, device, shape)),
+            _vector(weight, "weight", _F32, device, n),
+            *(none if y is None else _rows(y, "y", dtype, device, shape)),
+            *(none if summed is None else _rows(summed, "summed", dtype, device, shape)),
+            0 if rstd is None else _vector(rstd, "rstd", _F32, device, rows),
+            *(none if checkpoint is None else _held(checkpoint, device, rows, n)),
+            *((0, 0, 0, 0, 0) if y8 is None else _held8(y8, device, rows, n, "y8")))
+        status = _lib.load().rms_norm_forward(a, rows, n, eps, code, stream)
+    if status:
+        _check(status, "rms_norm_forward")
+    return y
+
+
+def rms_norm_backward(dy, u, weight, rstd, dx, dweight=None, *, add=None, workspace=None):
+    """Writes the norm's gradients: dx (+ ``add``), of x and of the residual alike, and float32 dweight if given.
+
+    ``u`` is what the forward left in ``summed`` (x itself without a residual), or its checkpoint (codes, scales); ``add`` a
+    gradient that reaches the sum another way.  ``dx`` may be ``dy`` or ``add``.
+    ``workspace``: ``rms_norm_backward_workspace(rows, n)`` bytes, allocated if not given (none without dweight).
+    """
+    status = None
+    values = isinstance(u, torch.Tensor)
+    if dy.is_cuda:
+        device = _current_device()
+        codes, scales = _NONE if values else u
+        status = _lib.binding().rms_norm_backward(dy, u if values else None, codes, scales, weight, rstd, add, dx, dweight,
+                                                  workspace, device, _raw_stream(device))
+    if status is None:
+        p, ld, shape, dtype, code, device, stream = _first(dy, "dy")
+        rows, n = shape
+        inputs = (*_rows(u, "u", dtype, device, shape), 0, 0) if values else (0, 0, *_held(u, device, rows, n))
+        keep, scratch, size = None, 0, 0
+        if dweight is not None:
+            keep, scratch, size = _scratch(_need("rms_norm_backward_workspace", rows, n), workspace, device,
+                                           "rms_norm_backward")
+        a = _lib.pack["rms_norm_backward"](
+            p, ld, *inputs, _vector(weight, "weight", _F32, device, n), _vector(rstd, "rstd", _F32, device, rows),
+            *((0, 0) if add is None else _rows(add, "add", dtype, device, shape)), *_rows(dx, "dx", dtype, device, shape),
+            0 if dweight is None else _vector(dweight, "dweight", _F32, device, n), scratch, size)
+        status = _lib.load().rms_norm_backward(a, rows, n, code, stream)
+    if status:
+        _check(status, "rms_norm_backward")
+    return dx, dweight
+
+
+def rms_norm_backward_workspace(rows: int, n: int) -> int:
+    """Bytes of workspace that ``rms_norm_backward`` needs for dweight."""
+    return _need("rms_norm_backward_workspace", rows, n)
+
+
+def linear_fp8_forward(x, w, y, *, bias=None, activation="none", residual=None, checkpoint=None, workspace=None):
+    """y = act(x w^T + bias) + residual, with x (tokens, d_in) and w (d_out, d_in) as (codes, scales) in 8-bit floating point.
+
+    bias, residual and y are of one storage type.  ``checkpoint``, of the pre-activation, is written if given.  ``y`` may be
+    ``residual``.  ``workspace``: ``linear_fp8_forward_workspace(...)`` bytes, allocated if not given.
+    """
+    status = None
+    act = ACTIVATIONS.get(activation)
+    if y.is_cuda and act is not None:
+        device = _current_device()
+        codes, scales = _NONE if checkpoint is None else checkpoint
+        status = _lib.binding().linear_fp8_forward(*x, *w, bias, residual, y, codes, scales, act, workspace, device,
+                                                   _raw_stream(device))
+    if status is None:
+        p, ld, shape, dtype, code, device, stream = _first(y, "y")
+        tokens, d_out = shape
+        d_in = w[0].shape[-1]
+        act = _activation(activation)
+        keep, scratch, size = _scratch(_need("linear_fp8_forward_workspace", d_in, d_out, tokens, code), workspace, device,
+                                       "linear_fp8_forward")
+        a = _lib.pack["linear_fp8_forward"](
+            *_held8(x, device, tokens, d_in, "x"), *_held8(w, device, d_out, d_in, "w"),
+            0 if bias is None else _vector(bias, "bias", dtype, device, d_out),
+            *((0, 0) if residual is None else _rows(residual, "residual", dtype, device, shape)), p, ld,
+            *((0, 0) if checkpoint is None else _held(checkpoint, device, tokens, d_out)), scratch, size)
+        status = _lib.load().linear_fp8_forward(a, d_in, d_out, tokens, act, code, stream)
+    if status:
+        _check(status, "linear_fp8_forward")
+    return y
+
+
+def linear_fp8_forward_workspace(d_in: int, d_out: int, tokens: int, dtype: torch.dtype) -> int:
+    """Bytes of workspace that ``linear_fp8_forward`` needs (0: none)."""
+    return _need("linear_fp8_forward_workspace", d_in, d_out, tokens, _CODES[dtype])
+
+
+def linear_fp8_backward(dy, x, w, *, dx=None, dw=None, db=None, activation="none", checkpoint=None, add=None,
+                        workspace=None):
+    """Writes those of dx = dz w (+ add), dw = dz^T x and db = sum of dz that are given, dz = dy act'(z) in 8 bits.
+
+    ``x`` (d_in, tokens) and ``w`` (d_in, d_out) are what ``fp8_quantize`` leaves in ``columns`` of x and W; ``x`` may be None
+    without dw, ``w`` without dx.  z is what ``checkpoint`` stands for (not needed without an activation; relu's slope at a
+    positive value that its block holds as zero is 0, as in ``linear_backward``).  ``dx`` may be ``add``.
+    ``workspace``: ``linear_fp8_backward_workspace(...)`` bytes, allocated if not given.
+    """
+    status = None
+    act = ACTIVATIONS.get(activation)
+    if dy.is_cuda and act is not None:
+        device = _current_device()
+        codes, scales = _NONE if checkpoint is None else checkpoint
+        status = _lib.binding().linear_fp8_backward(dy, *(_NONE if x is None else x), *(_NONE if w is None else w), dx, dw, db,
+                                                    add, codes, scales, act, workspace, device, _raw_stream(device))
+    if status is None:
+        p, ld, shape, dtype, code, device, stream = _first(dy, "dy")
+        tokens, d_out = shape
+        act = _activation(activation)
+        d_in = 1  # (db alone)
+        if dx is not None:
+            if w is None:
+                raise ValueError("dx needs w")
+            d_in = dx.shape[-1]
+        if dw is not None:
+            if x is None:
+                raise ValueError("dw needs x")
+            if dx is not None and dw.shape[-1] != d_in:
+                raise ValueError(f"dx and dw have {d_in} and {dw.shape[-1]} columns")
+            d_in = dw.shape[-1]
+        held = (0, 0)
+        if act != _lib.RDFFT_ACT_NONE:
+            if checkpoint is None:
+                raise ValueError(f"the gradient through {activation} needs the checkpoint of the pre-activation")
+            held = _held(checkpoint, device, tokens, d_out)
+        none, none8 = (0, 0), (0, 0, 0, 0, 0)
+        keep, scratch, size = _scratch(
+            _need("linear_fp8_backward_workspace", d_in, d_out, tokens, dx is not None, dw is not None, db is not None, code),
+            workspace, device, "linear_fp8_backward")
+        a = _lib.pack["linear_fp8_backward"](
+            p, ld, *held,
+            *(none8 if dw is None else _held8(x, device, d_in, tokens, "x")),
+            *(none8 if dx is None else _held8(w, device, d_in, d_out, "w")),
+            *(none if dx is None or add is None else _rows(add, "add", dtype, device, (tokens, d_in))),
+            *(none if dx is None else _rows(dx, "dx", dtype, device, (tokens, d_in))),
+            *(none if dw is None else _rows(dw, "dw", dtype, device, (d_out, d_in))),
+            0 if db is None else _vector(db, "db", dtype, device, d_out), scratch, size)
+        status = _lib.load().linear_fp8_backward(a, d_in, d_out, tokens, act, code, stream)
+    if status:
+        _check(status, "linear_fp8_backward")
+    return dx, dw, db
+
+
+def linear_fp8_backward_workspace(d_in: int, d_out: int, tokens: int, dtype: torch.dtype, *, dx: bool = True, dw: bool = True,
+                                  db: bool = True) -> int:
+    """Bytes of workspace that ``linear_fp8_backward`` needs for the gradients that are wanted."""
+    return _need("linear_fp8_backward_workspace", d_in, d_out, tokens, dx, dw, db, _CODES[dtype])
+
+
 def rdfft_init() -> None:
     _check(_lib.load().rdfft_init(), "rdfft_init")
 

@@ -21,7 +21,7 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "librdfft.so")
 
-SOURCES = ["bca_block_bf16.hip", "bca_block_f16.hip", "bca_block_f32.hip", "bca_store_bf16.hip", "bca_store_f16.hip", "bca_store_f32.hip", "rdfft_kernels.hip", "rdfft_hc_kernels.hip", "bca_kernels.hip", "bca_multipass.hip", "layout_kernels.hip", "mixed_kernels.hip", "act8_kernels.hip", "norm_kernels.hip", "linear_bf16.hip", "linear_f16.hip", "linear_f32.hip", "linear.hip", "capi.cpp", "capi_dense.cpp", "twiddles.cpp"]
+SOURCES = ["bca_block_bf16.hip", "bca_block_f16.hip", "bca_block_f32.hip", "bca_store_bf16.hip", "bca_store_f16.hip", "bca_store_f32.hip", "rdfft_kernels.hip", "rdfft_hc_kernels.hip", "bca_kernels.hip", "bca_multipass.hip", "layout_kernels.hip", "mixed_kernels.hip", "act8_kernels.hip", "norm_kernels.hip", "linear_bf16.hip", "linear_f16.hip", "linear_f32.hip", "linear.hip", "fp8_kernels.hip", "rms_norm_kernels.hip", "linear_fp8_bf16.hip", "linear_fp8_f16.hip", "linear_fp8_f32.hip", "linear_fp8.hip", "capi.cpp", "capi_dense.cpp", "twiddles.cpp"]
 
 BINDING = os.path.join(PKG, "_binding.so")
 

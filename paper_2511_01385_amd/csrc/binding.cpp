@@ -97,6 +97,29 @@ struct Call {
     if (s.dim() != 2 || s.size(0) != r || s.size(1) != (n + 31) / 32 || !s.is_contiguous()) throw NotPlain{};
     return {static_cast<int8_t*>(c.data_ptr()), static_cast<uint8_t*>(s.data_ptr())};
   }
+  // (rows, n) in 8-bit floating point: codes at i and scales at i + 1, by rows or in tiles
+  fp8_t held8(Py_ssize_t i, int64_t r, int64_t n) const {
+    if (!has(i)) {
+      if (has(i + 1)) throw NotPlain{};
+      return fp8_t{};
+    }
+    const at::Tensor &c = tensor(i, at::kFloat8_e4m3fn), &s = tensor(i + 1, at::kByte);
+    const int64_t blocks = (n + 127) / 128, bands = (r + 127) / 128;
+    if (c.dim() != 2 || c.size(0) != r || c.size(1) != n || s.dim() != 2 || s.size(1) != blocks) throw NotPlain{};
+    if (s.size(0) != r && s.size(0) != bands) throw NotPlain{};
+    for (const at::Tensor* t : {&c, &s})
+      if ((t->stride(1) != 1 && t->size(1) > 1) || (t->stride(0) < t->size(1) && t->size(0) > 1)) throw NotPlain{};
+    return {static_cast<uint8_t*>(c.data_ptr()), std::max(c.stride(0), n), static_cast<uint8_t*>(s.data_ptr()),
+            std::max(s.stride(0), blocks), s.size(0) == r ? 1 : 128};
+  }
+  // (rows, columns) of a matrix in 8-bit floating point
+  void size8(Py_ssize_t i, int64_t* rows, int64_t* n) const {
+    if (!THPVariable_Check(args[i])) throw NotPlain{};
+    const at::Tensor& t = THPVariable_Unpack(args[i]);
+    if (t.dim() != 2) throw NotPlain{};
+    *rows = t.size(0);
+    *n = t.size(1);
+  }
   // a workspace of `need` bytes: the caller's at i, or one allocated here; `keep` holds it until the call is made
   void workspace(Py_ssize_t i, int64_t need, at::Tensor* keep, void** p, int64_t* bytes) const {
     *p = nullptr;
@@ -272,6 +295,135 @@ PyObject* product_backward(PyObject*, PyObject* const* args, Py_ssize_t given) {
   });
 }
 
+// x codes scales column_codes column_scales
+PyObject* quantize8(PyObject*, PyObject* const* args, Py_ssize_t given) {
+  return guarded([&] {
+    Call c(args, given, 7);
+    int64_t rows, n, ld;
+    void* x;
+    c.first(0, &rows, &n);
+    c.rows(0, rows, n, &x, &ld);
+    const fp8_t held = c.held8(1, rows, n), columns = c.held8(3, n, rows);
+    return unlocked([&] {
+      return fp8_quantize(x, ld, held.codes ? &held : nullptr, columns.codes ? &columns : nullptr, rows, n, c.code, c.stream);
+    });
+  });
+}
+
+// codes scales out
+PyObject* dequantize8(PyObject*, PyObject* const* args, Py_ssize_t given) {
+  return guarded([&] {
+    Call c(args, given, 5);
+    int64_t rows, n, ld;
+    void* out;
+    c.first(2, &rows, &n);
+    c.needs({0, 1});
+    c.rows(2, rows, n, &out, &ld);
+    const fp8_t from = c.held8(0, rows, n);
+    return unlocked([&] { return fp8_dequantize(&from, out, ld, rows, n, c.code, c.stream); });
+  });
+}
+
+// x residual weight y summed rstd codes scales codes8 scales8 eps
+PyObject* rms_forward(PyObject*, PyObject* const* args, Py_ssize_t given) {
+  return guarded([&] {
+    Call c(args, given, 13);
+    int64_t rows, n;
+    c.first(0, &rows, &n);
+    c.needs({2});
+    rms_norm_forward_t a{};
+    c.rows(0, rows, n, &a.x, &a.ldx);
+    c.rows(1, rows, n, &a.residual, &a.ldr);
+    a.weight = c.floats(2, n);
+    c.rows(3, rows, n, &a.y, &a.ldy);
+    c.rows(4, rows, n, &a.summed, &a.lds);
+    a.rstd = c.floats(5, rows);
+    a.checkpoint = c.held(6, rows, n);
+    a.y8 = c.held8(8, rows, n);
+    const float eps = (float)c.number(10);
+    return unlocked([&] { return rms_norm_forward(&a, rows, n, eps, c.code, c.stream); });
+  });
+}
+
+// dy u codes scales weight rstd add dx dweight workspace
+PyObject* rms_backward(PyObject*, PyObject* const* args, Py_ssize_t given) {
+  return guarded([&] {
+    Call c(args, given, 12);
+    int64_t rows, n;
+    c.first(0, &rows, &n);
+    c.needs({4, 5, 7});
+    rms_norm_backward_t a{};
+    c.rows(0, rows, n, &a.dy, &a.ldg);
+    c.rows(1, rows, n, &a.u, &a.ldu);
+    a.checkpoint = c.held(2, rows, n);
+    a.weight = c.floats(4, n);
+    a.rstd = c.floats(5, rows);
+    c.rows(6, rows, n, &a.add, &a.lda);
+    c.rows(7, rows, n, &a.dx, &a.ldd);
+    a.dweight = c.floats(8, n);
+    at::Tensor keep;
+    if (c.has(8)) c.workspace(9, rms_norm_backward_workspace(rows, n), &keep, &a.workspace, &a.workspace_bytes);
+    return unlocked([&] { return rms_norm_backward(&a, rows, n, c.code, c.stream); });
+  });
+}
+
+// x_codes x_scales w_codes w_scales bias residual y codes scales act workspace
+PyObject* product8_forward(PyObject*, PyObject* const* args, Py_ssize_t given) {
+  return guarded([&] {
+    Call c(args, given, 13);
+    int64_t tokens, d_in, d_out;
+    c.needs({0, 2, 6});
+    c.first(6, &tokens, &d_out);
+    c.size8(2, &d_out, &d_in);
+    const auto act = (rdfft_activation_t)c.integer(9);
+    linear_fp8_forward_t a{};
+    a.x = c.held8(0, tokens, d_in);
+    a.w = c.held8(2, d_out, d_in);
+    a.bias = c.vector(4, c.type, d_out);
+    c.rows(5, tokens, d_out, &a.residual, &a.ldr);
+    c.rows(6, tokens, d_out, &a.y, &a.ldy);
+    a.checkpoint = c.held(7, tokens, d_out);
+    at::Tensor keep;
+    c.workspace(10, linear_fp8_forward_workspace(d_in, d_out, tokens, c.code), &keep, &a.workspace, &a.workspace_bytes);
+    return unlocked([&] { return linear_fp8_forward(&a, d_in, d_out, tokens, act, c.code, c.stream); });
+  });
+}
+
+// dy x_codes x_scales w_codes w_scales dx dw db add codes scales act workspace
+PyObject* product8_backward(PyObject*, PyObject* const* args, Py_ssize_t given) {
+  return guarded([&] {
+    Call c(args, given, 15);
+    int64_t tokens, d_in = 1, d_out, other;
+    const bool dx = c.has(5), dw = c.has(6), db = c.has(7);
+    if (dx) c.first(5, &other, &d_in);
+    if (dw) c.first(6, &other, &d_in);
+    c.first(0, &tokens, &d_out);
+    const auto act = (rdfft_activation_t)c.integer(11);
+    linear_fp8_backward_t a{};
+    c.rows(0, tokens, d_out, &a.dy, &a.ldg);
+    if (dw) {
+      c.needs({1});
+      a.x = c.held8(1, d_in, tokens);
+      c.rows(6, d_out, d_in, &a.dw, &a.lddw);
+    }
+    if (dx) {
+      c.needs({3});
+      a.w = c.held8(3, d_in, d_out);
+      c.rows(5, tokens, d_in, &a.dx, &a.ldd);
+      c.rows(8, tokens, d_in, &a.add, &a.lda);
+    }
+    a.db = c.vector(7, c.type, d_out);
+    if (act != RDFFT_ACT_NONE) {
+      c.needs({9, 10});
+      a.checkpoint = c.held(9, tokens, d_out);
+    }
+    at::Tensor keep;
+    c.workspace(12, linear_fp8_backward_workspace(d_in, d_out, tokens, dx, dw, db, c.code), &keep, &a.workspace,
+                &a.workspace_bytes);
+    return unlocked([&] { return linear_fp8_backward(&a, d_in, d_out, tokens, act, c.code, c.stream); });
+  });
+}
+
 #define FAST(name, fn) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fn)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST("act8_quantize", quantize),
                          FAST("act8_dequantize", dequantize),
@@ -279,6 +431,12 @@ PyMethodDef methods[] = {FAST("act8_quantize", quantize),
                          FAST("layer_norm_backward", norm_backward),
                          FAST("linear_forward", product_forward),
                          FAST("linear_backward", product_backward),
+                         FAST("fp8_quantize", quantize8),
+                         FAST("fp8_dequantize", dequantize8),
+                         FAST("rms_norm_forward", rms_forward),
+                         FAST("rms_norm_backward", rms_backward),
+                         FAST("linear_fp8_forward", product8_forward),
+                         FAST("linear_fp8_backward", product8_backward),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

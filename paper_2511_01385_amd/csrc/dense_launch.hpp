@@ -89,6 +89,9 @@ struct GemmArgs {
   int64_t k_split;
   int tiles_m, tiles_n;
 };
+// D from the float32 sums of a product whose k was split (linear.hip), with its epilogue
+hipError_t launch_linear_join(GemmArgs g, int storage, hipStream_t stream);
+
 // the instances for one storage type; null where one is not built.  Last index: 1 where
 // both operands' memory rows hold whole chunks of 16 bytes, at addresses that can be loaded straight to LDS
 enum LinearTile { kTile32x64, kTile64, kTile128, kTile128x256, kTile256, kLinearTiles };

@@ -34,8 +34,7 @@ __global__ void __launch_bounds__(kJoinWG) linear_join_kernel(GemmArgs g, const 
   finish_group<E>(g, m, n, bias, z);
 }
 
-template <class E>
-static hipError_t join(GemmArgs g, hipStream_t stream) {
+hipError_t launch_linear_join(GemmArgs g, int storage, hipStream_t stream) {
   const float* const partial = g.partial;
   g.partial = nullptr;
   int lanes = kCkLanes;
@@ -45,8 +44,11 @@ static hipError_t join(GemmArgs g, hipStream_t stream) {
   constexpr int64_t kMaxY = 65535;
   const int64_t gy = (g.m + per - 1) / per;
   if (gy > kMaxY) return hipErrorInvalidValue;  // (a product of so many rows is never split)
-  hipLaunchKernelGGL(linear_join_kernel<E>, dim3((unsigned)gx, (unsigned)gy), dim3(kJoinWG), 0, stream, g, partial, lanes);
-  return hipGetLastError();
+  return with_elem(storage, [&](auto e) {
+    hipLaunchKernelGGL(linear_join_kernel<decltype(e)>, dim3((unsigned)gx, (unsigned)gy), dim3(kJoinWG), 0, stream, g, partial,
+                       lanes);
+    return hipGetLastError();
+  });
 }
 
 // ----------------------------------------------------------------------------------
@@ -254,7 +256,7 @@ static hipError_t product(GemmArgs& g, int64_t a_len, LinearOperands kind, int s
   g.partial = p.splits > 1 ? static_cast<float*>(workspace) : nullptr;
   const hipError_t e = t.fn[p.tile][kind][direct](g, stream);
   if (e != hipSuccess || g.partial == nullptr) return e;
-  return with_elem(storage, [&](auto elem) { return join<decltype(elem)>(g, stream); });
+  return launch_linear_join(g, storage, stream);
 }
 
 // Which tile dW and dx share in one launch, or kLinearTiles where two launches cost less.  The product with the longer k

@@ -1,0 +1,195 @@
+// linear_fp8.hip -- the dense product of operands in 8-bit floating point and its gradients: which kernel of
+// linear_fp8_kernels.hpp runs, in how many parts, and the order of a backward's passes.
+//
+// All three products are one kernel, because each operand comes in blocks along its own k: y = x W^T takes the rows of
+// x and W, dx = dz W the rows of dz and the columns of W, dW = dz^T x the columns of dz and x.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "fp8_launch.hpp"
+
+namespace rdfft {
+
+// the plans count on this many CUs, so that a workspace's size follows from the sizes of a call alone
+constexpr int64_t kCUs = 256;
+constexpr int64_t kStage = 128;  // k to a stage
+
+// What a tile costs, in us: a stage where a CU has one workgroup of them, a stage of each where it has more
+// (`together` fit), and what comes before and after.
+struct TileCost {
+  int bm, bn, together;
+  double alone, each, ends;
+};
+constexpr TileCost kCost[kLinear8Tiles] = {{32, 64, 4, 0.19, 0.14, 3.4},
+                                           {64, 64, 3, 0.235, 0.175, 3.6},
+                                           {128, 128, 2, 0.50, 0.445, 4.0},
+                                           {128, 256, 1, 0.82, 0.82, 4.8},
+                                           {256, 256, 1, 1.30, 1.30, 13.0}};
+
+static const Linear8Table& table_of(int storage) {
+  static const Linear8Table tables[] = {linear_fp8_table_f32(), linear_fp8_table_bf16(), linear_fp8_table_f16()};
+  return tables[storage];
+}
+
+struct Plan {
+  Linear8Tile tile;
+  int64_t splits, k_split;
+  double cost;
+};
+
+// The tile and the number of k ranges that cost least.  The join of s ranges costs a launch (4 us) and 8 s bytes a
+// result, at 4 TB/s.
+static Plan plan_of(int64_t m, int64_t n, int64_t k, int storage) {
+  const int64_t stages = std::max<int64_t>(1, (k + kStage - 1) / kStage);
+  Plan best{kTile8_64, 1, stages * kStage, 0};
+  for (int t = 0; t < kLinear8Tiles; ++t) {
+    if (storage == kStorageF32 && t > kTile8_128) continue;  // (not built)
+    const TileCost& c = kCost[t];
+    const int64_t tiles = ((m + c.bm - 1) / c.bm) * ((n + c.bn - 1) / c.bn);
+    for (int64_t want = 1; want <= 16; ++want) {
+      const int64_t each = (stages + want - 1) / want, splits = (stages + each - 1) / each;
+      if (splits != want) continue;  // (as many ranges of another length)
+      if (splits > 1 && (each < 2 || tiles * splits > 4 * kCUs)) break;
+      const int64_t per_cu = std::max<int64_t>(1, (tiles * splits + kCUs - 1) / kCUs);
+      const double stage = per_cu == 1 ? c.alone : c.each * (double)per_cu;
+      double cost = (double)each * stage + c.ends * (double)((per_cu + c.together - 1) / c.together);
+      if (splits > 1) cost += 4.0 + 8.0 * (double)splits * (double)m * (double)n / 4e6;
+      if (best.cost == 0 || cost < best.cost) best = {(Linear8Tile)t, splits, each * kStage, cost};
+    }
+  }
+  return best;
+}
+static int64_t split_bytes(int64_t m, int64_t n, int64_t k, int storage) {
+  if (m <= kFewTokens) return 0;
+  const Plan p = plan_of(m, n, k, storage);
+  return p.splits > 1 ? p.splits * m * n * 4 : 0;
+}
+
+static hipError_t product(Gemm8Args& args, int storage, void* workspace, hipStream_t stream) {
+  GemmArgs& g = args.g;
+  const Linear8Table& t = table_of(storage);
+  g.splits = 1;
+  if (g.m <= kFewTokens) {
+    // 32 rows of B to a workgroup where that still fills the chip, or a checkpoint's blocks ask for it
+    const bool wide = g.ck.codes != nullptr || g.n >= 32 * kCUs;
+    return t.few[g.m <= 16 ? 0 : g.m <= 32 ? 1 : 2][wide](args, stream);
+  }
+  const Plan p = plan_of(g.m, g.n, g.k, storage);
+  g.splits = (int)p.splits;
+  g.k_split = p.k_split;
+  g.partial = p.splits > 1 ? static_cast<float*>(workspace) : nullptr;
+  const hipError_t e = t.fn[p.tile](args, stream);
+  return e != hipSuccess || g.partial == nullptr ? e : launch_linear_join(g, storage, stream);
+}
+
+int64_t linear_fp8_forward_workspace(const LinearSizes& s) { return split_bytes(s.tokens, s.d_out, s.d_in, s.storage); }
+
+hipError_t launch_linear_fp8_forward(const LinearFp8Forward& a, hipStream_t stream) {
+  Gemm8Args p{};
+  p.a = a.x;
+  p.b = a.w;
+  p.g.m = a.s.tokens;
+  p.g.n = a.s.d_out;
+  p.g.k = a.s.d_in;
+  p.g.d = a.y;
+  p.g.ldd = a.ldy;
+  p.g.bias = a.bias;
+  p.g.residual = a.residual;
+  p.g.ldr = a.ldr;
+  p.g.ck = a.ck;
+  p.g.act = a.s.act;
+  return product(p, a.s.storage, a.workspace, stream);
+}
+
+// ----------------------------------------------------------------------------------
+// the backward's workspace: dz by rows, dz by columns, then the partial sums of whichever pass runs (they follow
+// each other on the stream)
+static int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+struct BackwardSpace {
+  Fp8Operand rows, columns;
+  char* parts;
+  int64_t bytes;  // before the parts
+};
+static BackwardSpace space_of(const LinearSizes& s, bool dx, bool dw, void* workspace) {
+  char* p = static_cast<char*>(workspace);
+  BackwardSpace b{};
+  const auto take = [&](int64_t rows, int64_t n) {
+    Fp8Operand o;
+    o.ld = round_up(n, 16);
+    o.lds = round_up((n + kStage - 1) / kStage, 4);
+    o.codes = reinterpret_cast<uint8_t*>(p + b.bytes);
+    b.bytes += round_up(rows * o.ld, 256);
+    o.scales = reinterpret_cast<uint8_t*>(p + b.bytes);
+    b.bytes += round_up(rows * o.lds, 256);
+    return o;
+  };
+  if (dx) b.rows = take(s.tokens, s.d_out);
+  if (dw) b.columns = take(s.d_out, s.tokens);
+  b.parts = p + b.bytes;
+  return b;
+}
+
+int64_t linear_fp8_backward_workspace(const LinearSizes& s, bool dx, bool dw, bool db) {
+  int64_t parts = 0;
+  if (db) parts = std::max(parts, (s.tokens + kStage - 1) / kStage * s.d_out * 4);
+  if (dx) parts = std::max(parts, split_bytes(s.tokens, s.d_in, s.d_out, s.storage));
+  if (dw) parts = std::max(parts, split_bytes(s.d_out, s.d_in, s.tokens, s.storage));
+  return space_of(s, dx, dw, nullptr).bytes + parts;
+}
+
+hipError_t launch_linear_fp8_backward(const LinearFp8Backward& a, hipStream_t stream) {
+  const int64_t T = a.s.tokens, n = a.s.d_out;
+  const int storage = a.s.storage;
+  const bool dx = a.dx != nullptr && T > 0, dw = a.dw != nullptr;
+  const BackwardSpace space = space_of(a.s, a.dx != nullptr, dw, a.workspace);
+  hipError_t e = hipSuccess;
+  if (T > 0) {
+    Fp8Quantize q{};
+    q.x = a.dy;
+    q.ldx = a.ldg;
+    q.rows = T;
+    q.n = n;
+    if (dx) q.held = space.rows;
+    if (dw) q.columns = space.columns;
+    q.act = a.s.act;
+    q.ck = a.s.act == kActNone ? Checkpoint{} : a.ck;
+    q.sums = a.db == nullptr ? nullptr : reinterpret_cast<float*>(space.parts);
+    q.storage = storage;
+    e = launch_fp8_quantize(q, stream);
+    if (e != hipSuccess) return e;
+  }
+  if (a.db != nullptr) {
+    e = launch_column_finish(reinterpret_cast<const float*>(space.parts), (T + kStage - 1) / kStage, n, n, a.db, nullptr,
+                             storage, stream);
+    if (e != hipSuccess) return e;
+  }
+  if (dx) {
+    Gemm8Args p{};
+    p.a = space.rows;
+    p.b = a.w;
+    p.g.m = T;
+    p.g.n = a.s.d_in;
+    p.g.k = n;
+    p.g.d = a.dx;
+    p.g.ldd = a.ldd;
+    p.g.residual = a.add;
+    p.g.ldr = a.lda;
+    e = product(p, storage, space.parts, stream);
+  }
+  if (e == hipSuccess && dw) {
+    Gemm8Args p{};
+    p.a = space.columns;
+    p.b = a.x;
+    p.g.m = n;
+    p.g.n = a.s.d_in;
+    p.g.k = T;
+    p.g.d = a.dw;
+    p.g.ldd = a.lddw;
+    e = product(p, storage, space.parts, stream);
+  }
+  return e;
+}
+
+}  // namespace rdfft

@@ -23,61 +23,9 @@
 
 #include "dense_device.hpp"
 #include "dense_launch.hpp"
+#include "norm_device.hpp"
 
 namespace rdfft {
-
-// Sums of K values over the TPR threads of a group, in each of them.  Groups longer than a wave are a
-// workgroup's only ones or run in step; `red` holds [2][waves][K] and `turn` alternates.
-template <int TPR, int K>
-__device__ __forceinline__ void group_sums(float* v, float* red, int& turn) {
-#pragma unroll
-  for (int k = 0; k < K; ++k) v[k] = wave_sum(v[k]);
-  if constexpr (TPR > 64) {
-    const int waves = (int)blockDim.x / 64, wave = threadIdx.x / 64;
-    float* const r = red + turn * waves * K;
-    if ((threadIdx.x & 63) == 0) {
-#pragma unroll
-      for (int k = 0; k < K; ++k) r[wave * K + k] = v[k];
-    }
-    turn ^= 1;
-    __syncthreads();
-    const float* const mine = r + wave / (TPR / 64) * (TPR / 64) * K;
-#pragma unroll
-    for (int k = 0; k < K; ++k) v[k] = mine[k];
-#pragma unroll
-    for (int w = 1; w < TPR / 64; ++w)
-#pragma unroll
-      for (int k = 0; k < K; ++k) v[k] += mine[w * K + k];
-  }
-}
-
-// Eight values of a row from i0, zeros past its end.  EXACT: n is a multiple of eight, so a group is in the
-// row or out of it and its load needs no branch (an absent group's reads the row's start).
-template <class E, bool EXACT>
-struct RowGroup {
-  using T = typename E::T;
-  typename E::Raw raw;
-  __device__ __forceinline__ void load(const T* row, int i0, int n) {
-    if constexpr (EXACT) raw = E::load(row + (i0 < n ? i0 : 0));
-  }
-  __device__ __forceinline__ void widen(const T* row, int i0, int n, float* v) const {
-    if constexpr (EXACT) {
-      E::widen(raw, v);
-#pragma unroll
-      for (int k = 0; k < kVec; ++k) v[k] = i0 < n ? v[k] : 0.f;
-    } else {
-      read_group<E>(row, i0, n, v);
-    }
-  }
-};
-template <class E, bool EXACT>
-__device__ __forceinline__ void store_group(typename E::T* row, int i0, int n, const float* v) {
-  if constexpr (EXACT) {
-    if (i0 < n) E::store(row + i0, v);
-  } else {
-    write_group<E>(row, i0, n, v);
-  }
-}
 
 template <int TPR>
 constexpr int norm_fwd_wg() {
@@ -379,39 +327,6 @@ hipError_t launch_column_finish(const float* partials, int64_t groups, int64_t c
                        partials, groups, cols, n, static_cast<typename E::T*>(out0), static_cast<typename E::T*>(out1));
     return hipGetLastError();
   });
-}
-
-// fn(threads of a row, groups of eight per thread) by the row's length
-template <class F>
-static hipError_t with_row(int64_t n, F&& fn) {
-  using std::integral_constant;
-  const auto go = [&](auto tpr, auto c) { return fn(tpr, c); };
-  if (n <= 512) return go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
-  if (n <= 1024) return go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
-  if (n <= 2048) return go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
-  if (n <= 4096) return go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
-  if (n <= 8192) return go(integral_constant<int, 512>{}, integral_constant<int, 2>{});
-  return go(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
-}
-
-// the same for the backward, whose threads also hold sums
-template <class F>
-static hipError_t with_row_backward(int64_t n, F&& fn) {
-  using std::integral_constant;
-  const auto go = [&](auto tpr, auto c) { return fn(tpr, c); };
-  if (n <= 512) return go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
-  if (n <= 1024) return go(integral_constant<int, 128>{}, integral_constant<int, 1>{});
-  if (n <= 2048) return go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
-  if (n <= 4096) return go(integral_constant<int, 512>{}, integral_constant<int, 1>{});
-  if (n <= 8192) return go(integral_constant<int, 1024>{}, integral_constant<int, 1>{});
-  return go(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
-}
-
-// whether rows are loaded and stored in whole groups only
-static bool exact_rows(int64_t n) { return n % kVec == 0; }
-template <class F>
-static hipError_t with_exact(int64_t n, F&& fn) {
-  return exact_rows(n) ? fn(std::true_type{}) : fn(std::false_type{});
 }
 
 hipError_t launch_layer_norm_forward(const NormArgs& a, hipStream_t stream, int num_cu) {
