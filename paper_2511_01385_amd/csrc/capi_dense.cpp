@@ -79,7 +79,9 @@ bool fp8(const fp8_t& o, int64_t rows, int64_t n, Rows* codes, Rows* scales, rdf
   if (rows == 0 || n == 0) return true;
   if (!aligned16(o.codes) || reinterpret_cast<uintptr_t>(o.scales) % 4 != 0) return false;
   if ((rows > 1 && o.ld % 16 != 0) || (bands > 1 && o.lds % 4 != 0)) return false;
-  *out = {o.codes, codes->pitch, o.scales, scales->pitch, o.block_rows == 1 ? 0 : 7};
+  // (a single row's strides are such as a next row's would be)
+  *out = {o.codes, rows == 1 ? (n + 15) / 16 * 16 : codes->pitch, o.scales,
+          bands == 1 ? (blocks + 3) / 4 * 4 : scales->pitch, o.block_rows == 1 ? 0 : 7};
   return true;
 }
 

@@ -29,9 +29,55 @@ namespace rdfft {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-// codes as an operand's elements
+// codes as the fragments' elements
 struct ElemCode {
   using T = uint8_t;
+};
+
+// R rows of one operand's stage on their way to LDS, as Operand of linear_kernels.hpp loads them, in fewer registers:
+// a lane's part of line j lies 8 j rows below that of line 0, in the same chunk, and rows past the last are out of the
+// buffer's bounds.
+template <int R, int WAVES>
+struct CodeOperand {
+  static constexpr int BYTES = R * kStageBytes, LINES = BYTES / 1024 / WAVES;
+  static_assert(LINES * WAVES * 1024 == BYTES);
+  const uint8_t* base;  // row 0 and this stage's k 0 of the tile
+  uint32_t ld, offset;  // bytes from row to row; of this lane's part of line 0
+  uint32_t above;       // bytes of the rows that exist but for the last
+  int depth;            // k that is left
+  int chunk, wave;
+
+  __device__ __forceinline__ void init(const Fp8Operand& o, int64_t r0, int64_t r_end, int64_t k0, int64_t k_end, int wave_,
+                                       int lane) {
+    base = o.codes + r0 * o.ld + k0;
+    ld = (uint32_t)o.ld;
+    const int rows = (int)min(r_end - r0, (int64_t)R);
+    above = (uint32_t)(rows - 1) * ld;
+    depth = (int)(k_end - k0);
+    wave = wave_;
+    chunk = (lane & 7) ^ (lane >> 3);
+    offset = (uint32_t)(wave * LINES * 8 + lane / 8) * ld + (uint32_t)chunk * 16u;
+  }
+  // (a row's last chunk counts whole)
+  __device__ __forceinline__ int records() const { return (int)(above + ((uint32_t)depth + 15) / 16 * 16); }
+  // line j of a stage in front of the end of k; step() after the last
+  __device__ __forceinline__ void fetch_line(int j, uint32_t lds) const {
+    load_to_lds<16>(reinterpret_cast<const char*>(base), offset + (uint32_t)(8 * j) * ld, lds + (uint32_t)(wave * LINES + j) * 1024u,
+                    records());
+  }
+  __device__ __forceinline__ void step() {
+    base += kStageBytes;
+    depth -= kStageBytes;
+  }
+  // any stage: chunks past the end of k are zeros
+  __device__ __forceinline__ void fetch(uint32_t lds) {
+    const bool in = chunk * 16 < depth;
+#pragma unroll
+    for (int j = 0; j < LINES; ++j)
+      load_to_lds<16>(reinterpret_cast<const char*>(base), in ? offset + (uint32_t)(8 * j) * ld : kNowhere,
+                      lds + (uint32_t)(wave * LINES + j) * 1024u, records());
+    step();
+  }
 };
 
 // bytes 8q ... 8q+7 of a lane's 32 as bfloat16 values (exact)
@@ -82,19 +128,19 @@ __device__ __forceinline__ i32x8 join_chunks(u32x4 lo, u32x4 hi) {
 
 // Fragments of 32 rows at row0 + 32 f, half kk of a stage.
 struct Fragments32 {
-  uint32_t at[2][2];
+  uint32_t first;  // half 0's first chunk: the others' places differ in two bits
   __device__ __forceinline__ void init(int row0, int lane) {
-    const uint32_t first = (uint32_t)((row0 + (lane & 31)) * kStageBytes + ((lane >> 5) ^ (lane & 7)) * 16);
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-      for (int q = 0; q < 2; ++q) at[kk][q] = first ^ (uint32_t)(kk * 64 + q * 32);
+    first = (uint32_t)((row0 + (lane & 31)) * kStageBytes + ((lane >> 5) ^ (lane & 7)) * 16);
   }
   __device__ __forceinline__ i32x8 read(const char* lds, int f, int kk) const {
     const char* const p = lds + f * 32 * kStageBytes;
-    return join_chunks(*reinterpret_cast<const u32x4*>(p + at[kk][0]), *reinterpret_cast<const u32x4*>(p + at[kk][1]));
+    return join_chunks(*reinterpret_cast<const u32x4*>(p + (first ^ (uint32_t)(kk * 64))),
+                       *reinterpret_cast<const u32x4*>(p + (first ^ (uint32_t)(kk * 64 + 32))));
   }
 };
+
+// Keeps what is computed from v inside the loop that this stands in: else it would lie in registers all along.
+__device__ __forceinline__ void recompute(uint32_t& v) { asm volatile("" : "+v"(v)); }
 
 // Zeros in place of what follows the last `left` bytes of k in a stage's rows (left % 16 != 0; whole chunks past the
 // end are zeros already): what lies behind a row's end may be anything.
@@ -138,8 +184,9 @@ __device__ __forceinline__ void linear_fp8_tile(const Gemm8Args& args, int id) {
   constexpr bool WIDE = E::kId == kStorageF32;
   constexpr int WAVES = WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32;
   constexpr int BK = kStageBytes, STAGE = Tile::STAGE;
-  using OpA = Operand<ElemCode, BM, WAVES, false, kDirect>;
-  using OpB = Operand<ElemCode, BN, WAVES, false, kDirect>;
+  constexpr bool STREAM = FM >= 4 && !WIDE;  // fragments of A one at a time: two halves of a stage take too many registers
+  using OpA = CodeOperand<BM, WAVES>;
+  using OpB = CodeOperand<BN, WAVES>;
   extern __shared__ __attribute__((aligned(1024))) char linear_lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
   const int wm = wave / WN, wn = wave % WN;
@@ -149,8 +196,8 @@ __device__ __forceinline__ void linear_fp8_tile(const Gemm8Args& args, int id) {
 
   OpA a;
   OpB b;
-  a.init(args.a.codes, args.a.ld, m0, g.m, k0, k1, wave, lane);
-  b.init(args.b.codes, args.b.ld, n0, g.n, k0, k1, wave, lane);
+  a.init(args.a, m0, g.m, k0, k1, wave, lane);
+  b.init(args.b, n0, g.n, k0, k1, wave, lane);
   Fragments32 fa, fb;
   fa.init(wm * TM, lane);
   fb.init(wn * TN, lane);
@@ -263,7 +310,41 @@ __device__ __forceinline__ void linear_fp8_tile(const Gemm8Args& args, int id) {
     reads_wait();
     wave_barrier();
   };
-  Half h0, h1;
+  // One half's products with the other's reads and a stage's loads between them, a row of fragments at a time.
+  const auto weave = [&](const Half& h, Half& to, const char* from, int slot) {
+    constexpr int TOTAL = FM + FN;
+    const uint32_t la = lds0 + (uint32_t)slot * STAGE, lb = la + OpA::BYTES;
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+#pragma unroll
+      for (int e = i * EACH / FM; e < (i + 1) * EACH / FM; ++e) {
+        if (e < OpA::LINES) a.fetch_line(e, la);
+        else b.fetch_line(e - OpA::LINES, lb);
+      }
+#pragma unroll
+      for (int e = i * TOTAL / FM; e < (i + 1) * TOTAL / FM; ++e) {
+        if (e < FN) to.b[e] = fb.read(from + OpA::BYTES, e, 0);
+        else to.a[e - FN] = fa.read(from, e - FN, 0);
+      }
+#pragma unroll
+      for (int j = 0; j < FN; ++j) {
+        if constexpr (WIDE) block[i][j] = product32_wide(h.b[j], h.a[i], block[i][j]);
+        else acc[i][j] = product32(h.b[j], h.a[i], acc[i][j], sb[j][0], sa[i]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    a.step();
+    b.step();
+  };
+  constexpr int PRODUCTS = FM * FN * (WIDE ? 4 : 1), READS = 2 * (FM + FN);
+  const auto interleave = [&] {
+    constexpr int GROUPS = READS < PRODUCTS ? READS : PRODUCTS;
+#pragma unroll
+    for (int q = 0; q < GROUPS; ++q) {
+      __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS / GROUPS, 0);  // matrix instructions
+      __builtin_amdgcn_sched_group_barrier(0x100, READS / GROUPS, 0);    // LDS reads
+    }
+  };
   if (steps > 0) {
     // (older than the stages, so that the waits for those cover them)
     fetch_group(s0 >> 2);
@@ -278,26 +359,106 @@ __device__ __forceinline__ void linear_fp8_tile(const Gemm8Args& args, int id) {
     if (steps == 1) cut(0);
     take_group(s0 >> 2);
     shift_scales((s0 & 3) * 8);
-    read(h0, linear_lds, 0);
   }
   int cur = 0, t = 0;
   const auto next = [](int slot) { return slot + 1 == STAGES ? 0 : slot + 1; };
-  for (; t < steps; ++t) {
-    scales_of(t);
-    read(h1, linear_lds + cur * STAGE, 1);
-    clear_block();
-    multiply(h0);
-    if (t + 1 < steps) {
-      // this stage is read; the next has landed when those after it are all that is left
-      if (STAGES > 2 && t + STAGES - 1 < steps) stage_wait<(STAGES - 2) * EACH>();
-      else stage_wait<0>();
-      if (t + STAGES < steps) fetch(cur);
+  const int steady = steps - 1 - STAGES;  // (the stage that is fetched is not the last)
+  if constexpr (STREAM) {
+    // Fragments of A come one at a time, AHEAD steps before their products, into a ring; those of B half a stage
+    // before.  The barrier comes when the stage's last fragment is read, AHEAD steps before its end.
+    constexpr int STEPS = 2 * FM, AHEAD = 3, RING = 4, LAST = STEPS - AHEAD;
+    static_assert(STEPS % RING == 0 && FN <= AHEAD && FN <= LAST);
+    i32x8 ring[RING], hb[2][FN];
+    const auto stage = [&](auto is_steady) {
+      constexpr bool STEADY = decltype(is_steady)::value;
+      const char* const here = linear_lds + cur * STAGE;
+      const char* const there = linear_lds + next(cur) * STAGE;
+      const uint32_t la = lds0 + (uint32_t)cur * STAGE, lb = la + OpA::BYTES;
+      recompute(a.offset);
+      recompute(b.offset);
+      recompute(fa.first);
+      recompute(fb.first);
+      scales_of(t);
+      const bool more = STEADY || t + 1 < steps;
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) {
+        if (s == LAST) {
+          if constexpr (STEADY) {
+            stage_wait<(STAGES - 2) * EACH>();
+          } else if (more) {
+            stage_wait<0>();
+            if (t + STAGES < steps) fetch(cur);
+            if (t + 2 == steps) cut(next(cur));
+          }
+        }
+        if constexpr (STEADY) {
+          if (s >= LAST) {
+#pragma unroll
+            for (int e = (s - LAST) * EACH / AHEAD; e < (s - LAST + 1) * EACH / AHEAD; ++e) {
+              if (e < OpA::LINES) a.fetch_line(e, la);
+              else b.fetch_line(e - OpA::LINES, lb);
+            }
+          }
+        }
+        const int to = s + AHEAD;
+        if (s < FN) hb[1][s] = fb.read(here + OpA::BYTES, s, 1);
+        if (s < LAST) {
+          ring[to % RING] = fa.read(here, to % FM, to / FM);
+        } else if (more) {
+          if (s - LAST < FN) hb[0][s - LAST] = fb.read(there + OpA::BYTES, s - LAST, 0);
+          ring[to % RING] = fa.read(there, (to - STEPS) % FM, (to - STEPS) / FM);
+        }
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+          acc[s % FM][j] = product32(hb[s / FM][j], ring[s % RING], acc[s % FM][j], sb[j][0], sa[s % FM]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if constexpr (STEADY) {
+        a.step();
+        b.step();
+      }
       cur = next(cur);
-      if (t + 2 == steps) cut(cur);
-      read(h0, linear_lds + cur * STAGE, 0);
+    };
+    if (steps > 0) {
+#pragma unroll
+      for (int j = 0; j < FN; ++j) hb[0][j] = fb.read(linear_lds + OpA::BYTES, j, 0);
+#pragma unroll
+      for (int s = 0; s < AHEAD; ++s) ring[s] = fa.read(linear_lds, s % FM, s / FM);
     }
-    multiply(h1);
-    add_block();
+    for (; t < steady; ++t) stage(std::true_type{});
+#pragma unroll 1
+    for (; t < steps; ++t) stage(std::false_type{});
+  } else {
+    Half h0, h1;
+    if (steps > 0) read(h0, linear_lds, 0);
+    for (; t < steady; ++t) {
+      scales_of(t);
+      clear_block();
+      read(h1, linear_lds + cur * STAGE, 1);
+      multiply(h0);
+      interleave();
+      stage_wait<(STAGES - 2) * EACH>();
+      weave(h1, h0, linear_lds + next(cur) * STAGE, cur);
+      add_block();
+      cur = next(cur);
+    }
+    for (; t < steps; ++t) {
+      scales_of(t);
+      read(h1, linear_lds + cur * STAGE, 1);
+      clear_block();
+      multiply(h0);
+      if (t + 1 < steps) {
+        // this stage is read; the next has landed when those after it are all that is left
+        if (STAGES > 2 && t + STAGES - 1 < steps) stage_wait<(STAGES - 2) * EACH>();
+        else stage_wait<0>();
+        if (t + STAGES < steps) fetch(cur);
+        cur = next(cur);
+        if (t + 2 == steps) cut(cur);
+        read(h0, linear_lds + cur * STAGE, 0);
+      }
+      multiply(h1);
+      add_block();
+    }
   }
   stage_wait<0>();
 
@@ -392,10 +553,10 @@ __global__ void __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu
   const int64_t stages = (g.k + BK - 1) / BK, per = (stages + WAVES - 1) / WAVES * BK;
   const int64_t k0 = min(wave * per, g.k), k1 = min(k0 + per, g.k);
 
-  Operand<ElemCode, 16 * NT, 1, false, kDirect> w;
-  Operand<ElemCode, 16 * MT, 1, false, kDirect> x;
-  w.init(args.b.codes, args.b.ld, n0, g.n, k0, k1, 0, lane);
-  x.init(args.a.codes, args.a.ld, 0, g.m, k0, k1, 0, lane);
+  CodeOperand<16 * NT, 1> w;
+  CodeOperand<16 * MT, 1> x;
+  w.init(args.b, n0, g.n, k0, k1, 0, lane);
+  x.init(args.a, 0, g.m, k0, k1, 0, lane);
   Fragments<ElemCode, 16, false> f;
   f.init(0, lane);
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mine;

@@ -145,21 +145,21 @@ __device__ __forceinline__ void times_slope8(int act, const float* z, float* g) 
 constexpr int kStageBytes = 128;  // of k, per row and stage
 
 // Loads that go straight to LDS: 64 lanes of 16 bytes (or four) from `base` + their offset to consecutive
-// LDS bytes from `lds`.  A lane whose offset is kNowhere stores zeros.  They are written as assembly
+// LDS bytes from `lds`.  A lane whose offset is not under `records`, such as kNowhere, stores zeros.  They are written as assembly
 // because the compiler, which cannot tell the stages apart, would wait for them before each LDS
 // read; stage_wait() and loads_wait() are the waits.  (No register receives anything.)
 constexpr uint32_t kNowhere = 0x80000000u;
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
 template <int BYTES = 16>
-__device__ __forceinline__ void load_to_lds(const char* base, uint32_t offset, uint32_t lds) {
+__device__ __forceinline__ void load_to_lds(const char* base, uint32_t offset, uint32_t lds, int records = (int)(kNowhere - 1)) {
   // (base and lds are the same in all lanes, which the compiler does not always see)
   const uint64_t p = reinterpret_cast<uint64_t>(base);
   const uint64_t u = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(p >> 32)) << 32 |
                      (uint32_t)__builtin_amdgcn_readfirstlane((int)p);
   lds = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds);
   const __amdgpu_buffer_rsrc_t r =
-      __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<char*>(u), 0, (int)(kNowhere - 1), 0x00020000);
+      __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<char*>(u), 0, records, 0x00020000);
   if constexpr (BYTES == 16)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(r)
                  : "memory", "m0");
