@@ -44,6 +44,13 @@ __device__ __forceinline__ Bytes8 fp8_encode(const float* v, int s) {
   return r;
 }
 
+// Four codes; NaN for `inverse`: of a block that is not finite.
+__device__ __forceinline__ uint32_t fp8_word(float a, float b, float c, float d, float inverse) {
+  const int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * inverse, b * inverse, 0, false);
+  const uint32_t r = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c * inverse, d * inverse, w, true);
+  return inverse != inverse ? kFp8NaNs : r;
+}
+
 // Eight values.  Of a value within 1/32 of the type's largest number M the code can stand for the power of two past M: it
 // stands for +-M, so what was finite comes back finite (Elem*::kMost, kPast).
 template <class E>

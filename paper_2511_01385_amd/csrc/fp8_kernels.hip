@@ -4,9 +4,10 @@
 // of the transpose) for dW = dz^T x, a weight both ways.  One pass reads the matrix and leaves whichever are
 // wanted; in a backward pass it also takes dy through the activation's slope and sums dz over the rows.
 //
-// A workgroup holds a tile of 128 x 128 values in registers, eight rows by eight columns to a thread: a block
-// along the row is then 16 lanes of a DPP row, a block along the column all the threads with the same columns (four
-// in a wave, by LDS from wave to wave), and a thread has eight consecutive codes in either direction.
+// A workgroup of 512 threads holds a tile of 128 x 128 values in registers, four rows by eight columns to a thread.  A
+// block along the row is 16 lanes (a DPP row).  A block along the column is the 32 threads with the same columns: four in
+// a wave, reached by lane swaps, and by LDS from wave to wave; its codes are turned in LDS so that they leave in
+// whole cache lines too.
 #include <hip/hip_runtime.h>
 
 #include "fp8_device.hpp"
@@ -15,38 +16,52 @@
 
 namespace rdfft {
 
-constexpr int kFp8WG = 256, kFp8Waves = kFp8WG / 64;
+constexpr int kFp8WG = 512, kFp8Waves = kFp8WG / 64, kFp8Rows = kFp8Block * kFp8Lanes / kFp8WG;
+constexpr int kFp8Pitch = kFp8Block / 4 + 1;  // words of a column's codes in LDS: the 16 columns of a write on most banks
+static_assert(kFp8Rows == 4, "a thread's codes of a column are a word");
 
-// the maximum and the sum over the four lanes of a wave that are equal modulo 16, in a fixed order
-__device__ __forceinline__ uint32_t across_rows_max(uint32_t v) {
-  v = max(v, (uint32_t)__shfl_xor((int)v, 16));
-  return max(v, (uint32_t)__shfl_xor((int)v, 32));
-}
-__device__ __forceinline__ float across_rows_sum(float v) {
-  v += __shfl_xor(v, 16);
-  return v + __shfl_xor(v, 32);
+// fn over the four lanes that are equal modulo 16, in each of them and in a fixed order
+template <class F>
+__device__ __forceinline__ uint32_t across_rows(uint32_t v, F&& fn) {
+  const auto near = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = fn(near[0], near[1]);
+  const auto far = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return fn(far[0], far[1]);
 }
 
-template <class E, bool EXACT>
+template <class E, bool EXACT, bool SLOPE>
 __global__ void __launch_bounds__(kFp8WG) fp8_quantize_kernel(Fp8Quantize q) {
   using T = typename E::T;
   __shared__ uint32_t top[kFp8Waves][kFp8Block];
   __shared__ float sums[kFp8Waves][kFp8Block];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-  const int64_t row0 = ((int64_t)blockIdx.y * kFp8Block) + threadIdx.x / kFp8Lanes * kVec;
-  const int64_t col0 = (int64_t)blockIdx.x * kFp8Block, col = col0 + threadIdx.x % kFp8Lanes * kVec;
+  __shared__ float inverse[kFp8Block];
+  __shared__ uint32_t tile_top[2], turned[kFp8Block * kFp8Pitch];
+  const int thread = threadIdx.x, lane = thread & 63, wave = thread / 64;
+  const int64_t first_row = (int64_t)blockIdx.y * kFp8Block, row0 = first_row + thread / kFp8Lanes * kFp8Rows;
+  const int64_t col0 = (int64_t)blockIdx.x * kFp8Block, col = col0 + thread % kFp8Lanes * kVec;
   const int64_t rows = q.rows, n = q.n;
   const T* const x = static_cast<const T*>(q.x);
 
-  float v[kVec][kVec];
+  float v[kFp8Rows][kVec];
+  Bytes8 code[SLOPE ? kFp8Rows : 1];
+  int byte[SLOPE ? kFp8Rows : 1];
   if constexpr (EXACT) {
     // (rows and columns past the ends load what is near, without a branch)
-    typename E::Raw raw[kVec];
+    typename E::Raw raw[kFp8Rows];
     const int64_t c = min(col, n - kVec);
 #pragma unroll
-    for (int r = 0; r < kVec; ++r) raw[r] = E::load(x + min(row0 + r, rows - 1) * q.ldx + c);
+    for (int r = 0; r < kFp8Rows; ++r) raw[r] = E::load(x + min(row0 + r, rows - 1) * q.ldx + c);
+    if constexpr (SLOPE) {
+      const int64_t blocks = (n + kCkBlock - 1) / kCkBlock;
 #pragma unroll
-    for (int r = 0; r < kVec; ++r) {
+      for (int r = 0; r < kFp8Rows; ++r) {
+        const int64_t at = min(row0 + r, rows - 1);
+        code[r] = *reinterpret_cast<const Bytes8*>(q.ck.codes + at * n + c);
+        byte[r] = q.ck.scales[at * blocks + c / kCkBlock];
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < kFp8Rows; ++r) {
       E::widen(raw[r], v[r]);
       const bool in = row0 + r < rows && col < n;
 #pragma unroll
@@ -54,99 +69,143 @@ __global__ void __launch_bounds__(kFp8WG) fp8_quantize_kernel(Fp8Quantize q) {
     }
   } else {
 #pragma unroll
-    for (int r = 0; r < kVec; ++r) {
-      if (row0 + r < rows && col < n) {
+    for (int r = 0; r < kFp8Rows; ++r) {
+      const bool in = row0 + r < rows && col < n;
+      if (in) {
         read_group<E>(x + (row0 + r) * q.ldx, col, n, v[r]);
       } else {
 #pragma unroll
         for (int i = 0; i < kVec; ++i) v[r][i] = 0.f;
       }
+      if constexpr (SLOPE) {
+        code[r] = {{0, 0}};
+        byte[r] = 0;
+        if (in) {
+          code[r] = tail_codes(q.ck.codes + (row0 + r) * n, col, n);
+          byte[r] = q.ck.scales[(row0 + r) * ((n + kCkBlock - 1) / kCkBlock) + col / kCkBlock];
+        }
+      }
     }
   }
-  if (q.act != kActNone) {
-    const int64_t blocks = (n + kCkBlock - 1) / kCkBlock;
+  if constexpr (SLOPE) {
 #pragma unroll
-    for (int r = 0; r < kVec; ++r) {
+    for (int r = 0; r < kFp8Rows; ++r) {
       if (row0 + r >= rows || col >= n) continue;
       float z[kVec];
-      const int8_t* const codes = q.ck.codes + (row0 + r) * n;
-      const Bytes8 code = col + kVec <= n ? *reinterpret_cast<const Bytes8*>(codes + col) : tail_codes(codes, col, n);
-      ck_decode<ElemF32>(code, ck_scale(q.ck.scales[(row0 + r) * blocks + col / kCkBlock]), z);
+      ck_decode<ElemF32>(code[r], ck_scale(byte[r]), z);
       times_slope8(q.act, z, v[r]);
     }
   }
   if (q.sums != nullptr) {
+    float s[kVec];
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
-      float s = v[0][i];
+      s[i] = v[0][i];
 #pragma unroll
-      for (int r = 1; r < kVec; ++r) s += v[r][i];
-      s = across_rows_sum(s);
-      if (lane < kFp8Lanes) sums[wave][lane * kVec + i] = s;
+      for (int r = 1; r < kFp8Rows; ++r) s[i] += v[r][i];
+      s[i] = __uint_as_float(across_rows(__float_as_uint(s[i]), [](uint32_t a, uint32_t b) {
+        return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+      }));
+    }
+    if (lane < kFp8Lanes) {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) sums[wave][lane * kVec + i] = s[i];
     }
   }
   // the largest of each column
   const bool by_column = q.columns.codes != nullptr || q.tiles;
   if (by_column) {
+    uint32_t m[kVec];
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
-      uint32_t m = abs_bits(v[0][i]);
+      m[i] = abs_bits(v[0][i]);
 #pragma unroll
-      for (int r = 1; r < kVec; ++r) m = max(m, abs_bits(v[r][i]));
-      m = across_rows_max(m);
-      if (lane < kFp8Lanes) top[wave][lane * kVec + i] = m;
+      for (int r = 1; r < kFp8Rows; ++r) m[i] = max(m[i], abs_bits(v[r][i]));
+      m[i] = across_rows(m[i], [](uint32_t a, uint32_t b) { return max(a, b); });
+    }
+    if (lane < kFp8Lanes) {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) top[wave][lane * kVec + i] = m[i];
     }
   }
   if (by_column || q.sums != nullptr) __syncthreads();
-  if (q.sums != nullptr && threadIdx.x < kFp8Block && col0 + threadIdx.x < n) {
-    float s = sums[0][threadIdx.x];
+  if (thread < kFp8Block) {
+    if (q.sums != nullptr && col0 + thread < n) {
+      float s = sums[0][thread];
 #pragma unroll
-    for (int w = 1; w < kFp8Waves; ++w) s += sums[w][threadIdx.x];
-    q.sums[(int64_t)blockIdx.y * n + col0 + threadIdx.x] = s;
+      for (int w = 1; w < kFp8Waves; ++w) s += sums[w][thread];
+      q.sums[(int64_t)blockIdx.y * n + col0 + thread] = s;
+    }
+    if (by_column) {
+      uint32_t m = top[0][thread];
+#pragma unroll
+      for (int w = 1; w < kFp8Waves; ++w) m = max(m, top[w][thread]);
+      if (q.tiles) {
+        m = row_max(m);
+        m = across_rows(m, [](uint32_t a, uint32_t b) { return max(a, b); });
+        if (lane == 0) tile_top[wave] = m;
+      } else {
+        const int s = fp8_scale_byte(m);
+        inverse[thread] = s == kCkNaN ? __uint_as_float(0x7fc00000u) : ck_inverse(s);
+        if (col0 + thread < n) q.columns.scales[(col0 + thread) * q.columns.lds + blockIdx.y] = (uint8_t)s;
+      }
+    }
   }
-  uint32_t column_top[kVec];
   int tile = 0;
   if (by_column) {
-    uint32_t all = 0;
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-      uint32_t m = 0;
-#pragma unroll
-      for (int w = 0; w < kFp8Waves; ++w) m = max(m, top[w][threadIdx.x % kFp8Lanes * kVec + i]);
-      column_top[i] = m;
-      all = max(all, m);
-    }
-    tile = fp8_scale_byte(row_max(all));
-  }
-  if (q.held.codes != nullptr) {
-#pragma unroll
-    for (int r = 0; r < kVec; ++r) {
-      const int s = q.tiles ? tile : fp8_scale_byte(row_max(max_bits8(v[r])));
-      if (row0 + r >= rows || col >= n) continue;
-      write_bytes(q.held.codes + (row0 + r) * q.held.ld, col, n, fp8_encode(v[r], s));
-      if (threadIdx.x % kFp8Lanes == 0 && (!q.tiles || (threadIdx.x == 0 && r == 0)))
-        q.held.scales[(q.tiles ? (int64_t)blockIdx.y : row0 + r) * q.held.lds + blockIdx.x] = (uint8_t)s;
+    __syncthreads();
+    if (q.tiles) {
+      tile = fp8_scale_byte(max(tile_top[0], tile_top[1]));
+      if (thread == 0) {
+        if (q.held.codes != nullptr) q.held.scales[(int64_t)blockIdx.y * q.held.lds + blockIdx.x] = (uint8_t)tile;
+        if (q.columns.codes != nullptr) q.columns.scales[(int64_t)blockIdx.x * q.columns.lds + blockIdx.y] = (uint8_t)tile;
+      }
     }
   }
   if (q.columns.codes != nullptr) {
+    const float all = tile == kCkNaN ? __uint_as_float(0x7fc00000u) : ck_inverse(tile);
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
-      if (row0 >= rows || col + i >= n) continue;
-      const int s = q.tiles ? tile : fp8_scale_byte(column_top[i]);
-      float t[kVec];
-#pragma unroll
-      for (int r = 0; r < kVec; ++r) t[r] = v[r][i];
-      write_bytes(q.columns.codes + (col + i) * q.columns.ld, row0, rows, fp8_encode(t, s));
-      if (threadIdx.x < kFp8Lanes && (!q.tiles || (threadIdx.x == 0 && i == 0)))
-        q.columns.scales[(q.tiles ? (int64_t)blockIdx.x : col + i) * q.columns.lds + blockIdx.y] = (uint8_t)s;
+      const int c = thread % kFp8Lanes * kVec + i;
+      turned[c * kFp8Pitch + thread / kFp8Lanes] = fp8_word(v[0][i], v[1][i], v[2][i], v[3][i], q.tiles ? all : inverse[c]);
     }
+  }
+  if (q.held.codes != nullptr) {
+#pragma unroll
+    for (int r = 0; r < kFp8Rows; ++r) {
+      const int s = q.tiles ? tile : fp8_scale_byte(row_max(max_bits8(v[r])));
+      if (row0 + r >= rows || col >= n) continue;
+      write_bytes(q.held.codes + (row0 + r) * q.held.ld, col, n, fp8_encode(v[r], s));
+      if (!q.tiles && thread % kFp8Lanes == 0) q.held.scales[(row0 + r) * q.held.lds + blockIdx.x] = (uint8_t)s;
+    }
+  }
+  if (q.columns.codes == nullptr) return;
+  __syncthreads();
+  // a quarter of a column to a thread
+  const int c = thread / 4, part = thread % 4 * 8;
+  const int64_t left = min(rows - first_row - part * 4, (int64_t)32);
+  if (col0 + c >= n || left <= 0) return;
+  uint32_t w[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = turned[c * kFp8Pitch + part + i];
+  uint8_t* const to = q.columns.codes + (col0 + c) * q.columns.ld + first_row + part * 4;
+  if (left == 32) {
+    *reinterpret_cast<Bytes16*>(to) = {{w[0], w[1], w[2], w[3]}};
+    *reinterpret_cast<Bytes16*>(to + 16) = {{w[4], w[5], w[6], w[7]}};
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (i * 4 + e < left) to[i * 4 + e] = (uint8_t)(w[i] >> (8 * e));
   }
 }
 
+constexpr int kDequantizeWG = 256;
 template <class E>
-__global__ void __launch_bounds__(kFp8WG) fp8_dequantize_kernel(Fp8Operand from, typename E::T* __restrict__ out, int64_t ldo,
+__global__ void __launch_bounds__(kDequantizeWG) fp8_dequantize_kernel(Fp8Operand from, typename E::T* __restrict__ out, int64_t ldo,
                                                                 int64_t row0, int64_t rows, int64_t n, int lanes) {
-  const int64_t row = row0 + (int64_t)blockIdx.y * (kFp8WG / lanes) + threadIdx.x / lanes;
+  const int64_t row = row0 + (int64_t)blockIdx.y * (kDequantizeWG / lanes) + threadIdx.x / lanes;
   if (row >= rows) return;
   const int lane = threadIdx.x & (lanes - 1);
   out += row * ldo;
@@ -192,7 +251,9 @@ hipError_t launch_fp8_quantize(const Fp8Quantize& q, hipStream_t stream) {
       }
       return hipSuccess;
     };
-    return q.n % kVec == 0 ? go(fp8_quantize_kernel<E, true>) : go(fp8_quantize_kernel<E, false>);
+    if (q.act != kActNone)
+      return q.n % kVec == 0 ? go(fp8_quantize_kernel<E, true, true>) : go(fp8_quantize_kernel<E, false, true>);
+    return q.n % kVec == 0 ? go(fp8_quantize_kernel<E, true, false>) : go(fp8_quantize_kernel<E, false, false>);
   });
 }
 
@@ -202,13 +263,13 @@ hipError_t launch_fp8_dequantize(const Fp8Operand& from, void* out, int64_t ldo,
     using E = decltype(e);
     const int64_t groups = (n + kVec - 1) / kVec;
     int lanes = 1;
-    while (lanes < kFp8WG && lanes < groups) lanes *= 2;
-    const int per = kFp8WG / lanes;
+    while (lanes < kDequantizeWG && lanes < groups) lanes *= 2;
+    const int per = kDequantizeWG / lanes;
     constexpr int64_t kMaxY = 65535;
     for (int64_t r0 = 0; r0 < rows; r0 += kMaxY * per) {
       const int64_t gy = (std::min(rows - r0, kMaxY * per) + per - 1) / per;
       const int64_t gx = std::min((groups + lanes - 1) / lanes, std::max<int64_t>(1, (int64_t)num_cu * 32 / gy));
-      hipLaunchKernelGGL(fp8_dequantize_kernel<E>, dim3((unsigned)gx, (unsigned)gy), dim3(kFp8WG), 0, stream, from,
+      hipLaunchKernelGGL(fp8_dequantize_kernel<E>, dim3((unsigned)gx, (unsigned)gy), dim3(kDequantizeWG), 0, stream, from,
                          static_cast<typename E::T*>(out), ldo, r0, rows, n, lanes);
       const hipError_t err = hipGetLastError();
       if (err != hipSuccess) return err;

@@ -80,10 +80,12 @@ struct Gemm8Args {
   GemmArgs g;  // (a, b, lda and ldb are not used)
   Fp8Operand a, b;
 };
-enum Linear8Tile { kTile8_32x64, kTile8_64, kTile8_128, kTile8_128x256, kTile8_256, kLinear8Tiles };
+enum Linear8Tile { kTile8_32x64, kTile8_64, kTile8_64x128, kTile8_128, kTile8_128Deep, kTile8_128x256, kTile8_256, kLinear8Tiles };
 using Linear8Fn = hipError_t (*)(const Gemm8Args&, hipStream_t);
+using Linear8PairFn = hipError_t (*)(const Gemm8Args&, const Gemm8Args&, hipStream_t);
 struct Linear8Table {
   Linear8Fn fn[kLinear8Tiles];  // null where one is not built
+  Linear8PairFn pair[kLinear8Tiles];
   Linear8Fn few[3][2];          // 16, 32, 64 rows of A at most; 16 or 32 rows of B to a workgroup
 };
 Linear8Table linear_fp8_table_f32();

@@ -21,11 +21,10 @@ struct TileCost {
   int bm, bn, together;
   double alone, each, ends;
 };
-constexpr TileCost kCost[kLinear8Tiles] = {{32, 64, 4, 0.19, 0.14, 3.4},
-                                           {64, 64, 3, 0.235, 0.175, 3.6},
-                                           {128, 128, 2, 0.50, 0.445, 4.0},
-                                           {128, 256, 1, 0.82, 0.82, 4.8},
-                                           {256, 256, 1, 1.30, 1.30, 13.0}};
+constexpr TileCost kCost[kLinear8Tiles] = {{32, 64, 4, 0.19, 0.145, 2.5},  {64, 64, 3, 0.205, 0.20, 3.0},
+                                           {64, 128, 2, 0.29, 0.31, 3.0},  {128, 128, 2, 0.68, 0.49, 3.5},
+                                           {128, 128, 1, 0.55, 0.60, 3.0}, {128, 256, 1, 0.80, 0.80, 4.9},
+                                           {256, 256, 1, 1.46, 1.46, 7.2}};
 
 static const Linear8Table& table_of(int storage) {
   static const Linear8Table tables[] = {linear_fp8_table_f32(), linear_fp8_table_bf16(), linear_fp8_table_f16()};
@@ -44,7 +43,7 @@ static Plan plan_of(int64_t m, int64_t n, int64_t k, int storage) {
   const int64_t stages = std::max<int64_t>(1, (k + kStage - 1) / kStage);
   Plan best{kTile8_64, 1, stages * kStage, 0};
   for (int t = 0; t < kLinear8Tiles; ++t) {
-    if (storage == kStorageF32 && t > kTile8_128) continue;  // (not built)
+    if (table_of(storage).fn[t] == nullptr) continue;  // (not built)
     const TileCost& c = kCost[t];
     const int64_t tiles = ((m + c.bm - 1) / c.bm) * ((n + c.bn - 1) / c.bn);
     for (int64_t want = 1; want <= 16; ++want) {
@@ -64,6 +63,35 @@ static int64_t split_bytes(int64_t m, int64_t n, int64_t k, int storage) {
   if (m <= kFewTokens) return 0;
   const Plan p = plan_of(m, n, k, storage);
   return p.splits > 1 ? p.splits * m * n * 4 : 0;
+}
+
+// Which tile two products share in one launch, the first one's k being the longer, or kLinear8Tiles where two launches
+// cost less.  Where the first has a workgroup for every CU the rounds are simply full; where it has fewer, its CUs deal
+// part of their time to the second's tiles until those run out, and finish alone.  4 us: the launch that is saved.
+static Linear8Tile together_of(const GemmArgs& first, const GemmArgs& second, int storage) {
+  const double k1 = (double)((first.k + kStage - 1) / kStage), k2 = (double)((second.k + kStage - 1) / kStage);
+  if (first.m <= kFewTokens || second.m <= kFewTokens) return kLinear8Tiles;
+  Linear8Tile best = kLinear8Tiles;
+  double least = 4.0 + plan_of(first.m, first.n, first.k, storage).cost + plan_of(second.m, second.n, second.k, storage).cost;
+  for (int t = 0; t < kLinear8Tiles; ++t) {
+    if (table_of(storage).pair[t] == nullptr) continue;
+    const TileCost& c = kCost[t];
+    const auto tiles = [&](const GemmArgs& g) { return (double)((g.m + c.bm - 1) / c.bm * ((g.n + c.bn - 1) / c.bn)); };
+    const double cus = (double)kCUs, n1 = tiles(first), n2 = tiles(second), per_cu = std::ceil((n1 + n2) / cus);
+    const double full = (n1 * k1 + n2 * k2) / cus * c.each;
+    double cost = std::max(full, k1 * c.alone);
+    if (n1 < cus && per_cu > 1) {
+      const double share = 1 / std::min((double)c.together, per_cu);  // of such a CU that the longer k has
+      const double until = n2 * k2 / cus * c.each / (1 - n1 / cus * share);
+      cost = std::max(full, until + std::max(0.0, k1 - until * share / c.each) * c.alone);
+    }
+    cost += c.ends * std::ceil(per_cu / c.together);
+    if (cost < least) {
+      least = cost;
+      best = (Linear8Tile)t;
+    }
+  }
+  return best;
 }
 
 static hipError_t product(Gemm8Args& args, int storage, void* workspace, hipStream_t stream) {
@@ -165,30 +193,37 @@ hipError_t launch_linear_fp8_backward(const LinearFp8Backward& a, hipStream_t st
                              storage, stream);
     if (e != hipSuccess) return e;
   }
-  if (dx) {
-    Gemm8Args p{};
-    p.a = space.rows;
-    p.b = a.w;
-    p.g.m = T;
-    p.g.n = a.s.d_in;
-    p.g.k = n;
-    p.g.d = a.dx;
-    p.g.ldd = a.ldd;
-    p.g.residual = a.add;
-    p.g.ldr = a.lda;
-    e = product(p, storage, space.parts, stream);
+  Gemm8Args x{}, w{};
+  x.a = space.rows;
+  x.b = a.w;
+  x.g.m = T;
+  x.g.n = a.s.d_in;
+  x.g.k = n;
+  x.g.d = a.dx;
+  x.g.ldd = a.ldd;
+  x.g.residual = a.add;
+  x.g.ldr = a.lda;
+  w.a = space.columns;
+  w.b = a.x;
+  w.g.m = n;
+  w.g.n = a.s.d_in;
+  w.g.k = T;
+  w.g.d = a.dw;
+  w.g.ldd = a.lddw;
+  if (dx && dw) {
+    const bool dw_first = T >= n;  // (the longer k)
+    Gemm8Args &first = dw_first ? w : x, &second = dw_first ? x : w;
+    const Linear8Tile t = together_of(first.g, second.g, storage);
+    if (t != kLinear8Tiles) {
+      for (GemmArgs* g : {&first.g, &second.g}) {
+        g->splits = 1;
+        g->k_split = g->k;
+      }
+      return table_of(storage).pair[t](first, second, stream);
+    }
   }
-  if (e == hipSuccess && dw) {
-    Gemm8Args p{};
-    p.a = space.columns;
-    p.b = a.x;
-    p.g.m = n;
-    p.g.n = a.s.d_in;
-    p.g.k = T;
-    p.g.d = a.dw;
-    p.g.ldd = a.lddw;
-    e = product(p, storage, space.parts, stream);
-  }
+  if (dx) e = product(x, storage, space.parts, stream);
+  if (e == hipSuccess && dw) e = product(w, storage, space.parts, stream);
   return e;
 }
 

@@ -184,6 +184,7 @@ __device__ __forceinline__ void linear_fp8_tile(const Gemm8Args& args, int id) {
   constexpr bool WIDE = E::kId == kStorageF32;
   constexpr int WAVES = WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32;
   constexpr int BK = kStageBytes, STAGE = Tile::STAGE;
+  static_assert(STAGES <= 4);
   constexpr bool STREAM = FM >= 4 && !WIDE;  // fragments of A one at a time: two halves of a stage take too many registers
   using OpA = CodeOperand<BM, WAVES>;
   using OpB = CodeOperand<BN, WAVES>;
@@ -367,7 +368,7 @@ __device__ __forceinline__ void linear_fp8_tile(const Gemm8Args& args, int id) {
     // Fragments of A come one at a time, AHEAD steps before their products, into a ring; those of B half a stage
     // before.  The barrier comes when the stage's last fragment is read, AHEAD steps before its end.
     constexpr int STEPS = 2 * FM, AHEAD = 3, RING = 4, LAST = STEPS - AHEAD;
-    static_assert(STEPS % RING == 0 && FN <= AHEAD && FN <= LAST);
+    static_assert(STEPS % RING == 0 && FN <= LAST);
     i32x8 ring[RING], hb[2][FN];
     const auto stage = [&](auto is_steady) {
       constexpr bool STEADY = decltype(is_steady)::value;
@@ -405,7 +406,8 @@ __device__ __forceinline__ void linear_fp8_tile(const Gemm8Args& args, int id) {
         if (s < LAST) {
           ring[to % RING] = fa.read(here, to % FM, to / FM);
         } else if (more) {
-          if (s - LAST < FN) hb[0][s - LAST] = fb.read(there + OpA::BYTES, s - LAST, 0);
+#pragma unroll
+          for (int j = (s - LAST) * FN / AHEAD; j < (s - LAST + 1) * FN / AHEAD; ++j) hb[0][j] = fb.read(there + OpA::BYTES, j, 0);
           ring[to % RING] = fa.read(there, (to - STEPS) % FM, (to - STEPS) / FM);
         }
 #pragma unroll
@@ -449,7 +451,9 @@ __device__ __forceinline__ void linear_fp8_tile(const Gemm8Args& args, int id) {
       multiply(h0);
       if (t + 1 < steps) {
         // this stage is read; the next has landed when those after it are all that is left
-        if (STAGES > 2 && t + STAGES - 1 < steps) stage_wait<(STAGES - 2) * EACH>();
+        const int after = steps - t - 2;
+        if (STAGES > 3 && after >= 2) stage_wait<(STAGES > 3 ? 2 : 0) * EACH>();
+        else if (STAGES > 2 && after >= 1) stage_wait<(STAGES > 2 ? 1 : 0) * EACH>();
         else stage_wait<0>();
         if (t + STAGES < steps) fetch(cur);
         cur = next(cur);
@@ -508,7 +512,8 @@ __device__ __forceinline__ void linear_fp8_tile(const Gemm8Args& args, int id) {
 }
 
 template <class E, int BM, int BN, int WM, int WN, int STAGES>
-__global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2))) linear_fp8_kernel(Gemm8Args args) {
+__global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(BM / WM * BN / WN > 128 * 64 ? 1 : 2)))
+    linear_fp8_kernel(Gemm8Args args) {
   linear_fp8_tile<E, BM, BN, WM, WN, STAGES>(args, (int)blockIdx.x);
 }
 
@@ -524,6 +529,34 @@ hipError_t linear_fp8_launch(const Gemm8Args& args, hipStream_t stream) {
   t.g.tiles_m = (int)((args.g.m + BM - 1) / BM);
   t.g.tiles_n = (int)((args.g.n + BN - 1) / BN);
   hipLaunchKernelGGL(kernel, dim3((unsigned)(t.g.tiles_m * t.g.tiles_n * t.g.splits)), dim3(WM * WN * 64), lds, stream, t);
+  return hipGetLastError();
+}
+
+// Two products in one launch, neither with its k split: where each alone leaves CUs idle they fill each other's rounds.
+// The first workgroups take the tiles of the first.
+template <class E, int BM, int BN, int WM, int WN, int STAGES>
+__global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(2)))
+    linear_fp8_pair_kernel(Gemm8Args first, Gemm8Args second) {
+  const int id = (int)blockIdx.x, tiles = first.g.tiles_m * first.g.tiles_n;
+  // (the same code for both: they differ in their arguments alone)
+  linear_fp8_tile<E, BM, BN, WM, WN, STAGES>(id < tiles ? first : second, id < tiles ? id : id - tiles);
+}
+
+template <class E, int BM, int BN, int WM, int WN, int STAGES>
+hipError_t linear_fp8_pair_launch(const Gemm8Args& first, const Gemm8Args& second, hipStream_t stream) {
+  constexpr int lds = Fp8Tile<E, BM, BN, WM, WN, STAGES>::LDS;
+  static_assert(lds <= 160 * 1024);
+  const auto kernel = linear_fp8_pair_kernel<E, BM, BN, WM, WN, STAGES>;
+  static const hipError_t ready = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                                      hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (ready != hipSuccess) return ready;
+  Gemm8Args t[2] = {first, second};
+  for (Gemm8Args& p : t) {
+    p.g.tiles_m = (int)((p.g.m + BM - 1) / BM);
+    p.g.tiles_n = (int)((p.g.n + BN - 1) / BN);
+  }
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(t[0].g.tiles_m * t[0].g.tiles_n + t[1].g.tiles_m * t[1].g.tiles_n)),
+                     dim3(WM * WN * 64), lds, stream, t[0], t[1]);
   return hipGetLastError();
 }
 
@@ -684,7 +717,12 @@ Linear8Table make_linear_fp8_table() {
   Linear8Table t{};
   t.fn[kTile8_32x64] = linear_fp8_launch<E, 32, 64, 1, 2, 3>;
   t.fn[kTile8_64] = linear_fp8_launch<E, 64, 64, 2, 2, 3>;
-  t.fn[kTile8_128] = linear_fp8_launch<E, 128, 128, 2, 4, 2>;
+  t.fn[kTile8_64x128] = linear_fp8_launch<E, 64, 128, 2, 2, 3>;
+  t.fn[kTile8_128] = linear_fp8_launch<E, 128, 128, 2, 2, 2>;
+  t.fn[kTile8_128Deep] = linear_fp8_launch<E, 128, 128, 2, 2, 4>;
+  t.pair[kTile8_64] = linear_fp8_pair_launch<E, 64, 64, 2, 2, 3>;
+  t.pair[kTile8_64x128] = linear_fp8_pair_launch<E, 64, 128, 2, 2, 3>;
+  t.pair[kTile8_128] = linear_fp8_pair_launch<E, 128, 128, 2, 2, 2>;
   if constexpr (E::kId != kStorageF32) {
     t.fn[kTile8_128x256] = linear_fp8_launch<E, 128, 256, 2, 4, 3>;
     t.fn[kTile8_256] = linear_fp8_launch<E, 256, 256, 2, 4, 2>;
