@@ -727,8 +727,8 @@ Linear8Table make_linear_fp8_table() {
     t.fn[kTile8_128x256] = linear_fp8_launch<E, 128, 256, 2, 4, 3>;
     t.fn[kTile8_256] = linear_fp8_launch<E, 256, 256, 2, 4, 2>;
   }
-  t.few[0][0] = few_fp8_launch<E, 1, 1, 8, 4>;
-  t.few[0][1] = few_fp8_launch<E, 1, 2, 4, 6>;
+  t.few[0][0] = few_fp8_launch<E, 1, 1, 8, 2>;
+  t.few[0][1] = few_fp8_launch<E, 1, 2, 8, 2>;
   t.few[1][0] = few_fp8_launch<E, 2, 1, 4, 6>;
   t.few[1][1] = few_fp8_launch<E, 2, 2, 4, 4>;
   t.few[2][0] = few_fp8_launch<E, 4, 1, 4, 3>;

@@ -54,6 +54,33 @@ struct RowGroup {
     }
   }
 };
+// The same for rows of any length of at least eight, loaded without a branch: a group that the row's end cuts is loaded so
+// as to end there and shifted into place by the lanes that hold it.
+template <class E>
+struct ShiftedGroup {
+  using T = typename E::T;
+  typename E::Raw raw;
+  __device__ __forceinline__ void load(const T* row, int i0, int n) { raw = E::load(row + min(i0, n - kVec)); }
+  __device__ __forceinline__ void widen(const T*, int i0, int n, float* v) const {
+    E::widen(raw, v);
+    int past = i0 + kVec - n;
+    if (past > 0) {
+      asm volatile("" : "+v"(past));  // (what follows from it is not worth registers from row to row)
+#pragma unroll
+      for (int by = 4; by > 0; by /= 2)
+#pragma unroll
+        for (int k = 0; k < kVec; ++k) v[k] = past >= kVec ? 0.f : !(past & by) ? v[k] : k + by < kVec ? v[k + by] : 0.f;
+    }
+  }
+};
+// Eight codes of such a row's checkpoint, zeros past its end.
+__device__ __forceinline__ Bytes8 shifted_codes(const int8_t* row, int i0, int n) {
+  const Bytes8 c = *reinterpret_cast<const Bytes8*>(row + min(i0, n - kVec));
+  const int past = min(max(i0 + kVec - n, 0), kVec);
+  const uint64_t w = past == kVec ? 0 : ((uint64_t)c.w[1] << 32 | c.w[0]) >> (8 * past);
+  return {{(uint32_t)w, (uint32_t)(w >> 32)}};
+}
+
 template <class E, bool EXACT>
 __device__ __forceinline__ void store_group(typename E::T* row, int i0, int n, const float* v) {
   if constexpr (EXACT) {

@@ -23,6 +23,11 @@ constexpr int rms_fwd_wg() {
   return TPR > 256 ? TPR : 256;
 }
 
+// Rows of whole groups, of any length of at least eight, and shorter ones (value by value)
+enum RowsOf { kWholeGroups, kCutGroups, kShort };
+template <class E, RowsOf ROWS>
+using RmsGroup = std::conditional_t<ROWS == kCutGroups, ShiftedGroup<E>, RowGroup<E, ROWS == kWholeGroups>>;
+
 // eight values as the storage type holds them
 template <class E>
 __device__ __forceinline__ void round_group(float* v) {
@@ -33,7 +38,7 @@ __device__ __forceinline__ void round_group(float* v) {
   }
 }
 
-template <class E, int TPR, int C, bool EXACT>
+template <class E, int TPR, int C, RowsOf ROWS>
 __global__ void __launch_bounds__(rms_fwd_wg<TPR>()) rms_norm_forward_kernel(RmsArgs a) {
   using T = typename E::T;
   constexpr int WG = rms_fwd_wg<TPR>(), GROUPS = TPR > 64 ? 1 : WG / TPR;
@@ -57,7 +62,7 @@ __global__ void __launch_bounds__(rms_fwd_wg<TPR>()) rms_norm_forward_kernel(Rms
     const T* const x = static_cast<const T*>(a.x) + row * a.ldx;
     const T* const r = static_cast<const T*>(a.residual) + row * a.ldr;
     float u[C][kVec];
-    RowGroup<E, EXACT> xs[C], rs[C];
+    RmsGroup<E, ROWS> xs[C], rs[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) xs[c].load(x, at[c], n);
     if (a.residual != nullptr) {
@@ -98,7 +103,7 @@ __global__ void __launch_bounds__(rms_fwd_wg<TPR>()) rms_norm_forward_kernel(Rms
     if (a.summed != nullptr) {
       T* const h = static_cast<T*>(a.summed) + row * a.lds;
 #pragma unroll
-      for (int c = 0; c < C; ++c) store_group<E, EXACT>(h, at[c], n, u[c]);
+      for (int c = 0; c < C; ++c) store_group<E, ROWS == kWholeGroups>(h, at[c], n, u[c]);
     }
     if (a.ck.codes != nullptr) {
 #pragma unroll
@@ -111,7 +116,7 @@ __global__ void __launch_bounds__(rms_fwd_wg<TPR>()) rms_norm_forward_kernel(Rms
     if (a.y != nullptr) {
       T* const y = static_cast<T*>(a.y) + row * a.ldy;
 #pragma unroll
-      for (int c = 0; c < C; ++c) store_group<E, EXACT>(y, at[c], n, u[c]);
+      for (int c = 0; c < C; ++c) store_group<E, ROWS == kWholeGroups>(y, at[c], n, u[c]);
     }
     if (a.y8.codes != nullptr) {
 #pragma unroll
@@ -128,29 +133,29 @@ constexpr int rms_bwd_lds() {
 }
 
 // A row's dy, what is added to dx, and the norm's input (or its checkpoint), on their way from memory
-template <class E, int TPR, int C, bool CK, bool EXACT>
+template <class E, int TPR, int C, bool CK, RowsOf ROWS>
 struct RmsRow {
   using T = typename E::T;
-  RowGroup<E, EXACT> dy[C], u[CK ? 1 : C], add[C];
+  RmsGroup<E, ROWS> dy[C], u[CK ? 1 : C], add[C];
   Bytes8 codes[CK ? C : 1];
   int scale[CK ? C : 1];
   float rstd;
 
   __device__ __forceinline__ void load(const RmsGradArgs& a, int64_t row, const int* at, int n, int blocks) {
     rstd = a.rstd[row];
-    if constexpr (EXACT) {
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        dy[c].load(static_cast<const T*>(a.dy) + row * a.ldg, at[c], n);
+    for (int c = 0; c < C; ++c) {
+      dy[c].load(static_cast<const T*>(a.dy) + row * a.ldg, at[c], n);
+      if constexpr (CK) {
         const int i = at[c] < n ? at[c] : 0;
-        if constexpr (CK) {
-          codes[c] = *reinterpret_cast<const Bytes8*>(a.ck.codes + row * n + i);
-          scale[c] = a.ck.scales[row * blocks + i / kCkBlock];
-        } else {
-          u[c].load(static_cast<const T*>(a.u) + row * a.ldu, at[c], n);
-        }
-        if (a.add != nullptr) add[c].load(static_cast<const T*>(a.add) + row * a.lda, at[c], n);
+        if constexpr (ROWS == kWholeGroups) codes[c] = *reinterpret_cast<const Bytes8*>(a.ck.codes + row * n + i);
+        else if constexpr (ROWS == kCutGroups) codes[c] = shifted_codes(a.ck.codes + row * n, at[c], n);
+        else codes[c] = tail_codes(a.ck.codes + row * n, at[c], n);
+        scale[c] = a.ck.scales[row * blocks + i / kCkBlock];
+      } else {
+        u[c].load(static_cast<const T*>(a.u) + row * a.ldu, at[c], n);
       }
+      if (a.add != nullptr) add[c].load(static_cast<const T*>(a.add) + row * a.lda, at[c], n);
     }
   }
   __device__ __forceinline__ void widen(const RmsGradArgs& a, int64_t row, const int* at, int n, int blocks,
@@ -158,13 +163,10 @@ struct RmsRow {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       dy[c].widen(static_cast<const T*>(a.dy) + row * a.ldg, at[c], n, g[c]);
-      if constexpr (CK && EXACT) {
+      if constexpr (CK) {
         ck_decode<ElemF32>(codes[c], ck_scale(scale[c]), v[c]);
 #pragma unroll
         for (int k = 0; k < kVec; ++k) v[c][k] = at[c] < n ? v[c][k] : 0.f;
-      } else if constexpr (CK) {
-        const int s = at[c] < n ? a.ck.scales[row * blocks + at[c] / kCkBlock] : 0;
-        ck_decode<ElemF32>(tail_codes(a.ck.codes + row * n, at[c], n), ck_scale(s), v[c]);
       } else {
         u[c].widen(static_cast<const T*>(a.u) + row * a.ldu, at[c], n, v[c]);
       }
@@ -173,7 +175,7 @@ struct RmsRow {
 };
 
 // Each workgroup's sums go to dw_out + blockIdx.x * n.
-template <class E, int TPR, int C, bool CK, bool EXACT>
+template <class E, int TPR, int C, bool CK, RowsOf ROWS>
 __global__ void __launch_bounds__(kRmsBwdWG) rms_norm_backward_kernel(RmsGradArgs a, float* dw_out) {
   using T = typename E::T;
   constexpr int WG = kRmsBwdWG, GROUPS = WG / TPR;
@@ -193,7 +195,7 @@ __global__ void __launch_bounds__(kRmsBwdWG) rms_norm_backward_kernel(RmsGradArg
     for (int k = 0; k < kVec; ++k) dw[c][k] = 0.f;
   }
   int64_t row = (int64_t)blockIdx.x * GROUPS + grp;
-  using Row = RmsRow<E, TPR, C, CK, EXACT>;
+  using Row = RmsRow<E, TPR, C, CK, ROWS>;
   // (the groups of a workgroup take the same number of rows: they meet at barriers)
   const auto work = [&](const Row& in, bool act, auto&& loads) {
     float u[C][kVec], g[C][kVec], more[C][kVec];
@@ -236,7 +238,7 @@ __global__ void __launch_bounds__(kRmsBwdWG) rms_norm_backward_kernel(RmsGradArg
         float v[kVec];
 #pragma unroll
         for (int k = 0; k < kVec; ++k) v[k] = fmaf(rstd, g[c][k] - u[c][k] * mean, more[c][k]);
-        store_group<E, EXACT>(dx, at[c], n, v);
+        store_group<E, ROWS == kWholeGroups>(dx, at[c], n, v);
       }
     }
     row += step;
@@ -285,19 +287,29 @@ __global__ void __launch_bounds__(kRmsBwdWG) rms_norm_backward_kernel(RmsGradArg
   }
 }
 
-hipError_t launch_rms_norm_forward(const RmsArgs& a, hipStream_t stream, int num_cu) {
-  return with_elem(a.storage, [&](auto e) {
-    return with_row(a.n, [&](auto tpr, auto c) {
-      return with_exact(a.n, [&](auto exact) {
-        constexpr int TPR = decltype(tpr)::value, C = decltype(c)::value, WG = rms_fwd_wg<TPR>();
-        constexpr int groups = TPR > 64 ? 1 : WG / TPR;
-        // as many workgroups as are on the chip at once
-        const int64_t grid = std::min((a.rows + groups - 1) / groups, (int64_t)num_cu * (2048 / WG));
-        hipLaunchKernelGGL((rms_norm_forward_kernel<decltype(e), TPR, C, decltype(exact)::value>), dim3((unsigned)grid),
-                           dim3(WG), 0, stream, a);
-        return hipGetLastError();
-      });
+// fn(storage type, threads of a row, groups of eight per thread, RowsOf); pick: with_row or with_row_backward
+template <class Pick, class F>
+static hipError_t with_rows(int storage, int64_t n, Pick&& pick, F&& fn) {
+  using std::integral_constant;
+  return with_elem(storage, [&](auto e) {
+    if (n < kVec) return fn(e, integral_constant<int, 64>{}, integral_constant<int, 1>{}, integral_constant<RowsOf, kShort>{});
+    return pick(n, [&](auto tpr, auto c) {
+      return n % kVec == 0 ? fn(e, tpr, c, integral_constant<RowsOf, kWholeGroups>{})
+                           : fn(e, tpr, c, integral_constant<RowsOf, kCutGroups>{});
     });
+  });
+}
+
+hipError_t launch_rms_norm_forward(const RmsArgs& a, hipStream_t stream, int num_cu) {
+  const auto pick = [](int64_t n, auto&& fn) { return with_row(n, fn); };
+  return with_rows(a.storage, a.n, pick, [&](auto e, auto tpr, auto c, auto of) {
+    constexpr int TPR = decltype(tpr)::value, C = decltype(c)::value, WG = rms_fwd_wg<TPR>();
+    constexpr int groups = TPR > 64 ? 1 : WG / TPR;
+    // as many workgroups as are on the chip at once
+    const int64_t grid = std::min((a.rows + groups - 1) / groups, (int64_t)num_cu * (2048 / WG));
+    hipLaunchKernelGGL((rms_norm_forward_kernel<decltype(e), TPR, C, decltype(of)::value>), dim3((unsigned)grid), dim3(WG), 0,
+                       stream, a);
+    return hipGetLastError();
   });
 }
 
@@ -313,10 +325,10 @@ int64_t rms_partials(int64_t rows, int64_t n) {
   return rows <= 2 * groups ? 1 : std::min((rows + groups - 1) / groups, kRmsMaxPartials);
 }
 
-template <class E, int TPR, int C, bool CK, bool EXACT>
+template <class E, int TPR, int C, bool CK, RowsOf ROWS>
 static hipError_t rms_backward_launch(const RmsGradArgs& a, int64_t grid, float* dw, hipStream_t stream) {
   constexpr int lds = rms_bwd_lds<TPR, C>();
-  const auto kernel = rms_norm_backward_kernel<E, TPR, C, CK, EXACT>;
+  const auto kernel = rms_norm_backward_kernel<E, TPR, C, CK, ROWS>;
   static const hipError_t ready = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                                       hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (ready != hipSuccess) return ready;
@@ -328,16 +340,13 @@ hipError_t launch_rms_norm_backward(const RmsGradArgs& a, hipStream_t stream) {
   const int64_t grid = rms_partials(a.rows, a.n);
   // a single workgroup's sums are the result
   float* const dw = a.dweight == nullptr ? nullptr : grid == 1 ? a.dweight : a.partials;
-  const hipError_t err = with_elem(a.storage, [&](auto e) {
-    return with_row_backward(a.n, [&](auto tpr, auto c) {
-      return with_exact(a.n, [&](auto exact) {
-        using E = decltype(e);
-        constexpr int TPR = decltype(tpr)::value, C = decltype(c)::value;
-        constexpr bool EXACT = decltype(exact)::value;
-        return a.u == nullptr ? rms_backward_launch<E, TPR, C, true, EXACT>(a, grid, dw, stream)
-                              : rms_backward_launch<E, TPR, C, false, EXACT>(a, grid, dw, stream);
-      });
-    });
+  const auto pick = [](int64_t n, auto&& fn) { return with_row_backward(n, fn); };
+  const hipError_t err = with_rows(a.storage, a.n, pick, [&](auto e, auto tpr, auto c, auto of) {
+    using E = decltype(e);
+    constexpr int TPR = decltype(tpr)::value, C = decltype(c)::value;
+    constexpr RowsOf ROWS = decltype(of)::value;
+    return a.u == nullptr ? rms_backward_launch<E, TPR, C, true, ROWS>(a, grid, dw, stream)
+                          : rms_backward_launch<E, TPR, C, false, ROWS>(a, grid, dw, stream);
   });
   if (err != hipSuccess || grid == 1 || dw == nullptr) return err;
   return launch_column_finish(a.partials, grid, a.n, a.n, a.dweight, nullptr, kStorageF32, stream);
