@@ -96,7 +96,8 @@ __global__ void __launch_bounds__(kFp8WG) fp8_quantize_kernel(Fp8Quantize q) {
       times_slope8(q.act, z, v[r]);
     }
   }
-  if (q.sums != nullptr) {
+  const bool by_sums = q.sums != nullptr || q.total != nullptr;
+  if (by_sums) {
     float s[kVec];
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
@@ -128,13 +129,14 @@ __global__ void __launch_bounds__(kFp8WG) fp8_quantize_kernel(Fp8Quantize q) {
       for (int i = 0; i < kVec; ++i) top[wave][lane * kVec + i] = m[i];
     }
   }
-  if (by_column || q.sums != nullptr) __syncthreads();
+  if (by_column || by_sums) __syncthreads();
   if (thread < kFp8Block) {
-    if (q.sums != nullptr && col0 + thread < n) {
+    if (by_sums && col0 + thread < n) {
       float s = sums[0][thread];
 #pragma unroll
       for (int w = 1; w < kFp8Waves; ++w) s += sums[w][thread];
-      q.sums[(int64_t)blockIdx.y * n + col0 + thread] = s;
+      if (q.total != nullptr) E::put(static_cast<T*>(q.total) + col0 + thread, s);
+      else q.sums[(int64_t)blockIdx.y * n + col0 + thread] = s;
     }
     if (by_column) {
       uint32_t m = top[0][thread];

@@ -19,7 +19,8 @@ struct Fp8Operand {
 };
 
 // x [rows][n] (times the slope of `act` at what ck stands for) by rows into `held`, by columns into `columns`
-// (either null); tiles: both with one scale for 128 x 128.  sums: [ceil(rows/128)][n], over each 128 rows.
+// (either null); tiles: both with one scale for 128 x 128.  sums: [ceil(rows/128)][n], over each 128 rows; or
+// total: of at most 128 rows, in the storage type.
 struct Fp8Quantize {
   const void* x;
   int64_t ldx;
@@ -29,6 +30,7 @@ struct Fp8Quantize {
   int act;
   Checkpoint ck;
   float* sums;
+  void* total;
   int storage;
 };
 hipError_t launch_fp8_quantize(const Fp8Quantize& q, hipStream_t stream);

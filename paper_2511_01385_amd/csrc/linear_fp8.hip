@@ -38,23 +38,32 @@ struct Plan {
 };
 
 // The tile and the number of k ranges that cost least.  The join of s ranges costs a launch (4 us) and 8 s bytes a
-// result, at 4 TB/s.
+// result, at 4 TB/s; a product that takes less than that whole is not looked at in ranges.
 static Plan plan_of(int64_t m, int64_t n, int64_t k, int storage) {
   const int64_t stages = std::max<int64_t>(1, (k + kStage - 1) / kStage);
+  const Linear8Table& table = table_of(storage);
   Plan best{kTile8_64, 1, stages * kStage, 0};
-  for (int t = 0; t < kLinear8Tiles; ++t) {
-    if (table_of(storage).fn[t] == nullptr) continue;  // (not built)
+  const auto look = [&](int t, int64_t tiles, int64_t splits, int64_t each) {
     const TileCost& c = kCost[t];
-    const int64_t tiles = ((m + c.bm - 1) / c.bm) * ((n + c.bn - 1) / c.bn);
-    for (int64_t want = 1; want <= 16; ++want) {
+    const int64_t per_cu = std::max<int64_t>(1, (tiles * splits + kCUs - 1) / kCUs);
+    const double stage = per_cu == 1 ? c.alone : c.each * (double)per_cu;
+    double cost = (double)each * stage + c.ends * (double)((per_cu + c.together - 1) / c.together);
+    if (splits > 1) cost += 4.0 + 8.0 * (double)splits * (double)m * (double)n / 4e6;
+    if (best.cost == 0 || cost < best.cost) best = {(Linear8Tile)t, splits, each * kStage, cost};
+  };
+  int64_t tiles[kLinear8Tiles];
+  for (int t = 0; t < kLinear8Tiles; ++t) {
+    if (table.fn[t] == nullptr) continue;  // (not built)
+    tiles[t] = ((m + kCost[t].bm - 1) / kCost[t].bm) * ((n + kCost[t].bn - 1) / kCost[t].bn);
+    look(t, tiles[t], 1, stages);
+  }
+  for (int t = 0; t < kLinear8Tiles; ++t) {
+    if (table.fn[t] == nullptr) continue;
+    for (int64_t want = 2; want <= 16; ++want) {
       const int64_t each = (stages + want - 1) / want, splits = (stages + each - 1) / each;
-      if (splits != want) continue;  // (as many ranges of another length)
-      if (splits > 1 && (each < 2 || tiles * splits > 4 * kCUs)) break;
-      const int64_t per_cu = std::max<int64_t>(1, (tiles * splits + kCUs - 1) / kCUs);
-      const double stage = per_cu == 1 ? c.alone : c.each * (double)per_cu;
-      double cost = (double)each * stage + c.ends * (double)((per_cu + c.together - 1) / c.together);
-      if (splits > 1) cost += 4.0 + 8.0 * (double)splits * (double)m * (double)n / 4e6;
-      if (best.cost == 0 || cost < best.cost) best = {(Linear8Tile)t, splits, each * kStage, cost};
+      if (each < 2 || tiles[t] * want > 4 * kCUs) break;
+      if (4.0 + kCost[t].ends + 8.0 * (double)want * (double)m * (double)n / 4e6 >= best.cost) break;
+      if (splits == want) look(t, tiles[t], splits, each);  // (else as many ranges of another length)
     }
   }
   return best;
@@ -70,9 +79,12 @@ static int64_t split_bytes(int64_t m, int64_t n, int64_t k, int storage) {
 // part of their time to the second's tiles until those run out, and finish alone.  4 us: the launch that is saved.
 static Linear8Tile together_of(const GemmArgs& first, const GemmArgs& second, int storage) {
   const double k1 = (double)((first.k + kStage - 1) / kStage), k2 = (double)((second.k + kStage - 1) / kStage);
-  if (first.m <= kFewTokens || second.m <= kFewTokens) return kLinear8Tiles;
+  // (the few rows' kernel: B's bytes at the rate of memory, 3 us before and after)
+  const auto alone = [&](const GemmArgs& g) {
+    return g.m <= kFewTokens ? 3.0 + (double)g.n * (double)g.k / 5e6 : plan_of(g.m, g.n, g.k, storage).cost;
+  };
   Linear8Tile best = kLinear8Tiles;
-  double least = 4.0 + plan_of(first.m, first.n, first.k, storage).cost + plan_of(second.m, second.n, second.k, storage).cost;
+  double least = 4.0 + alone(first) + alone(second);
   for (int t = 0; t < kLinear8Tiles; ++t) {
     if (table_of(storage).pair[t] == nullptr) continue;
     const TileCost& c = kCost[t];
@@ -161,7 +173,7 @@ static BackwardSpace space_of(const LinearSizes& s, bool dx, bool dw, void* work
 
 int64_t linear_fp8_backward_workspace(const LinearSizes& s, bool dx, bool dw, bool db) {
   int64_t parts = 0;
-  if (db) parts = std::max(parts, (s.tokens + kStage - 1) / kStage * s.d_out * 4);
+  if (db && s.tokens > kStage) parts = std::max(parts, (s.tokens + kStage - 1) / kStage * s.d_out * 4);
   if (dx) parts = std::max(parts, split_bytes(s.tokens, s.d_in, s.d_out, s.storage));
   if (dw) parts = std::max(parts, split_bytes(s.d_out, s.d_in, s.tokens, s.storage));
   return space_of(s, dx, dw, nullptr).bytes + parts;
@@ -183,12 +195,14 @@ hipError_t launch_linear_fp8_backward(const LinearFp8Backward& a, hipStream_t st
     if (dw) q.columns = space.columns;
     q.act = a.s.act;
     q.ck = a.s.act == kActNone ? Checkpoint{} : a.ck;
-    q.sums = a.db == nullptr ? nullptr : reinterpret_cast<float*>(space.parts);
+    // (the sums of a single band are db itself)
+    if (a.db != nullptr && T <= kStage) q.total = a.db;
+    else if (a.db != nullptr) q.sums = reinterpret_cast<float*>(space.parts);
     q.storage = storage;
     e = launch_fp8_quantize(q, stream);
     if (e != hipSuccess) return e;
   }
-  if (a.db != nullptr) {
+  if (a.db != nullptr && (T == 0 || T > kStage)) {
     e = launch_column_finish(reinterpret_cast<const float*>(space.parts), (T + kStage - 1) / kStage, n, n, a.db, nullptr,
                              storage, stream);
     if (e != hipSuccess) return e;
