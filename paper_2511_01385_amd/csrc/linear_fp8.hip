@@ -21,10 +21,13 @@ struct TileCost {
   int bm, bn, together;
   double alone, each, ends;
 };
-constexpr TileCost kCost[kLinear8Tiles] = {{32, 64, 4, 0.19, 0.145, 2.5},  {64, 64, 3, 0.205, 0.20, 3.0},
+constexpr TileCost kCost16[kLinear8Tiles] = {{32, 64, 4, 0.19, 0.145, 2.5},  {64, 64, 3, 0.205, 0.20, 3.0},
                                            {64, 128, 2, 0.29, 0.31, 3.0},  {128, 128, 2, 0.68, 0.49, 3.5},
                                            {128, 128, 1, 0.55, 0.60, 3.0}, {128, 256, 1, 0.80, 0.80, 4.9},
                                            {256, 256, 1, 1.46, 1.46, 7.2}};
+// float32 results
+constexpr TileCost kCost32[] = {{32, 64, 4, 0.24, 0.32, 2.5}, {64, 64, 3, 0.45, 0.45, 3.0}, {64, 128, 2, 0.85, 0.80, 3.0}};
+static const TileCost* costs_of(int storage) { return storage == kStorageF32 ? kCost32 : kCost16; }
 
 static const Linear8Table& table_of(int storage) {
   static const Linear8Table tables[] = {linear_fp8_table_f32(), linear_fp8_table_bf16(), linear_fp8_table_f16()};
@@ -42,9 +45,10 @@ struct Plan {
 static Plan plan_of(int64_t m, int64_t n, int64_t k, int storage) {
   const int64_t stages = std::max<int64_t>(1, (k + kStage - 1) / kStage);
   const Linear8Table& table = table_of(storage);
+  const TileCost* const costs = costs_of(storage);
   Plan best{kTile8_64, 1, stages * kStage, 0};
   const auto look = [&](int t, int64_t tiles, int64_t splits, int64_t each) {
-    const TileCost& c = kCost[t];
+    const TileCost& c = costs[t];
     const int64_t per_cu = std::max<int64_t>(1, (tiles * splits + kCUs - 1) / kCUs);
     const double stage = per_cu == 1 ? c.alone : c.each * (double)per_cu;
     double cost = (double)each * stage + c.ends * (double)((per_cu + c.together - 1) / c.together);
@@ -54,7 +58,7 @@ static Plan plan_of(int64_t m, int64_t n, int64_t k, int storage) {
   int64_t tiles[kLinear8Tiles];
   for (int t = 0; t < kLinear8Tiles; ++t) {
     if (table.fn[t] == nullptr) continue;  // (not built)
-    tiles[t] = ((m + kCost[t].bm - 1) / kCost[t].bm) * ((n + kCost[t].bn - 1) / kCost[t].bn);
+    tiles[t] = ((m + costs[t].bm - 1) / costs[t].bm) * ((n + costs[t].bn - 1) / costs[t].bn);
     look(t, tiles[t], 1, stages);
   }
   for (int t = 0; t < kLinear8Tiles; ++t) {
@@ -62,7 +66,7 @@ static Plan plan_of(int64_t m, int64_t n, int64_t k, int storage) {
     for (int64_t want = 2; want <= 16; ++want) {
       const int64_t each = (stages + want - 1) / want, splits = (stages + each - 1) / each;
       if (each < 2 || tiles[t] * want > 4 * kCUs) break;
-      if (4.0 + kCost[t].ends + 8.0 * (double)want * (double)m * (double)n / 4e6 >= best.cost) break;
+      if (4.0 + costs[t].ends + 8.0 * (double)want * (double)m * (double)n / 4e6 >= best.cost) break;
       if (splits == want) look(t, tiles[t], splits, each);  // (else as many ranges of another length)
     }
   }
@@ -87,7 +91,7 @@ static Linear8Tile together_of(const GemmArgs& first, const GemmArgs& second, in
   double least = 4.0 + alone(first) + alone(second);
   for (int t = 0; t < kLinear8Tiles; ++t) {
     if (table_of(storage).pair[t] == nullptr) continue;
-    const TileCost& c = kCost[t];
+    const TileCost& c = costs_of(storage)[t];
     const auto tiles = [&](const GemmArgs& g) { return (double)((g.m + c.bm - 1) / c.bm * ((g.n + c.bn - 1) / c.bn)); };
     const double cus = (double)kCUs, n1 = tiles(first), n2 = tiles(second), per_cu = std::ceil((n1 + n2) / cus);
     const double full = (n1 * k1 + n2 * k2) / cus * c.each;

@@ -116,9 +116,10 @@ __device__ __forceinline__ f32x4 product16_wide(i32x8 a, i32x8 b) {
     c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen_codes(a, q), widen_codes(b, q), c, 0, 0, 0);
   return c;
 }
-// a block's sum of codes' products times its two powers of two, each the lowest byte
-__device__ __forceinline__ float scaled(float v, uint32_t sa, uint32_t sb) {
-  const int a = (int)(sa & 255), b = (int)(sb & 255);
+// whether one of a dword's bytes is the scale of a block that is not finite
+__device__ __forceinline__ bool has_nan_scale(uint32_t v) { return (((v & 0x7f7f7f7fu) + 0x01010101u) & v & 0x80808080u) != 0; }
+// a block's sum of codes' products times its two powers of two, or NaN
+__device__ __forceinline__ float scaled_or_nan(float v, int a, int b) {
   return a == kCkNaN || b == kCkNaN ? __uint_as_float(0x7fc00000u) : ldexpf(v, a + b - 254);
 }
 
@@ -246,14 +247,21 @@ __device__ __forceinline__ void linear_fp8_tile(const Gemm8Args& args, int id) {
           for (int e = 0; e < 16; ++e) block[i][j][e] = 0.f;
     }
   };
+  int odd_scales = 0;  // wide: whether this wave has a block that is not finite in this group of stages
   const auto add_block = [&] {
     if constexpr (WIDE) {
+      const auto each = [&](auto&& times) {
 #pragma unroll
-      for (int i = 0; i < FM; ++i)
+        for (int i = 0; i < FM; ++i) {
+          const int of_a = (int)(sa[i] & 255), power = of_a - 254;
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
+          for (int j = 0; j < FN; ++j)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) acc[i][j][e] += scaled(block[i][j][e], sa[i], sb[j][e]);
+            for (int e = 0; e < 16; ++e) acc[i][j][e] += times(block[i][j][e], of_a, power, (int)(sb[j][e] & 255));
+        }
+      };
+      if (__builtin_amdgcn_readfirstlane(odd_scales)) each([](float v, int a, int, int b) { return scaled_or_nan(v, a, b); });
+      else each([](float v, int, int power, int b) { return ldexpf(v, power + b); });
     }
   };
   const int steps = (int)((k1 - k0 + BK - 1) / BK), s0 = (int)(k0 / BK);
@@ -276,6 +284,16 @@ __device__ __forceinline__ void linear_fp8_tile(const Gemm8Args& args, int id) {
       const uint32_t* const of = p + Tile::SA + wn * TN + j * 32;
 #pragma unroll
       for (int e = 0; e < SBS; ++e) sb[j][e] = of[WIDE ? 8 * (e / 4) + 4 * (lane >> 5) + e % 4 : lane & 31];
+    }
+    if constexpr (WIDE) {
+      bool odd = false;
+#pragma unroll
+      for (int i = 0; i < FM; ++i) odd |= has_nan_scale(sa[i]);
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int e = 0; e < SBS; ++e) odd |= has_nan_scale(sb[j][e]);
+      odd_scales = __any(odd);
     }
   };
   const auto shift_scales = [&](int bits) {
@@ -666,7 +684,7 @@ __global__ void __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu
         if constexpr (WIDE) {
           const f32x4 block = product16_wide(vw[j], vx[i]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) acc[j][i][e] += scaled(block[e], sx[i], sw[j][e]);
+          for (int e = 0; e < 4; ++e) acc[j][i][e] += scaled_or_nan(block[e], (int)(sx[i] & 255), (int)(sw[j][e] & 255));
         } else {
           acc[j][i] = product16(vw[j], vx[i], acc[j][i], sw[j][0], sx[i]);
         }
@@ -718,14 +736,15 @@ Linear8Table make_linear_fp8_table() {
   t.fn[kTile8_32x64] = linear_fp8_launch<E, 32, 64, 1, 2, 3>;
   t.fn[kTile8_64] = linear_fp8_launch<E, 64, 64, 2, 2, 3>;
   t.fn[kTile8_64x128] = linear_fp8_launch<E, 64, 128, 2, 2, 3>;
-  t.fn[kTile8_128] = linear_fp8_launch<E, 128, 128, 2, 2, 2>;
-  t.fn[kTile8_128Deep] = linear_fp8_launch<E, 128, 128, 2, 2, 4>;
   t.pair[kTile8_64] = linear_fp8_pair_launch<E, 64, 64, 2, 2, 3>;
   t.pair[kTile8_64x128] = linear_fp8_pair_launch<E, 64, 128, 2, 2, 3>;
-  t.pair[kTile8_128] = linear_fp8_pair_launch<E, 128, 128, 2, 2, 2>;
+  // (the wide form needs registers for a block's sums and scales)
   if constexpr (E::kId != kStorageF32) {
+    t.fn[kTile8_128] = linear_fp8_launch<E, 128, 128, 2, 2, 2>;
+    t.fn[kTile8_128Deep] = linear_fp8_launch<E, 128, 128, 2, 2, 4>;
     t.fn[kTile8_128x256] = linear_fp8_launch<E, 128, 256, 2, 4, 3>;
     t.fn[kTile8_256] = linear_fp8_launch<E, 256, 256, 2, 4, 2>;
+    t.pair[kTile8_128] = linear_fp8_pair_launch<E, 128, 128, 2, 2, 2>;
   }
   t.few[0][0] = few_fp8_launch<E, 1, 1, 8, 2>;
   t.few[0][1] = few_fp8_launch<E, 1, 2, 8, 2>;
