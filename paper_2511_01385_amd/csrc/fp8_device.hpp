@@ -31,24 +31,37 @@ __device__ __forceinline__ int fp8_scale_byte(uint32_t amax) {
   const int s = (int)((amax + 0x1fffffu) >> 23) - 8;
   return amax >= 0x7f800000u ? kCkNaN : max(s, 0);
 }
-// Eight codes: hardware conversion, half to even, of x * 2^-e (at most 448, so nothing saturates).
-__device__ __forceinline__ Bytes8 fp8_encode(const float* v, int s) {
-  if (s == kCkNaN) return {{kFp8NaNs, kFp8NaNs}};
-  const float inv = ck_inverse(s);
-  Bytes8 r;
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h] * inv, v[4 * h + 1] * inv, 0, false);
-    r.w[h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h + 2] * inv, v[4 * h + 3] * inv, w, true);
-  }
-  return r;
-}
+// What the conversions take for a scale byte: the float 2^e, of which they look at the exponent alone (so 0 is 2^-127).
+__device__ __forceinline__ float fp8_scale(int s) { return __uint_as_float((uint32_t)s << 23); }
 
-// Four codes; NaN for `inverse`: of a block that is not finite.
-__device__ __forceinline__ uint32_t fp8_word(float a, float b, float c, float d, float inverse) {
-  const int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * inverse, b * inverse, 0, false);
-  const uint32_t r = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c * inverse, d * inverse, w, true);
-  return inverse != inverse ? kFp8NaNs : r;
+// Four codes of x / 2^e, half to even (at most 448, so nothing saturates): of floats, or of two pairs of 16-bit values.
+__device__ __forceinline__ uint32_t fp8_word(float a, float b, float c, float d, float scale) {
+  typedef short s16x2 __attribute__((ext_vector_type(2)));
+  s16x2 r = {0, 0};
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, a, b, scale, false);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, c, d, scale, true);
+  return __builtin_bit_cast(uint32_t, r);
+}
+template <class E>
+__device__ __forceinline__ uint32_t fp8_word(uint32_t ab, uint32_t cd, float scale) {
+  typedef short s16x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 b16x2 __attribute__((ext_vector_type(2)));
+  typedef _Float16 h16x2 __attribute__((ext_vector_type(2)));
+  s16x2 r = {0, 0};
+  if constexpr (E::kId == ElemBF16::kId) {
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(b16x2, ab), scale, false);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(b16x2, cd), scale, true);
+  } else {
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(r, __builtin_bit_cast(h16x2, ab), scale, false);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(r, __builtin_bit_cast(h16x2, cd), scale, true);
+  }
+  return __builtin_bit_cast(uint32_t, r);
+}
+// Eight codes; NaN for a block that is not finite.
+__device__ __forceinline__ Bytes8 fp8_encode(const float* v, int s) {
+  const float scale = fp8_scale(s);
+  const Bytes8 r = {{fp8_word(v[0], v[1], v[2], v[3], scale), fp8_word(v[4], v[5], v[6], v[7], scale)}};
+  return s == kCkNaN ? Bytes8{{kFp8NaNs, kFp8NaNs}} : r;
 }
 
 // Eight values.  Of a value within 1/32 of the type's largest number M the code can stand for the power of two past M: it

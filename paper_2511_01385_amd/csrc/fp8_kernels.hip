@@ -29,12 +29,87 @@ __device__ __forceinline__ uint32_t across_rows(uint32_t v, F&& fn) {
   return fn(far[0], far[1]);
 }
 
+// A thread's four rows by eight columns: as floats, or 16-bit values in the pairs they come in, for which the largest, the
+// conversion and the turn take two values an instruction.
+struct FloatRows {
+  static constexpr int kMaxima = kVec;  // words that hold eight columns' maxima
+  using Top = uint32_t;
+  float v[kFp8Rows][kVec];
+  __device__ __forceinline__ static uint32_t bits(uint32_t m) { return m; }  // a maximum as a float's bits
+  __device__ __forceinline__ uint32_t row_top(int r) const { return max_bits8(v[r]); }
+  __device__ __forceinline__ uint32_t column_tops(int i) const {
+    uint32_t m = abs_bits(v[0][i]);
+#pragma unroll
+    for (int r = 1; r < kFp8Rows; ++r) m = max(m, abs_bits(v[r][i]));
+    return across_rows(m, [](uint32_t a, uint32_t b) { return max(a, b); });
+  }
+  __device__ __forceinline__ Bytes8 row_codes(int r, int s) const { return fp8_encode(v[r], s); }
+  __device__ __forceinline__ uint32_t column_codes(int i, float scale) const {
+    return fp8_word(v[0][i], v[1][i], v[2][i], v[3][i], scale);
+  }
+  __device__ __forceinline__ void column_sums(float* s) const {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+      s[i] = v[0][i];
+#pragma unroll
+      for (int r = 1; r < kFp8Rows; ++r) s[i] += v[r][i];
+    }
+  }
+};
+template <class E>
+struct PairRows {
+  typedef unsigned short Pair __attribute__((ext_vector_type(2)));
+  static constexpr int kMaxima = kVec / 2;
+  using Top = uint16_t;
+  uint32_t p[kFp8Rows][kVec / 2];
+  __device__ __forceinline__ static uint32_t larger(uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(Pair, a), __builtin_bit_cast(Pair, b)));
+  }
+  __device__ __forceinline__ static uint32_t size(uint32_t w) { return w & 0x7fff7fffu; }
+  __device__ __forceinline__ static uint32_t bits(uint32_t m) {
+    if constexpr (E::kId == ElemBF16::kId) return m << 16;
+    else return __float_as_uint(E::get(reinterpret_cast<const uint16_t*>(&m)));
+  }
+  __device__ __forceinline__ uint32_t row_top(int r) const {
+    const uint32_t m = larger(larger(size(p[r][0]), size(p[r][1])), larger(size(p[r][2]), size(p[r][3])));
+    return bits(max(m & 0xffffu, m >> 16));
+  }
+  __device__ __forceinline__ uint32_t column_tops(int i) const {
+    uint32_t m = size(p[0][i]);
+#pragma unroll
+    for (int r = 1; r < kFp8Rows; ++r) m = larger(m, size(p[r][i]));
+    return across_rows(m, [](uint32_t a, uint32_t b) { return larger(a, b); });
+  }
+  __device__ __forceinline__ Bytes8 row_codes(int r, int s) const {
+    const float scale = fp8_scale(s);
+    const Bytes8 c = {{fp8_word<E>(p[r][0], p[r][1], scale), fp8_word<E>(p[r][2], p[r][3], scale)}};
+    return s == kCkNaN ? Bytes8{{kFp8NaNs, kFp8NaNs}} : c;
+  }
+  __device__ __forceinline__ uint32_t column_codes(int i, float scale) const {
+    const uint32_t half = i % 2 ? 0x07060302u : 0x05040100u;
+    return fp8_word<E>(__builtin_amdgcn_perm(p[1][i / 2], p[0][i / 2], half), __builtin_amdgcn_perm(p[3][i / 2], p[2][i / 2], half),
+                       scale);
+  }
+  __device__ __forceinline__ void column_sums(float* s) const {
+    float v[kVec];
+#pragma unroll
+    for (int r = 0; r < kFp8Rows; ++r) {
+      E::widen(typename E::Raw{{p[r][0], p[r][1], p[r][2], p[r][3]}}, v);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) s[i] = r == 0 ? v[i] : s[i] + v[i];
+    }
+  }
+};
+
 template <class E, bool EXACT, bool SLOPE>
 __global__ void __launch_bounds__(kFp8WG) fp8_quantize_kernel(Fp8Quantize q) {
   using T = typename E::T;
-  __shared__ uint32_t top[kFp8Waves][kFp8Block];
+  constexpr bool PAIRS = sizeof(T) == 2 && !SLOPE;
+  using Rows = std::conditional_t<PAIRS, PairRows<E>, FloatRows>;
+  using Top = typename Rows::Top;
+  __shared__ uint32_t top[kFp8Waves][kFp8Block * sizeof(Top) / 4];
   __shared__ float sums[kFp8Waves][kFp8Block];
-  __shared__ float inverse[kFp8Block];
+  __shared__ float scale_of[kFp8Block];
   __shared__ uint32_t tile_top[2], turned[kFp8Block * kFp8Pitch];
   const int thread = threadIdx.x, lane = thread & 63, wave = thread / 64;
   const int64_t first_row = (int64_t)blockIdx.y * kFp8Block, row0 = first_row + thread / kFp8Lanes * kFp8Rows;
@@ -42,15 +117,17 @@ __global__ void __launch_bounds__(kFp8WG) fp8_quantize_kernel(Fp8Quantize q) {
   const int64_t rows = q.rows, n = q.n;
   const T* const x = static_cast<const T*>(q.x);
 
-  float v[kFp8Rows][kVec];
+  Rows m;
   Bytes8 code[SLOPE ? kFp8Rows : 1];
   int byte[SLOPE ? kFp8Rows : 1];
-  if constexpr (EXACT) {
+  if constexpr (EXACT || PAIRS) {
     // (rows and columns past the ends load what is near, without a branch)
     typename E::Raw raw[kFp8Rows];
     const int64_t c = min(col, n - kVec);
+    if (EXACT || n >= kVec) {
 #pragma unroll
-    for (int r = 0; r < kFp8Rows; ++r) raw[r] = E::load(x + min(row0 + r, rows - 1) * q.ldx + c);
+      for (int r = 0; r < kFp8Rows; ++r) raw[r] = E::load(x + min(row0 + r, rows - 1) * q.ldx + c);
+    }
     if constexpr (SLOPE) {
       const int64_t blocks = (n + kCkBlock - 1) / kCkBlock;
 #pragma unroll
@@ -62,20 +139,38 @@ __global__ void __launch_bounds__(kFp8WG) fp8_quantize_kernel(Fp8Quantize q) {
     }
 #pragma unroll
     for (int r = 0; r < kFp8Rows; ++r) {
-      E::widen(raw[r], v[r]);
       const bool in = row0 + r < rows && col < n;
+      if constexpr (PAIRS) {
+        u32x4 w = {raw[r].w[0], raw[r].w[1], raw[r].w[2], raw[r].w[3]};
+        if constexpr (!EXACT) {
+          if (n < kVec) {
+            const T* const row = x + min(row0 + r, rows - 1) * q.ldx;
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) v[r][i] = in ? v[r][i] : 0.f;
+            for (int i = 0; i < kVec; i += 2) {
+              const uint32_t a = i < n ? row[min((int64_t)i, n - 1)] : 0, b = i + 1 < n ? row[min((int64_t)i + 1, n - 1)] : 0;
+              w[i / 2] = a | b << 16;
+            }
+          } else if (col + kVec > n) {  // the row's end cuts this group: it was loaded so as to end there
+            w = drop_bytes(w, (int)min(col + kVec - n, (int64_t)(kVec - 1)) * 2);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m.p[r][i] = in ? w[i] : 0u;
+      } else {
+        E::widen(raw[r], m.v[r]);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) m.v[r][i] = in ? m.v[r][i] : 0.f;
+      }
     }
   } else {
 #pragma unroll
     for (int r = 0; r < kFp8Rows; ++r) {
       const bool in = row0 + r < rows && col < n;
       if (in) {
-        read_group<E>(x + (row0 + r) * q.ldx, col, n, v[r]);
+        read_group<E>(x + (row0 + r) * q.ldx, col, n, m.v[r]);
       } else {
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) v[r][i] = 0.f;
+        for (int i = 0; i < kVec; ++i) m.v[r][i] = 0.f;
       }
       if constexpr (SLOPE) {
         code[r] = {{0, 0}};
@@ -93,17 +188,15 @@ __global__ void __launch_bounds__(kFp8WG) fp8_quantize_kernel(Fp8Quantize q) {
       if (row0 + r >= rows || col >= n) continue;
       float z[kVec];
       ck_decode<ElemF32>(code[r], ck_scale(byte[r]), z);
-      times_slope8(q.act, z, v[r]);
+      times_slope8(q.act, z, m.v[r]);
     }
   }
   const bool by_sums = q.sums != nullptr || q.total != nullptr;
   if (by_sums) {
     float s[kVec];
+    m.column_sums(s);
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
-      s[i] = v[0][i];
-#pragma unroll
-      for (int r = 1; r < kFp8Rows; ++r) s[i] += v[r][i];
       s[i] = __uint_as_float(across_rows(__float_as_uint(s[i]), [](uint32_t a, uint32_t b) {
         return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
       }));
@@ -116,17 +209,12 @@ __global__ void __launch_bounds__(kFp8WG) fp8_quantize_kernel(Fp8Quantize q) {
   // the largest of each column
   const bool by_column = q.columns.codes != nullptr || q.tiles;
   if (by_column) {
-    uint32_t m[kVec];
+    uint32_t t[Rows::kMaxima];
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-      m[i] = abs_bits(v[0][i]);
-#pragma unroll
-      for (int r = 1; r < kFp8Rows; ++r) m[i] = max(m[i], abs_bits(v[r][i]));
-      m[i] = across_rows(m[i], [](uint32_t a, uint32_t b) { return max(a, b); });
-    }
+    for (int i = 0; i < Rows::kMaxima; ++i) t[i] = m.column_tops(i);
     if (lane < kFp8Lanes) {
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) top[wave][lane * kVec + i] = m[i];
+      for (int i = 0; i < Rows::kMaxima; ++i) top[wave][lane * Rows::kMaxima + i] = t[i];
     }
   }
   if (by_column || by_sums) __syncthreads();
@@ -139,16 +227,17 @@ __global__ void __launch_bounds__(kFp8WG) fp8_quantize_kernel(Fp8Quantize q) {
       else q.sums[(int64_t)blockIdx.y * n + col0 + thread] = s;
     }
     if (by_column) {
-      uint32_t m = top[0][thread];
+      uint32_t t = reinterpret_cast<const Top*>(top[0])[thread];
 #pragma unroll
-      for (int w = 1; w < kFp8Waves; ++w) m = max(m, top[w][thread]);
+      for (int w = 1; w < kFp8Waves; ++w) t = max(t, (uint32_t)reinterpret_cast<const Top*>(top[w])[thread]);
+      t = Rows::bits(t);
       if (q.tiles) {
-        m = row_max(m);
-        m = across_rows(m, [](uint32_t a, uint32_t b) { return max(a, b); });
-        if (lane == 0) tile_top[wave] = m;
+        t = row_max(t);
+        t = across_rows(t, [](uint32_t a, uint32_t b) { return max(a, b); });
+        if (lane == 0) tile_top[wave] = t;
       } else {
-        const int s = fp8_scale_byte(m);
-        inverse[thread] = s == kCkNaN ? __uint_as_float(0x7fc00000u) : ck_inverse(s);
+        const int s = fp8_scale_byte(t);
+        scale_of[thread] = fp8_scale(s);
         if (col0 + thread < n) q.columns.scales[(col0 + thread) * q.columns.lds + blockIdx.y] = (uint8_t)s;
       }
     }
@@ -165,19 +254,20 @@ __global__ void __launch_bounds__(kFp8WG) fp8_quantize_kernel(Fp8Quantize q) {
     }
   }
   if (q.columns.codes != nullptr) {
-    const float all = tile == kCkNaN ? __uint_as_float(0x7fc00000u) : ck_inverse(tile);
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
       const int c = thread % kFp8Lanes * kVec + i;
-      turned[c * kFp8Pitch + thread / kFp8Lanes] = fp8_word(v[0][i], v[1][i], v[2][i], v[3][i], q.tiles ? all : inverse[c]);
+      const float scale = q.tiles ? fp8_scale(tile) : scale_of[c];
+      const uint32_t w = m.column_codes(i, scale);
+      turned[c * kFp8Pitch + thread / kFp8Lanes] = scale == __builtin_inff() ? kFp8NaNs : w;  // (byte 255)
     }
   }
   if (q.held.codes != nullptr) {
 #pragma unroll
     for (int r = 0; r < kFp8Rows; ++r) {
-      const int s = q.tiles ? tile : fp8_scale_byte(row_max(max_bits8(v[r])));
+      const int s = q.tiles ? tile : fp8_scale_byte(row_max(m.row_top(r)));
       if (row0 + r >= rows || col >= n) continue;
-      write_bytes(q.held.codes + (row0 + r) * q.held.ld, col, n, fp8_encode(v[r], s));
+      write_bytes(q.held.codes + (row0 + r) * q.held.ld, col, n, m.row_codes(r, s));
       if (!q.tiles && thread % kFp8Lanes == 0) q.held.scales[(row0 + r) * q.held.lds + blockIdx.x] = (uint8_t)s;
     }
   }
