@@ -82,7 +82,19 @@ struct Gemm8Args {
   GemmArgs g;  // (a, b, lda and ldb are not used)
   Fp8Operand a, b;
 };
-enum Linear8Tile { kTile8_32x64, kTile8_64, kTile8_64x128, kTile8_128, kTile8_128Deep, kTile8_128x256, kTile8_256, kLinear8Tiles };
+// K2, K4: two or four groups of waves, each with stages of its own
+enum Linear8Tile {
+  kTile8_32x64,
+  kTile8_64,
+  kTile8_64x128,
+  kTile8_32x64K4,
+  kTile8_64x128K2,
+  kTile8_128,
+  kTile8_128K2,
+  kTile8_128x256,
+  kTile8_256,
+  kLinear8Tiles
+};
 using Linear8Fn = hipError_t (*)(const Gemm8Args&, hipStream_t);
 using Linear8PairFn = hipError_t (*)(const Gemm8Args&, const Gemm8Args&, hipStream_t);
 struct Linear8Table {

@@ -21,12 +21,14 @@ struct TileCost {
   int bm, bn, together;
   double alone, each, ends;
 };
-constexpr TileCost kCost16[kLinear8Tiles] = {{32, 64, 4, 0.19, 0.145, 2.5},  {64, 64, 3, 0.205, 0.20, 3.0},
-                                           {64, 128, 2, 0.29, 0.31, 3.0},  {128, 128, 2, 0.68, 0.49, 3.5},
-                                           {128, 128, 1, 0.55, 0.60, 3.0}, {128, 256, 1, 0.80, 0.80, 4.9},
-                                           {256, 256, 1, 1.46, 1.46, 7.2}};
+constexpr TileCost kCost16[kLinear8Tiles] = {{32, 64, 4, 0.20, 0.155, 1.6}, {64, 64, 3, 0.21, 0.205, 1.8},
+                                             {64, 128, 2, 0.29, 0.33, 2.5}, {32, 64, 1, 0.125, 0.20, 2.0},
+                                             {64, 128, 1, 0.25, 0.36, 2.8}, {128, 128, 2, 0.62, 0.49, 3.5},
+                                             {128, 128, 1, 0.52, 0.60, 3.8}, {128, 256, 1, 0.80, 0.80, 4.9},
+                                             {256, 256, 1, 1.46, 1.46, 7.2}};
 // float32 results
-constexpr TileCost kCost32[] = {{32, 64, 4, 0.24, 0.32, 2.5}, {64, 64, 3, 0.45, 0.45, 3.0}, {64, 128, 2, 0.85, 0.80, 3.0}};
+constexpr TileCost kCost32[] = {{32, 64, 4, 0.50, 0.31, 2.0}, {64, 64, 3, 0.60, 0.45, 2.0}, {64, 128, 2, 0.85, 0.80, 2.5},
+                                {32, 64, 1, 0.22, 0.50, 2.5}, {64, 128, 1, 0.78, 0.85, 3.0}};
 static const TileCost* costs_of(int storage) { return storage == kStorageF32 ? kCost32 : kCost16; }
 
 static const Linear8Table& table_of(int storage) {

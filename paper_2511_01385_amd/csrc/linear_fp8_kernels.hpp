@@ -37,7 +37,8 @@ struct ElemCode {
 // R rows of one operand's stage on their way to LDS, as Operand of linear_kernels.hpp loads them, in fewer registers:
 // a lane's part of line j lies 8 j rows below that of line 0, in the same chunk, and rows past the last are out of the
 // buffer's bounds.
-template <int R, int WAVES>
+// GROUPS: the stages that a step takes.
+template <int R, int WAVES, int GROUPS = 1>
 struct CodeOperand {
   static constexpr int BYTES = R * kStageBytes, LINES = BYTES / 1024 / WAVES;
   static_assert(LINES * WAVES * 1024 == BYTES);
@@ -59,15 +60,15 @@ struct CodeOperand {
     offset = (uint32_t)(wave * LINES * 8 + lane / 8) * ld + (uint32_t)chunk * 16u;
   }
   // (a row's last chunk counts whole)
-  __device__ __forceinline__ int records() const { return (int)(above + ((uint32_t)depth + 15) / 16 * 16); }
+  __device__ __forceinline__ int records() const { return depth > 0 ? (int)(above + ((uint32_t)depth + 15) / 16 * 16) : 0; }
   // line j of a stage in front of the end of k; step() after the last
   __device__ __forceinline__ void fetch_line(int j, uint32_t lds) const {
     load_to_lds<16>(reinterpret_cast<const char*>(base), offset + (uint32_t)(8 * j) * ld, lds + (uint32_t)(wave * LINES + j) * 1024u,
                     records());
   }
   __device__ __forceinline__ void step() {
-    base += kStageBytes;
-    depth -= kStageBytes;
+    base += GROUPS * kStageBytes;
+    depth -= GROUPS * kStageBytes;
   }
   // any stage: chunks past the end of k are zeros
   __device__ __forceinline__ void fetch(uint32_t lds) {
@@ -169,28 +170,33 @@ __device__ __forceinline__ void fetch_scales(const Fp8Operand& o, int64_t r0, in
   load_to_lds<4>(reinterpret_cast<const char*>(o.scales) + first * o.lds, r < r_end ? at : kNowhere, lds);
 }
 
-template <class E, int BM, int BN, int WM, int WN, int STAGES>
+template <class E, int BM, int BN, int WM, int WN, int STAGES, int KG>
 struct Fp8Tile {
-  static constexpr int WAVES = WM * WN;
+  static constexpr int THREADS = WM * WN * KG * 64;
   static constexpr int STAGE = (BM + BN) * kStageBytes;
   // rows of scales, in whole loads of 64
   static constexpr int SA = (BM + 63) / 64 * 64, SB = (BN + 63) / 64 * 64, SLOT = (SA + SB) * 4;
-  static constexpr int LDS = STAGES * STAGE + 2 * SLOT;
+  static constexpr int SLOTS = 4;
+  static constexpr int LDS = STAGES * KG * STAGE + SLOTS * SLOT;
+  static_assert(LDS <= 160 * 1024);
 };
 
-template <class E, int BM, int BN, int WM, int WN, int STAGES>
+// KG groups of WM x WN waves share the tile: of a step's KG stages each multiplies its own, and their sums meet in LDS at
+// the end.  A step of several stages costs little more than one where nothing but its own latency holds it up: where a CU
+// has one workgroup, and small tiles.
+template <class E, int BM, int BN, int WM, int WN, int STAGES, int KG>
 __device__ __forceinline__ void linear_fp8_tile(const Gemm8Args& args, int id) {
-  using Tile = Fp8Tile<E, BM, BN, WM, WN, STAGES>;
+  using Tile = Fp8Tile<E, BM, BN, WM, WN, STAGES, KG>;
   GemmArgs g = args.g;
   constexpr bool WIDE = E::kId == kStorageF32;
   constexpr int WAVES = WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32;
   constexpr int BK = kStageBytes, STAGE = Tile::STAGE;
-  static_assert(STAGES <= 4);
   constexpr bool STREAM = FM >= 4 && !WIDE;  // fragments of A one at a time: two halves of a stage take too many registers
-  using OpA = CodeOperand<BM, WAVES>;
-  using OpB = CodeOperand<BN, WAVES>;
+  using OpA = CodeOperand<BM, WAVES, KG>;
+  using OpB = CodeOperand<BN, WAVES, KG>;
   extern __shared__ __attribute__((aligned(1024))) char linear_lds[];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
+  const int lane = threadIdx.x & 63, any_wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
+  const int kg = any_wave / WAVES, wave = any_wave % WAVES;
   const int wm = wave / WN, wn = wave % WN;
   const TileAt at = tile_of(id, g.tiles_m, g.tiles_n, g.splits);
   const int64_t m0 = (int64_t)at.tm * BM, n0 = (int64_t)at.tn * BN;
@@ -198,8 +204,8 @@ __device__ __forceinline__ void linear_fp8_tile(const Gemm8Args& args, int id) {
 
   OpA a;
   OpB b;
-  a.init(args.a, m0, g.m, k0, k1, wave, lane);
-  b.init(args.b, n0, g.n, k0, k1, wave, lane);
+  a.init(args.a, m0, g.m, k0 + kg * BK, k1, wave, lane);
+  b.init(args.b, n0, g.n, k0 + kg * BK, k1, wave, lane);
   Fragments32 fa, fb;
   fa.init(wm * TM, lane);
   fb.init(wn * TN, lane);
@@ -264,19 +270,20 @@ __device__ __forceinline__ void linear_fp8_tile(const Gemm8Args& args, int id) {
       else each([](float v, int, int power, int b) { return ldexpf(v, power + b); });
     }
   };
-  const int steps = (int)((k1 - k0 + BK - 1) / BK), s0 = (int)(k0 / BK);
+  const int stages = (int)((k1 - k0 + BK - 1) / BK), steps = (stages + KG - 1) / KG, s0 = (int)(k0 / BK);
   const int groups = (int)((k1 + 4 * BK - 1) / (4 * BK));
+  constexpr int SCALES = STAGES * KG * STAGE;  // where they lie in LDS
   // the scales of a group of four stages on their way to its slot
   const auto fetch_group = [&](int group) {
     if (group >= groups) return;
-    const uint32_t slot = lds0 + STAGES * STAGE + (uint32_t)(group & 1) * Tile::SLOT;
-    for (int q = wave; q < (Tile::SA + Tile::SB) / 64; q += WAVES) {
+    const uint32_t slot = lds0 + SCALES + (uint32_t)(group & (Tile::SLOTS - 1)) * Tile::SLOT;
+    for (int q = any_wave; q < (Tile::SA + Tile::SB) / 64; q += WAVES * KG) {
       if (q < Tile::SA / 64) fetch_scales(args.a, m0, g.m, q * 64, group, slot + (uint32_t)q * 256u, lane);
       else fetch_scales(args.b, n0, g.n, q * 64 - Tile::SA, group, slot + (uint32_t)q * 256u, lane);
     }
   };
   const auto take_group = [&](int group) {
-    const uint32_t* const p = reinterpret_cast<const uint32_t*>(linear_lds + STAGES * STAGE + (group & 1) * Tile::SLOT);
+    const uint32_t* const p = reinterpret_cast<const uint32_t*>(linear_lds + SCALES + (group & (Tile::SLOTS - 1)) * Tile::SLOT);
 #pragma unroll
     for (int i = 0; i < FM; ++i) sa[i] = p[wm * TM + i * 32 + (lane & 31)];
 #pragma unroll
@@ -304,35 +311,39 @@ __device__ __forceinline__ void linear_fp8_tile(const Gemm8Args& args, int id) {
 #pragma unroll
       for (int e = 0; e < SBS; ++e) sb[j][e] >>= bits;
   };
-  // stage t's scales into the lowest place.  At the first of a group the next group sets out: into the slot that
-  // every wave has read at the start of the group before, with a barrier in each stage since.
+  // Step t's scales into the lowest place.  Three groups beyond the one that the step begins in are there or on their way, in
+  // four slots: a step and the next reach into two of them, and the slot that is filled anew was last read at the
+  // start of the step before, with a barrier since.
   const auto scales_of = [&](int t) {
     if (t == 0) return;
-    if (((s0 + t) & 3) == 0) {
-      const int group = (s0 + t) >> 2;
-      take_group(group);
-      fetch_group(group + 1);
+    const int first = s0 + t * KG, s = first + kg;
+    if ((s & 3) < KG) {
+      take_group(s >> 2);
+      if (KG > 1) shift_scales((s & 3) * 8);
     } else {
-      shift_scales(8);
+      shift_scales(8 * KG);
     }
+    if ((first & 3) < KG) fetch_group((first >> 2) + 3);
   };
+  static_assert(STAGES <= 3, "a group of scales has landed by the step that takes it");
   // STAGES - 1 stages are under way ahead of the one being multiplied; the barrier sits between a stage's halves.
   constexpr int EACH = OpA::LINES + OpB::LINES;
   const auto fetch = [&](int slot) {
-    a.fetch(lds0 + (uint32_t)slot * STAGE);
-    b.fetch(lds0 + (uint32_t)slot * STAGE + OpA::BYTES);
+    a.fetch(lds0 + (uint32_t)(slot * KG + kg) * STAGE);
+    b.fetch(lds0 + (uint32_t)(slot * KG + kg) * STAGE + OpA::BYTES);
   };
   const int tail = (int)((k1 - k0) % BK);
   const auto cut = [&](int slot) {
     if (tail % 16 == 0) return;
-    cut_stage(linear_lds + slot * STAGE, BM + BN, tail, (int)threadIdx.x, WAVES * 64);  // (BM is a multiple of eight rows)
+    cut_stage(linear_lds + (slot * KG + (stages - 1) % KG) * STAGE, BM + BN, tail, (int)threadIdx.x,
+              Tile::THREADS);  // (BM is a multiple of eight rows)
     reads_wait();
     wave_barrier();
   };
   // One half's products with the other's reads and a stage's loads between them, a row of fragments at a time.
   const auto weave = [&](const Half& h, Half& to, const char* from, int slot) {
     constexpr int TOTAL = FM + FN;
-    const uint32_t la = lds0 + (uint32_t)slot * STAGE, lb = la + OpA::BYTES;
+    const uint32_t la = lds0 + (uint32_t)(slot * KG + kg) * STAGE, lb = la + OpA::BYTES;
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
 #pragma unroll
@@ -355,6 +366,7 @@ __device__ __forceinline__ void linear_fp8_tile(const Gemm8Args& args, int id) {
     a.step();
     b.step();
   };
+  constexpr bool SMALL = FM * FN <= 2;
   constexpr int PRODUCTS = FM * FN * (WIDE ? 4 : 1), READS = 2 * (FM + FN);
   const auto interleave = [&] {
     constexpr int GROUPS = READS < PRODUCTS ? READS : PRODUCTS;
@@ -366,8 +378,7 @@ __device__ __forceinline__ void linear_fp8_tile(const Gemm8Args& args, int id) {
   };
   if (steps > 0) {
     // (older than the stages, so that the waits for those cover them)
-    fetch_group(s0 >> 2);
-    fetch_group((s0 >> 2) + 1);
+    for (int q = 0; q < Tile::SLOTS; ++q) fetch_group((s0 >> 2) + q);
   }
 #pragma unroll
   for (int q = 0; q < STAGES; ++q)
@@ -376,13 +387,14 @@ __device__ __forceinline__ void linear_fp8_tile(const Gemm8Args& args, int id) {
     if (steps >= STAGES) stage_wait<(STAGES - 1) * EACH>();
     else stage_wait<0>();
     if (steps == 1) cut(0);
-    take_group(s0 >> 2);
-    shift_scales((s0 & 3) * 8);
+    take_group((s0 + kg) >> 2);
+    shift_scales(((s0 + kg) & 3) * 8);
   }
   int cur = 0, t = 0;
   const auto next = [](int slot) { return slot + 1 == STAGES ? 0 : slot + 1; };
   const int steady = steps - 1 - STAGES;  // (the stage that is fetched is not the last)
   if constexpr (STREAM) {
+    static_assert(KG == 1);
     // Fragments of A come one at a time, AHEAD steps before their products, into a ring; those of B half a stage
     // before.  The barrier comes when the stage's last fragment is read, AHEAD steps before its end.
     constexpr int STEPS = 2 * FM, AHEAD = 3, RING = 4, LAST = STEPS - AHEAD;
@@ -449,46 +461,88 @@ __device__ __forceinline__ void linear_fp8_tile(const Gemm8Args& args, int id) {
 #pragma unroll 1
     for (; t < steps; ++t) stage(std::false_type{});
   } else {
+    const auto place = [&](int slot) { return linear_lds + (slot * KG + kg) * STAGE; };
     Half h0, h1;
-    if (steps > 0) read(h0, linear_lds, 0);
+    if (steps > 0) read(h0, place(0), 0);
     for (; t < steady; ++t) {
+      // (few products: the reads go first, else they would set out behind products that wait for the half before)
+      if (SMALL) {
+        read(h1, place(cur), 1);
+        __builtin_amdgcn_sched_barrier(0);
+      }
       scales_of(t);
       clear_block();
-      read(h1, linear_lds + cur * STAGE, 1);
+      if (!SMALL) read(h1, place(cur), 1);
       multiply(h0);
-      interleave();
+      if (!SMALL) interleave();
       stage_wait<(STAGES - 2) * EACH>();
-      weave(h1, h0, linear_lds + next(cur) * STAGE, cur);
+      weave(h1, h0, place(next(cur)), cur);
       add_block();
       cur = next(cur);
     }
     for (; t < steps; ++t) {
+      const bool mine = KG == 1 || t * KG + kg < stages;  // (the last step may have no stage for this group)
+      read(h1, place(cur), 1);
       scales_of(t);
-      read(h1, linear_lds + cur * STAGE, 1);
       clear_block();
-      multiply(h0);
+      if (mine) multiply(h0);
       if (t + 1 < steps) {
         // this stage is read; the next has landed when those after it are all that is left
-        const int after = steps - t - 2;
-        if (STAGES > 3 && after >= 2) stage_wait<(STAGES > 3 ? 2 : 0) * EACH>();
-        else if (STAGES > 2 && after >= 1) stage_wait<(STAGES > 2 ? 1 : 0) * EACH>();
+        if (STAGES > 2 && t + STAGES - 1 < steps) stage_wait<(STAGES - 2) * EACH>();
         else stage_wait<0>();
         if (t + STAGES < steps) fetch(cur);
         cur = next(cur);
         if (t + 2 == steps) cut(cur);
-        read(h0, linear_lds + cur * STAGE, 0);
+        read(h0, place(cur), 0);
       }
-      multiply(h1);
-      add_block();
+      if (mine) {
+        multiply(h1);
+        add_block();
+      }
     }
   }
   stage_wait<0>();
 
+  // the groups' sums, in their order
+  constexpr int MEET = (KG - 1) * BM * BN * 4;
+  if constexpr (KG > 1) {
+    const auto sums_of = [&](int group) {
+      return reinterpret_cast<f32x4*>(linear_lds + ((group - 1) * WAVES + wave) * (TM * TN * 4)) + lane;
+    };
+    if (kg > 0) {
+      f32x4* const p = sums_of(kg);
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            p[((i * FN + j) * 4 + q) * 64] =
+                f32x4{acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
+    }
+    __syncthreads();
+    if (kg > 0) return;
+#pragma unroll
+    for (int o = 1; o < KG; ++o) {
+      const f32x4* const p = sums_of(o);
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const f32x4 v = p[((i * FN + j) * 4 + q) * 64];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][j][q * 4 + e] += v[e];
+          }
+    }
+  }
+
   // Each wave turns its results through LDS of its own, 32 rows at a time, into runs of eight along n: the lanes of a row
   // then read and write whole cache lines.  16 bytes c of a row lie at (c / 2, odd ones in the second half) xor row.
   constexpr int CH = TN / 4, RUNS = TN / kVec, ROWS = 64 / RUNS, PASSES = 32 / ROWS;
-  static_assert(WAVES * 32 * TN * 4 <= STAGES * STAGE && 32 % ROWS == 0);
-  char* const turn = linear_lds + wave * (32 * TN * 4);
+  static_assert(MEET + WAVES * 32 * TN * 4 <= STAGES * KG * STAGE && 32 % ROWS == 0);
+  char* const turn = linear_lds + MEET + wave * (32 * TN * 4);
   const auto slot = [](int row, int c) { return (row * CH + (((c >> 1) | (c & 1) * (CH / 2)) ^ (row & (CH - 1)))) * 16; };
   const int64_t n = n0 + wn * TN + lane % RUNS * kVec;
   float bias[kVec];
@@ -529,24 +583,23 @@ __device__ __forceinline__ void linear_fp8_tile(const Gemm8Args& args, int id) {
   }
 }
 
-template <class E, int BM, int BN, int WM, int WN, int STAGES>
-__global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_eu(BM / WM * BN / WN > 128 * 64 ? 1 : 2)))
+template <class E, int BM, int BN, int WM, int WN, int STAGES, int KG>
+__global__ void __launch_bounds__(WM * WN * KG * 64) __attribute__((amdgpu_waves_per_eu(2)))
     linear_fp8_kernel(Gemm8Args args) {
-  linear_fp8_tile<E, BM, BN, WM, WN, STAGES>(args, (int)blockIdx.x);
+  linear_fp8_tile<E, BM, BN, WM, WN, STAGES, KG>(args, (int)blockIdx.x);
 }
 
-template <class E, int BM, int BN, int WM, int WN, int STAGES>
+template <class E, int BM, int BN, int WM, int WN, int STAGES, int KG = 1>
 hipError_t linear_fp8_launch(const Gemm8Args& args, hipStream_t stream) {
-  constexpr int lds = Fp8Tile<E, BM, BN, WM, WN, STAGES>::LDS;
-  static_assert(lds <= 160 * 1024);
-  const auto kernel = linear_fp8_kernel<E, BM, BN, WM, WN, STAGES>;
+  constexpr int lds = Fp8Tile<E, BM, BN, WM, WN, STAGES, KG>::LDS;
+  const auto kernel = linear_fp8_kernel<E, BM, BN, WM, WN, STAGES, KG>;
   static const hipError_t ready = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                                       hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (ready != hipSuccess) return ready;
   Gemm8Args t = args;
   t.g.tiles_m = (int)((args.g.m + BM - 1) / BM);
   t.g.tiles_n = (int)((args.g.n + BN - 1) / BN);
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(t.g.tiles_m * t.g.tiles_n * t.g.splits)), dim3(WM * WN * 64), lds, stream, t);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(t.g.tiles_m * t.g.tiles_n * t.g.splits)), dim3(WM * WN * KG * 64), lds, stream, t);
   return hipGetLastError();
 }
 
@@ -557,13 +610,12 @@ __global__ void __launch_bounds__(WM * WN * 64) __attribute__((amdgpu_waves_per_
     linear_fp8_pair_kernel(Gemm8Args first, Gemm8Args second) {
   const int id = (int)blockIdx.x, tiles = first.g.tiles_m * first.g.tiles_n;
   // (the same code for both: they differ in their arguments alone)
-  linear_fp8_tile<E, BM, BN, WM, WN, STAGES>(id < tiles ? first : second, id < tiles ? id : id - tiles);
+  linear_fp8_tile<E, BM, BN, WM, WN, STAGES, 1>(id < tiles ? first : second, id < tiles ? id : id - tiles);
 }
 
 template <class E, int BM, int BN, int WM, int WN, int STAGES>
 hipError_t linear_fp8_pair_launch(const Gemm8Args& first, const Gemm8Args& second, hipStream_t stream) {
-  constexpr int lds = Fp8Tile<E, BM, BN, WM, WN, STAGES>::LDS;
-  static_assert(lds <= 160 * 1024);
+  constexpr int lds = Fp8Tile<E, BM, BN, WM, WN, STAGES, 1>::LDS;
   const auto kernel = linear_fp8_pair_kernel<E, BM, BN, WM, WN, STAGES>;
   static const hipError_t ready = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                                       hipFuncAttributeMaxDynamicSharedMemorySize, lds);
@@ -736,12 +788,14 @@ Linear8Table make_linear_fp8_table() {
   t.fn[kTile8_32x64] = linear_fp8_launch<E, 32, 64, 1, 2, 3>;
   t.fn[kTile8_64] = linear_fp8_launch<E, 64, 64, 2, 2, 3>;
   t.fn[kTile8_64x128] = linear_fp8_launch<E, 64, 128, 2, 2, 3>;
+  t.fn[kTile8_32x64K4] = linear_fp8_launch<E, 32, 64, 1, 2, 2, 4>;
+  t.fn[kTile8_64x128K2] = linear_fp8_launch<E, 64, 128, 2, 2, 2, 2>;
   t.pair[kTile8_64] = linear_fp8_pair_launch<E, 64, 64, 2, 2, 3>;
   t.pair[kTile8_64x128] = linear_fp8_pair_launch<E, 64, 128, 2, 2, 3>;
   // (the wide form needs registers for a block's sums and scales)
   if constexpr (E::kId != kStorageF32) {
     t.fn[kTile8_128] = linear_fp8_launch<E, 128, 128, 2, 2, 2>;
-    t.fn[kTile8_128Deep] = linear_fp8_launch<E, 128, 128, 2, 2, 4>;
+    t.fn[kTile8_128K2] = linear_fp8_launch<E, 128, 128, 2, 2, 2, 2>;
     t.fn[kTile8_128x256] = linear_fp8_launch<E, 128, 256, 2, 4, 3>;
     t.fn[kTile8_256] = linear_fp8_launch<E, 256, 256, 2, 4, 2>;
     t.pair[kTile8_128] = linear_fp8_pair_launch<E, 128, 128, 2, 2, 2>;
