@@ -34,19 +34,28 @@ struct ElemCode {
   using T = uint8_t;
 };
 
+// Which chunk of LDS row r holds the row's chunk c: c ^ code_swizzle(r).  A read of 16 bytes a lane is done 16 lanes at a
+// time, lanes 0-3, 12-15, 20-27 and the like: with 32 rows to a fragment those are rows of which two agree modulo eight, and
+// bit 3 of the row keeps them apart (without it half of the cycles that the LDS was busy were conflicts).  With 16 rows to a
+// fragment the lanes' two chunks do.
+template <int FRAGMENT>
+__device__ __forceinline__ int code_swizzle(int r) {
+  return FRAGMENT == 32 ? (r & 7) ^ (r >> 3 & 1) : r & 7;
+}
+
 // R rows of one operand's stage on their way to LDS, as Operand of linear_kernels.hpp loads them, in fewer registers:
-// a lane's part of line j lies 8 j rows below that of line 0, in the same chunk, and rows past the last are out of the
-// buffer's bounds.
+// a lane's part of line j lies 8 j rows below that of line 0, in the same chunk or its neighbour, and rows past the last are
+// out of the buffer's bounds.
 // GROUPS: the stages that a step takes.
-template <int R, int WAVES, int GROUPS = 1>
+template <int R, int WAVES, int FRAGMENT, int GROUPS = 1>
 struct CodeOperand {
   static constexpr int BYTES = R * kStageBytes, LINES = BYTES / 1024 / WAVES;
-  static_assert(LINES * WAVES * 1024 == BYTES);
+  static_assert(LINES * WAVES * 1024 == BYTES && LINES % 2 == 0, "lines' parities are those of j");
   const uint8_t* base;  // row 0 and this stage's k 0 of the tile
   uint32_t ld, offset;  // bytes from row to row; of this lane's part of line 0
   uint32_t above;       // bytes of the rows that exist but for the last
   int depth;            // k that is left
-  int chunk, wave;
+  int chunk, wave;      // chunk: of line 0
 
   __device__ __forceinline__ void init(const Fp8Operand& o, int64_t r0, int64_t r_end, int64_t k0, int64_t k_end, int wave_,
                                        int lane) {
@@ -63,8 +72,11 @@ struct CodeOperand {
   __device__ __forceinline__ int records() const { return depth > 0 ? (int)(above + ((uint32_t)depth + 15) / 16 * 16) : 0; }
   // line j of a stage in front of the end of k; step() after the last
   __device__ __forceinline__ void fetch_line(int j, uint32_t lds) const {
-    load_to_lds<16>(reinterpret_cast<const char*>(base), offset + (uint32_t)(8 * j) * ld, lds + (uint32_t)(wave * LINES + j) * 1024u,
-                    records());
+    load_to_lds<16>(reinterpret_cast<const char*>(base), at(j), lds + (uint32_t)(wave * LINES + j) * 1024u, records());
+  }
+  __device__ __forceinline__ int chunk_of(int j) const { return FRAGMENT == 32 ? chunk ^ (j & 1) : chunk; }
+  __device__ __forceinline__ uint32_t at(int j) const {
+    return offset + (uint32_t)(8 * j) * ld + (uint32_t)((chunk_of(j) - chunk) * 16);
   }
   __device__ __forceinline__ void step() {
     base += GROUPS * kStageBytes;
@@ -72,10 +84,9 @@ struct CodeOperand {
   }
   // any stage: chunks past the end of k are zeros
   __device__ __forceinline__ void fetch(uint32_t lds) {
-    const bool in = chunk * 16 < depth;
 #pragma unroll
     for (int j = 0; j < LINES; ++j)
-      load_to_lds<16>(reinterpret_cast<const char*>(base), in ? offset + (uint32_t)(8 * j) * ld : kNowhere,
+      load_to_lds<16>(reinterpret_cast<const char*>(base), chunk_of(j) * 16 < depth ? at(j) : kNowhere,
                       lds + (uint32_t)(wave * LINES + j) * 1024u, records());
     step();
   }
@@ -132,7 +143,7 @@ __device__ __forceinline__ i32x8 join_chunks(u32x4 lo, u32x4 hi) {
 struct Fragments32 {
   uint32_t first;  // half 0's first chunk: the others' places differ in two bits
   __device__ __forceinline__ void init(int row0, int lane) {
-    first = (uint32_t)((row0 + (lane & 31)) * kStageBytes + ((lane >> 5) ^ (lane & 7)) * 16);
+    first = (uint32_t)((row0 + (lane & 31)) * kStageBytes + ((lane >> 5) ^ code_swizzle<32>(lane & 31)) * 16);
   }
   __device__ __forceinline__ i32x8 read(const char* lds, int f, int kk) const {
     const char* const p = lds + f * 32 * kStageBytes;
@@ -146,10 +157,11 @@ __device__ __forceinline__ void recompute(uint32_t& v) { asm volatile("" : "+v"(
 
 // Zeros in place of what follows the last `left` bytes of k in a stage's rows (left % 16 != 0; whole chunks past the
 // end are zeros already): what lies behind a row's end may be anything.
+template <int FRAGMENT>
 __device__ __forceinline__ void cut_stage(char* lds, int rows, int left, int thread, int threads) {
   const int c = left / 16, keep = left % 16;
   for (int r = thread; r < rows; r += threads) {
-    u32x4* const p = reinterpret_cast<u32x4*>(lds + r * kStageBytes + (c ^ (r & 7)) * 16);
+    u32x4* const p = reinterpret_cast<u32x4*>(lds + r * kStageBytes + (c ^ code_swizzle<FRAGMENT>(r)) * 16);
     u32x4 v = *p;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
@@ -192,8 +204,8 @@ __device__ __forceinline__ void linear_fp8_tile(const Gemm8Args& args, int id) {
   constexpr int WAVES = WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32;
   constexpr int BK = kStageBytes, STAGE = Tile::STAGE;
   constexpr bool STREAM = FM >= 4 && !WIDE;  // fragments of A one at a time: two halves of a stage take too many registers
-  using OpA = CodeOperand<BM, WAVES, KG>;
-  using OpB = CodeOperand<BN, WAVES, KG>;
+  using OpA = CodeOperand<BM, WAVES, 32, KG>;
+  using OpB = CodeOperand<BN, WAVES, 32, KG>;
   extern __shared__ __attribute__((aligned(1024))) char linear_lds[];
   const int lane = threadIdx.x & 63, any_wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
   const int kg = any_wave / WAVES, wave = any_wave % WAVES;
@@ -335,8 +347,8 @@ __device__ __forceinline__ void linear_fp8_tile(const Gemm8Args& args, int id) {
   const int tail = (int)((k1 - k0) % BK);
   const auto cut = [&](int slot) {
     if (tail % 16 == 0) return;
-    cut_stage(linear_lds + (slot * KG + (stages - 1) % KG) * STAGE, BM + BN, tail, (int)threadIdx.x,
-              Tile::THREADS);  // (BM is a multiple of eight rows)
+    cut_stage<32>(linear_lds + (slot * KG + (stages - 1) % KG) * STAGE, BM + BN, tail, (int)threadIdx.x,
+                  Tile::THREADS);  // (BM is a multiple of 16 rows)
     reads_wait();
     wave_barrier();
   };
@@ -656,8 +668,8 @@ __global__ void __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu
   const int64_t stages = (g.k + BK - 1) / BK, per = (stages + WAVES - 1) / WAVES * BK;
   const int64_t k0 = min(wave * per, g.k), k1 = min(k0 + per, g.k);
 
-  CodeOperand<16 * NT, 1> w;
-  CodeOperand<16 * MT, 1> x;
+  CodeOperand<16 * NT, 1, 16> w;
+  CodeOperand<16 * MT, 1, 16> x;
   w.init(args.b, n0, g.n, k0, k1, 0, lane);
   x.init(args.a, 0, g.m, k0, k1, 0, lane);
   Fragments<ElemCode, 16, false> f;
@@ -716,7 +728,7 @@ __global__ void __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu
     }
     char* const at = mine + slot * STAGE;
     if (t + 1 == steps && tail % 16 != 0) {
-      cut_stage(at, 16 * (MT + NT), tail, lane, 64);
+      cut_stage<16>(at, 16 * (MT + NT), tail, lane, 64);
       reads_wait();
     }
     i32x8 vw[NT], vx[MT];
