@@ -7,7 +7,12 @@
 // A workgroup of 512 threads holds a tile of 128 x 128 values in registers, four rows by eight columns to a thread.  A
 // block along the row is 16 lanes (a DPP row).  A block along the column is the 32 threads with the same columns: four in
 // a wave, reached by lane swaps, and by LDS from wave to wave; its codes are turned in LDS so that they leave in
-// whole cache lines too.
+// whole cache lines too.  The conversion instructions divide by the power of two themselves.
+//
+// Bound by HBM where the matrix is large: 8192 x 4096 bf16 16.7 us by rows (6.0 TB/s, part of it from the Infinity Cache),
+// 23.4 both ways (with 256 threads of eight rows each, shuffles through LDS and eight-byte stores down the columns 37.4).
+// dz = dy gelu'(z) of 8192 x 8192 both ways with its sums: 92 us (346 MB), of which the slope's arithmetic is a fifth.  A
+// small matrix takes the time of one tile on one CU, 4 us.  Back: 16.5 us for 8192 x 4096 bf16 (103 MB).
 #include <hip/hip_runtime.h>
 
 #include "fp8_device.hpp"

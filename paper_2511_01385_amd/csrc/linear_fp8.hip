@@ -15,17 +15,22 @@ namespace rdfft {
 constexpr int64_t kCUs = 256;
 constexpr int64_t kStage = 128;  // k to a stage
 
-// What a tile costs, in us: a stage where a CU has one workgroup of them, a stage of each where it has more
-// (`together` fit), and what comes before and after.
+// What a tile costs, in us, fitted to products of 100 to 8192: a stage where a CU has one workgroup of them, a stage of
+// each where it has more (`together` fit), and what comes before and after.  The largest tile is the fastest where its tiles
+// fill the chip in whole rounds; the smaller ones leave fewer CUs idle; groups of waves with stages of their own
+// shorten the way through k where a CU has one workgroup.  In the call (us): 8192 x 8192 -> 4096 199 in 256, 220 in 128 x 256,
+// 240 in 128; 2045 x 4096 -> 4096 34 in 128 x 256, 36 in 128; 1021 x 4096 -> 4096 22.8 in 128 of two groups, 25.9 in 128, 23.4 in
+// 64 x 128; 300 x 4096 -> 4096 13.2 in 64 x 128 of two groups, 14.3 of one; 128 x 4096 -> 4096 8.6 in 32 x 64 of four groups, 10.6
+// of one; 4093 x 768 -> 768 9.0 in 64, 13.0 in 32 x 64.  float32 results: 4096 x 2048 -> 2048 56 in 64 x 128, 63 in 64.
 struct TileCost {
   int bm, bn, together;
   double alone, each, ends;
 };
-constexpr TileCost kCost16[kLinear8Tiles] = {{32, 64, 4, 0.20, 0.155, 1.6}, {64, 64, 3, 0.21, 0.205, 1.8},
-                                             {64, 128, 2, 0.29, 0.33, 2.5}, {32, 64, 1, 0.125, 0.20, 2.0},
-                                             {64, 128, 1, 0.25, 0.36, 2.8}, {128, 128, 2, 0.62, 0.49, 3.5},
-                                             {128, 128, 1, 0.52, 0.60, 3.8}, {128, 256, 1, 0.80, 0.80, 4.9},
-                                             {256, 256, 1, 1.46, 1.46, 7.2}};
+constexpr TileCost kCost16[kLinear8Tiles] = {{32, 64, 4, 0.20, 0.13, 1.6},   {64, 64, 3, 0.205, 0.18, 1.8},
+                                             {64, 128, 2, 0.26, 0.29, 2.5},  {32, 64, 1, 0.12, 0.19, 2.0},
+                                             {64, 128, 1, 0.235, 0.35, 2.8}, {128, 128, 2, 0.60, 0.48, 3.5},
+                                             {128, 128, 1, 0.50, 0.58, 3.8}, {128, 256, 1, 0.77, 0.77, 4.9},
+                                             {256, 256, 1, 1.42, 1.42, 7.2}};
 // float32 results
 constexpr TileCost kCost32[] = {{32, 64, 4, 0.50, 0.31, 2.0}, {64, 64, 3, 0.60, 0.45, 2.0}, {64, 128, 2, 0.85, 0.80, 2.5},
                                 {32, 64, 1, 0.22, 0.50, 2.5}, {64, 128, 1, 0.78, 0.85, 3.0}};
@@ -83,6 +88,8 @@ static int64_t split_bytes(int64_t m, int64_t n, int64_t k, int storage) {
 // Which tile two products share in one launch, the first one's k being the longer, or kLinear8Tiles where two launches
 // cost less.  Where the first has a workgroup for every CU the rounds are simply full; where it has fewer, its CUs deal
 // part of their time to the second's tiles until those run out, and finish alone.  4 us: the launch that is saved.
+// One launch and two, with the pass that quantizes dz (us, tokens x d_in x d_out): 1000 x 768 x 768 14.0 and 17.6, 4093 x 768 x
+// 768 26 and 32, 2045 x 2048 x 2048 34 and 42; two stay for 30 x 4096 x 4096 (25.8, one 26.9) and 16384 x 512 x 512.
 static Linear8Tile together_of(const GemmArgs& first, const GemmArgs& second, int storage) {
   const double k1 = (double)((first.k + kStage - 1) / kStage), k2 = (double)((second.k + kStage - 1) / kStage);
   // (the few rows' kernel: B's bytes at the rate of memory, 3 us before and after)
