@@ -97,6 +97,13 @@ def random_operand(rows, n, seed, tiles=False, pad=0, spread=3):
 UNIT = {"f32": 2.0**-24, "bf16": 2.0**-8, "f16": 2.0**-11}
 
 
+def matmul64(a: np.ndarray, b: np.ndarray) -> np.ndarray:
+    """a b^T in float64."""
+    if a.shape[0] * b.shape[0] * a.shape[1] < 1 << 24 or not torch.cuda.is_available():
+        return a @ b.T
+    return (torch.from_numpy(a).cuda() @ torch.from_numpy(np.ascontiguousarray(b.T)).cuda()).cpu().numpy()
+
+
 def product_error(got: np.ndarray, a: np.ndarray, b: np.ndarray, dtype: str, more=0.0, slope=1.0, what=""):
     """Checks got against (a b^T, or `more`'s function of it), a (m, k) and b (n, k) being what the operands stand for.
 
@@ -106,10 +113,10 @@ def product_error(got: np.ndarray, a: np.ndarray, b: np.ndarray, dtype: str, mor
     difference a function of the product passes on.  float32 results: 2^-24 for every addition, in runs of k, taken as random:
     2^-22 sqrt(k) of the products' 2-norm at most.  A rounding to the type: UNIT of the value, 0.6 of that over all.
     """
-    z = a @ b.T
+    z = matmul64(a, b)
     want = more(z) if callable(more) else z + more
     k = a.shape[1]
-    size = np.sqrt((a * a) @ (b * b).T)
+    size = np.sqrt(matmul64(a * a, b * b))
     drop = 2.0**-22 * np.sqrt(max(k, 1)) if dtype == "f32" else 2.0**-10 * np.sqrt(-(-k // 64))
     tiny = 2.0**-25 if dtype == "f16" else 0.0  # (half a step of float16's smallest numbers)
     bound = UNIT[dtype] * np.abs(want) * 1.01 + slope * drop * size + 2.0**-22 * np.abs(want) + tiny

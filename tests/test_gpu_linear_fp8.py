@@ -17,8 +17,8 @@ def normal(rows, n, seed, dtype, wider=0):
     return torch.randn(rows, n + wider, generator=g, device="cuda").to(TYPES[dtype])[:, :n]
 
 
-def forward(tokens, d_in, d_out, dtype, tiles=True, pad=0, seed=0):
-    x, w = random_operand(tokens, d_in, seed, pad=pad), random_operand(d_out, d_in, seed + 1, tiles, pad)
+def forward(tokens, d_in, d_out, dtype, tiles=True, pad=0, seed=0, spread=3):
+    x, w = random_operand(tokens, d_in, seed, pad=pad, spread=spread), random_operand(d_out, d_in, seed + 1, tiles, pad, spread)
     y = torch.full((tokens, d_out + 3 * pad), 5.0, dtype=TYPES[dtype], device="cuda")
     api.linear_fp8_forward(x, w, y[:, :d_out])
     product_error(f64(y[:, :d_out]), value(x), value(w), dtype, what=f"{dtype} {tokens} {d_in}->{d_out}")
@@ -46,6 +46,25 @@ def test_tiles(dtype, tokens, d_in, d_out):
 @pytest.mark.parametrize("tokens,d_in,d_out", [(4096, 384, 4096), (4096 + 77, 1000, 4096 + 130), (2500, 700, 8192), (8192, 129, 2048)])
 def test_largest_tiles(tokens, d_in, d_out):
     forward(tokens, d_in, d_out, "bf16", pad=1)
+
+
+# sizes that every tile, with its k whole or split, is the cheapest for in one type or another; rows, columns, chunks and stages
+# that are cut, enough stages for the loop's steady part, and some without a cut
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens,d_in,d_out", [(2045, 1001, 5000), (600, 2049, 5000), (600, 2048, 5000), (2560, 1001, 2050),
+                                               (2560, 1024, 2048), (2045, 1291, 4100), (4096, 2048, 4096), (3000, 1001, 129),
+                                               (3000, 3001, 129), (1300, 1001, 777), (1300, 2049, 777), (1300, 1291, 777),
+                                               (257, 6000, 129), (130, 6000, 129), (600, 1001, 5000), (130, 6000, 4100),
+                                               (1000, 4097, 520)])
+def test_every_tile(dtype, tokens, d_in, d_out):
+    forward(tokens, d_in, d_out, dtype, tiles=d_in % 2 == 0, pad=d_in % 3, spread=1)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens,d_in,d_out", [(700, 3000, 770), (100, 3000, 1000), (300, 3000, 770), (100, 100, 129),
+                                               (100, 100, 3000), (45, 1030, 700)])
+def test_gradients_in_one_launch_and_two(dtype, tokens, d_in, d_out):
+    backward(tokens, d_in, d_out, dtype, add=True)
 
 
 @pytest.mark.parametrize("dtype", TYPES)
