@@ -23,17 +23,18 @@ constexpr int64_t kStage = 128;  // k to a stage
 // 64 x 128; 300 x 4096 -> 4096 13.2 in 64 x 128 of two groups, 14.3 of one; 128 x 4096 -> 4096 8.6 in 32 x 64 of four groups, 10.6
 // of one; 4093 x 768 -> 768 9.0 in 64, 13.0 in 32 x 64.  float32 results: 4096 x 2048 -> 2048 56 in 64 x 128, 63 in 64.
 struct TileCost {
-  int bm, bn, together;
+  int log_m, log_n, together;
   double alone, each, ends;
+  int bm = 1 << log_m, bn = 1 << log_n;
 };
-constexpr TileCost kCost16[kLinear8Tiles] = {{32, 64, 4, 0.20, 0.13, 1.6},   {64, 64, 3, 0.205, 0.18, 1.8},
-                                             {64, 128, 2, 0.26, 0.29, 2.5},  {32, 64, 1, 0.12, 0.19, 2.0},
-                                             {64, 128, 1, 0.235, 0.35, 2.8}, {128, 128, 2, 0.60, 0.48, 3.5},
-                                             {128, 128, 1, 0.50, 0.58, 3.8}, {128, 256, 1, 0.77, 0.77, 4.9},
-                                             {256, 256, 1, 1.42, 1.42, 7.2}};
+constexpr TileCost kCost16[kLinear8Tiles] = {{5, 6, 4, 0.20, 0.13, 1.6},   {6, 6, 3, 0.205, 0.18, 1.8},
+                                             {6, 7, 2, 0.26, 0.29, 2.5},  {5, 6, 1, 0.12, 0.19, 2.0},
+                                             {6, 7, 1, 0.235, 0.35, 2.8}, {7, 7, 2, 0.60, 0.48, 3.5},
+                                             {7, 7, 1, 0.50, 0.58, 3.8}, {7, 8, 1, 0.77, 0.77, 4.9},
+                                             {8, 8, 1, 1.42, 1.42, 7.2}};
 // float32 results
-constexpr TileCost kCost32[] = {{32, 64, 4, 0.50, 0.31, 2.0}, {64, 64, 3, 0.60, 0.45, 2.0}, {64, 128, 2, 0.85, 0.80, 2.5},
-                                {32, 64, 1, 0.22, 0.50, 2.5}, {64, 128, 1, 0.78, 0.85, 3.0}};
+constexpr TileCost kCost32[] = {{5, 6, 4, 0.50, 0.31, 2.0}, {6, 6, 3, 0.60, 0.45, 2.0}, {6, 7, 2, 0.85, 0.80, 2.5},
+                                {5, 6, 1, 0.22, 0.50, 2.5}, {6, 7, 1, 0.78, 0.85, 3.0}};
 static const TileCost* costs_of(int storage) { return storage == kStorageF32 ? kCost32 : kCost16; }
 
 static const Linear8Table& table_of(int storage) {
@@ -50,34 +51,44 @@ struct Plan {
 // The tile and the number of k ranges that cost least.  The join of s ranges costs a launch (4 us) and 8 s bytes a
 // result, at 4 TB/s; a product that takes less than that whole is not looked at in ranges.
 static Plan plan_of(int64_t m, int64_t n, int64_t k, int storage) {
-  const int64_t stages = std::max<int64_t>(1, (k + kStage - 1) / kStage);
+  // (a call works this out several times over, for the workspace's size too: 32 bits, which the sizes fit, and no
+  // divisions that the host would wait for)
+  const int stages = std::max(1, (int)((k + kStage - 1) / kStage)), cus = (int)kCUs;
   const Linear8Table& table = table_of(storage);
   const TileCost* const costs = costs_of(storage);
-  Plan best{kTile8_64, 1, stages * kStage, 0};
-  const auto look = [&](int t, int64_t tiles, int64_t splits, int64_t each) {
+  const double join = 8.0 * (double)m * (double)n / 4e6;
+  Linear8Tile tile = kLinear8Tiles;
+  int best_splits = 1, best_each = stages;
+  double least = 0;
+  const auto look = [&](int t, int tiles, int splits, int each) {
     const TileCost& c = costs[t];
-    const int64_t per_cu = std::max<int64_t>(1, (tiles * splits + kCUs - 1) / kCUs);
-    const double stage = per_cu == 1 ? c.alone : c.each * (double)per_cu;
-    double cost = (double)each * stage + c.ends * (double)((per_cu + c.together - 1) / c.together);
-    if (splits > 1) cost += 4.0 + 8.0 * (double)splits * (double)m * (double)n / 4e6;
-    if (best.cost == 0 || cost < best.cost) best = {(Linear8Tile)t, splits, each * kStage, cost};
+    const int per_cu = std::max(1, (tiles * splits + cus - 1) / cus);
+    const int rounds = (int)(((double)per_cu + c.together - 1) / c.together);
+    const double stage = per_cu == 1 ? c.alone : c.each * per_cu;
+    double cost = each * stage + c.ends * rounds;
+    if (splits > 1) cost += 4.0 + join * splits;
+    if (tile == kLinear8Tiles || cost < least) {
+      tile = (Linear8Tile)t;
+      best_splits = splits;
+      best_each = each;
+      least = cost;
+    }
   };
-  int64_t tiles[kLinear8Tiles];
+  int tiles[kLinear8Tiles];
   for (int t = 0; t < kLinear8Tiles; ++t) {
     if (table.fn[t] == nullptr) continue;  // (not built)
-    tiles[t] = ((m + costs[t].bm - 1) / costs[t].bm) * ((n + costs[t].bn - 1) / costs[t].bn);
+    tiles[t] = (int)((uint32_t)(m + costs[t].bm - 1) >> costs[t].log_m) * (int)((uint32_t)(n + costs[t].bn - 1) >> costs[t].log_n);
     look(t, tiles[t], 1, stages);
   }
   for (int t = 0; t < kLinear8Tiles; ++t) {
     if (table.fn[t] == nullptr) continue;
-    for (int64_t want = 2; want <= 16; ++want) {
-      const int64_t each = (stages + want - 1) / want, splits = (stages + each - 1) / each;
-      if (each < 2 || tiles[t] * want > 4 * kCUs) break;
-      if (4.0 + costs[t].ends + 8.0 * (double)want * (double)m * (double)n / 4e6 >= best.cost) break;
+    for (int want = 2; want <= 16; ++want) {
+      if (tiles[t] * want > 4 * cus || stages < 2 * want || 4.0 + costs[t].ends + join * want >= least) break;
+      const int each = (stages + want - 1) / want, splits = (stages + each - 1) / each;
       if (splits == want) look(t, tiles[t], splits, each);  // (else as many ranges of another length)
     }
   }
-  return best;
+  return {tile, best_splits, best_each * kStage, least};
 }
 static int64_t split_bytes(int64_t m, int64_t n, int64_t k, int storage) {
   if (m <= kFewTokens) return 0;
@@ -124,8 +135,9 @@ static hipError_t product(Gemm8Args& args, int storage, void* workspace, hipStre
   const Linear8Table& t = table_of(storage);
   g.splits = 1;
   if (g.m <= kFewTokens) {
-    // 32 rows of B to a workgroup where that still fills the chip, or a checkpoint's blocks ask for it
-    const bool wide = g.ck.codes != nullptr || g.n >= 32 * kCUs;
+    // 32 rows of B to a workgroup where 16 make more workgroups than CUs (one row of 4096 -> 6144 4.8 us, else 5.7; 64 rows of
+    // 2048 -> 6144 5.2, else 8.1; one row of 4096 -> 4096 4.8, with 16 4.5), or a checkpoint's blocks ask for it
+    const bool wide = g.ck.codes != nullptr || g.n > 16 * kCUs;
     return t.few[g.m <= 16 ? 0 : g.m <= 32 ? 1 : 2][wide](args, stream);
   }
   const Plan p = plan_of(g.m, g.n, g.k, storage);
