@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from paper_2511_01385_amd import api
-from tests._fp8 import TYPES, UNIT, decode, encode, f64, product_error, random_operand, value
+from tests._fp8 import TYPES, UNIT, decode, encode, f64, matmul64, product_error, random_operand, value
 
 pytestmark = pytest.mark.gpu
 
@@ -89,6 +89,27 @@ def test_epilogue(dtype, tokens, act):
     same = r.clone()
     api.linear_fp8_forward(x, w, same, bias=bias, activation=act, residual=same)
     assert torch.equal(same, y)
+
+
+# a bias, an activation, its checkpoint and a residual in place, rows of which are wider, on the large tiles (cut and whole) and
+# on products whose k is split
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens,d_in,d_out", [(4096 + 77, 290, 4096 + 130), (4096, 2048, 4096), (2045, 1001, 5000), (600, 2049, 5000),
+                                               (1300, 1291, 777), (257, 6000, 129), (130, 6000, 4100), (64, 17025, 40), (1, 300, 8200)])
+def test_epilogue_of_every_tile(dtype, tokens, d_in, d_out):
+    x, w = random_operand(tokens, d_in, 1, spread=0), random_operand(d_out, d_in, 2, True, spread=0)
+    bias, y = normal(1, d_out, 3, dtype)[0], normal(tokens, d_out, 4, dtype, 5)
+    behind = y.as_strided((tokens, 5), (d_out + 5, 1), d_out)
+    kept, r, held = behind.clone(), f64(y), api.checkpoint_like(y)
+    api.linear_fp8_forward(x, w, y, bias=bias, activation="silu", residual=y, checkpoint=held)
+    a, b = value(x), value(w)
+    silu = lambda z: z * 0.5 * (1 + np.tanh(z / 2))
+    product_error(f64(y), a, b, dtype, lambda z: silu(z + f64(bias)) + r, 1.13, what=f"{dtype} {tokens} {d_in}->{d_out}")
+    assert torch.equal(behind, kept)
+    z, size = matmul64(a, b) + f64(bias), np.sqrt(matmul64(a * a, b * b))
+    step = np.exp2(f64(held[1]) - 127).repeat(32, axis=1)[:, :d_out]
+    # half a step, and what the product itself may be off by (no more than 2^-10 of an instruction's 64 products)
+    assert (np.abs(f64(held[0]) * step - z) <= 0.5 * step + 2.0**-10 * np.sqrt(-(-d_in // 64)) * size).all()
 
 
 def test_row_scales_of_both_operands_and_their_extremes():
@@ -193,6 +214,50 @@ def test_gradients(dtype, tokens, d_in, d_out):
 def test_gradients_through_activations(act, tokens, d_in, d_out):
     for dtype in ("bf16", "f16"):
         backward(tokens, d_in, d_out, dtype, act, add=True)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens,d_in,d_out", [(1, 64, 130), (45, 1030, 700), (257, 640, 385), (700, 2100, 770), (2045, 1024, 1001),
+                                               (4096, 300, 2050)])
+def test_gradients_in_wider_rows_and_in_place(dtype, tokens, d_in, d_out):
+    """dx over its add and dw in wider rows, at odd distances: the same bits as apart, and nothing behind the rows."""
+    dy = normal(tokens, d_out, 1, dtype, 3)
+    x, w = random_operand(d_in, tokens, 2, pad=1), random_operand(d_in, d_out, 3, True, pad=1)
+    z = normal(tokens, d_out, 4, "f32")
+    ck = api.act8_quantize(z, *api.checkpoint_like(z))
+    add = normal(tokens, d_in, 5, dtype)
+    T = TYPES[dtype]
+    plain = api.linear_fp8_backward(dy, x, w, dx=torch.empty(tokens, d_in, dtype=T, device="cuda"),
+                                    dw=torch.empty(d_out, d_in, dtype=T, device="cuda"),
+                                    db=torch.empty(d_out, dtype=T, device="cuda"), activation="silu", checkpoint=ck, add=add)
+    dz = f64(dy) * SLOPES["silu"](f64(api.act8_dequantize(*ck, torch.empty_like(z))))
+    for got, of, other, more in ((plain[0], dz, w, f64(add)), (plain[1], dz.T, x, 0.0)):
+        a, b = decode(*encode(of)), value(other)
+        check(f64(got), a, b, dtype, 0.25 * np.abs(a).max() * np.abs(b).max(), more, f"{dtype} {tokens} {d_in}->{d_out}")
+    wide = torch.full((tokens, d_in + 3), 7.0, dtype=T, device="cuda"), torch.full((d_out, d_in + 5), 7.0, dtype=T, device="cuda")
+    dx, dw = (t[:, :d_in] for t in wide)
+    dx.copy_(add)
+    db = torch.empty(d_out, dtype=T, device="cuda")
+    api.linear_fp8_backward(dy, x, w, dx=dx, dw=dw, db=db, activation="silu", checkpoint=ck, add=dx)
+    assert all(torch.equal(a, b) for a, b in zip((dx, dw, db), plain))
+    assert all((t[:, d_in:] == 7).all() for t in wide)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+@pytest.mark.parametrize("tokens", [6, 200, 1100])
+def test_a_gradient_that_is_not_finite_stays_in_its_row_and_column(dtype, bad, tokens):
+    d_in, d_out = 260, 300
+    dy = normal(tokens, d_out, 1, dtype)
+    dy[5, 7] = bad
+    x, w = random_operand(d_in, tokens, 2, spread=0), random_operand(d_in, d_out, 3, True, spread=0)
+    T = TYPES[dtype]
+    dx, dw, db = api.linear_fp8_backward(dy, x, w, dx=torch.empty(tokens, d_in, dtype=T, device="cuda"),
+                                         dw=torch.empty(d_out, d_in, dtype=T, device="cuda"),
+                                         db=torch.empty(d_out, dtype=T, device="cuda"))
+    for t, row in ((dx, 5), (dw, 7)):
+        assert t[row].isnan().all() and t.isnan().sum() == d_in
+    assert not db[7].isfinite() and db.isfinite().sum() == d_out - 1
 
 
 @pytest.mark.parametrize("wanted", ["dx", "dw", "db", "dx dw", "dx db", "dw db"])
