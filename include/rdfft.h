@@ -426,7 +426,8 @@ RDFFT_API int fp8_dequantize(const fp8_t *from, void *out, int64_t ldo, int64_t 
  *              Either may be null.
  *   summed     u, written; may be null.
  *   y, summed  may be x or residual (same pointer and stride), but not each other.
- *   rstd       float32 [rows], written; may be null.
+ *   rstd       float32 [rows], written; may be null.  (With an eps of 0, infinite where it is 2^128 or more; y and y8 are
+ *              right there all the same.)
  *   checkpoint of u, written; codes null: none.
  *   eps        >= 0.
  */
@@ -452,7 +453,7 @@ RDFFT_API int rms_norm_forward(const rms_norm_forward_t *a, int64_t rows, int64_
  *   dx = rstd * (g - xh * mean(g * xh)) (+ add), the gradient of x and of residual,
  *   dweight = sum over rows of dy * xh  (float32 [n], overwritten; may be null).
  *   u          the norm's input, or with u null what the checkpoint stands for.
- *   rstd       as rms_norm_forward left it.
+ *   rstd       as rms_norm_forward left it; where it is infinite dx and dweight are not finite.
  *   add        the gradient that reaches the sum another way (the residual stream); may be null.
  *   dx         may be dy or add itself (same pointer and stride).
  * rows == 0 writes zeros into dweight.

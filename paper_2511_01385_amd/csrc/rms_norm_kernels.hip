@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(rms_fwd_wg<TPR>()) rms_norm_forward_kernel(Rms
       for (int k = 0; k < kVec; ++k) s[0] = fmaf(u[c][k], u[c][k], s[0]);
     group_sums<TPR, 1>(s, red, turn);
     // squares that leave float32's range are taken of the values times a power of two (the sum is the same in all
-    // threads; a row with an infinity ends up as NaN in any case)
+    // threads; with an infinity among them it is infinite again: the infinity becomes NaN, the row's other values 0)
     if (!(s[0] <= 0x1.fffffep127f) || (s[0] < 0x1p-80f && a.eps < 0x1p-100f)) {
       unit = s[0] < 1.f ? 0x1p100f : 0x1p-80f;
       s[0] = 0.f;
@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(rms_fwd_wg<TPR>()) rms_norm_forward_kernel(Rms
         for (int k = 0; k < kVec; ++k) s[0] = fmaf(u[c][k] * unit, u[c][k] * unit, s[0]);
       group_sums<TPR, 1>(s, red, turn);
     }
-    const float rstd = unit / sqrtf(s[0] / count + a.eps * unit * unit);
+    const float root = sqrtf(s[0] / count + a.eps * unit * unit), rstd = unit / root;
     if (lane == 0 && a.rstd != nullptr) a.rstd[row] = rstd;
     if (a.summed != nullptr) {
       T* const h = static_cast<T*>(a.summed) + row * a.lds;
@@ -114,10 +114,18 @@ __global__ void __launch_bounds__(rms_fwd_wg<TPR>()) rms_norm_forward_kernel(Rms
 #pragma unroll
       for (int c = 0; c < C; ++c) write_checkpoint(a.ck.codes + row * n, a.ck.scales + row * blocks, at[c], n, u[c]);
     }
+    float times = rstd;
+    if (unit > 1.f) {  // rstd may be past the largest number; values as small can be scaled without loss
+      times = 1.f / root;
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int k = 0; k < kVec; ++k) u[c][k] *= unit;
+    }
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-      for (int k = 0; k < kVec; ++k) u[c][k] = u[c][k] * rstd * w[c][k];
+      for (int k = 0; k < kVec; ++k) u[c][k] = u[c][k] * times * w[c][k];
     if (a.y != nullptr) {
       T* const y = static_cast<T*>(a.y) + row * a.ldy;
 #pragma unroll
