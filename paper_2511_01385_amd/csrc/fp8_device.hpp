@@ -65,7 +65,8 @@ __device__ __forceinline__ Bytes8 fp8_encode(const float* v, int s) {
 }
 
 // Eight values.  Of a value within 1/32 of the type's largest number M the code can stand for the power of two past M: it
-// stands for +-M, so what was finite comes back finite (Elem*::kMost, kPast).
+// stands for +-M, so what was finite comes back finite (Elem*::kMost, kPast).  2^128 is code 256 of byte 247, which is what
+// quantize leaves, and as well 128 of byte 248 and so on.
 template <class E>
 __device__ __forceinline__ void fp8_decode(const Bytes8& r, int s, float* v) {
   typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -83,7 +84,8 @@ __device__ __forceinline__ void fp8_decode(const Bytes8& r, int s, float* v) {
     const float code = v[i];
     v[i] = code * scale;
     if (E::kId == ElemF16::kId) v[i] = fabsf(v[i]) == 65536.f ? copysignf(E::kMost, v[i]) : v[i];
-    else if (s == 247) v[i] = fabsf(code) == 256.f ? copysignf(E::kMost, code) : v[i];
+    else if (s >= 247 && s != kCkNaN)
+      v[i] = fabsf(code) == __uint_as_float((uint32_t)(127 + 255 - s) << 23) ? copysignf(E::kMost, code) : v[i];
   }
 }
 
