@@ -139,9 +139,15 @@ __global__ void __launch_bounds__(rms_fwd_wg<TPR>()) rms_norm_forward_kernel(Rms
 }
 
 constexpr int kRmsBwdWG = 1024;
+// Groups that take a row each.  (With more threads to a row than a workgroup has there would be none, and no end to the rows.)
+template <int TPR>
+constexpr int rms_bwd_groups() {
+  static_assert(kRmsBwdWG % TPR == 0, "a workgroup holds whole rows");
+  return kRmsBwdWG / TPR;
+}
 template <int TPR, int C>
 constexpr int rms_bwd_lds() {
-  const int groups = kRmsBwdWG / TPR;
+  constexpr int groups = rms_bwd_groups<TPR>();
   return groups == 1 ? 0 : groups * TPR * C * kVec * 4;
 }
 
@@ -191,7 +197,7 @@ struct RmsRow {
 template <class E, int TPR, int C, bool CK, RowsOf ROWS>
 __global__ void __launch_bounds__(kRmsBwdWG) rms_norm_backward_kernel(RmsGradArgs a, float* dw_out) {
   using T = typename E::T;
-  constexpr int WG = kRmsBwdWG, GROUPS = WG / TPR;
+  constexpr int WG = kRmsBwdWG, GROUPS = rms_bwd_groups<TPR>();
   __shared__ float red[2 * (WG / 64)];
   int turn = 0;
   const int lane = threadIdx.x % TPR, grp = __builtin_amdgcn_readfirstlane((int)threadIdx.x / TPR);  // (one in a wave)
@@ -332,7 +338,7 @@ constexpr int64_t kRmsMaxPartials = 256;
 int64_t rms_partials(int64_t rows, int64_t n) {
   int64_t groups = 1;
   (void)with_row_backward(n, [&](auto tpr, auto) {
-    groups = kRmsBwdWG / decltype(tpr)::value;
+    groups = rms_bwd_groups<decltype(tpr)::value>();
     return hipSuccess;
   });
   return rows <= 2 * groups ? 1 : std::min((rows + groups - 1) / groups, kRmsMaxPartials);
