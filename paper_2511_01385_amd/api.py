@@ -612,7 +612,8 @@ def fp8_quantize(x: torch.Tensor, held=None, *, columns=None):
 
 
 def fp8_dequantize(held, out: torch.Tensor) -> torch.Tensor:
-    """What (codes, scales) in 8-bit floating point stand for, in ``out``'s type (exact in float32 and bfloat16)."""
+    """What (codes, scales) in 8-bit floating point stand for, in ``out``'s type: exact in float32, and in bfloat16 but for the
+    smallest codes of the smallest scales, which need bits below its 2^-133."""
     status = None
     if out.is_cuda:
         device = _current_device()
