@@ -485,8 +485,9 @@ RDFFT_API int rms_norm_backward(const rms_norm_backward_t *a, int64_t rows, int6
  *   bias [d_out], residual [tokens][d_out] (null: none) and y [tokens][d_out] in dtype; y may be residual itself.
  *   checkpoint of z (of its float32 value), written, for linear_fp8_backward; codes null: none.
  * Sums are float32.  For a 16-bit dtype the 8-bit matrix instructions drop what lies about 16 bits below the largest product
- * that they add (1.5e-5 of the result's norm for normal values); with RDFFT_F32 every product counts in full, at half the
- * rate.  Sizes as for linear_forward; strides at most 2^21.
+ * that they add (1.5e-5 of the result's norm for normal values).  That moves about one code in a thousand of the checkpoint to
+ * the next, and the backward's gradients with it.  With RDFFT_F32 every product counts in full, and a large product takes a
+ * little over three times as long.  Sizes as for linear_forward; strides at most 2^21.
  */
 typedef struct {
   fp8_t x;

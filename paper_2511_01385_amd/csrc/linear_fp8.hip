@@ -103,7 +103,9 @@ static int64_t split_bytes(int64_t m, int64_t n, int64_t k, int storage) {
 // 768 26 and 32, 2045 x 2048 x 2048 34 and 42; two stay for 30 x 4096 x 4096 (25.8, one 26.9) and 16384 x 512 x 512.
 static Linear8Tile together_of(const GemmArgs& first, const GemmArgs& second, int storage) {
   const double k1 = (double)((first.k + kStage - 1) / kStage), k2 = (double)((second.k + kStage - 1) / kStage);
-  // (the few rows' kernel: B's bytes at the rate of memory, 3 us before and after)
+  // (the few rows' kernel: B's bytes at the rate of memory, 3 us before and after.  That holds where its workgroups, one for
+  // 16 or 32 rows of B, are many and k is no longer than a layer is wide; the few of dW with few outputs over many tokens take
+  // longer, 64 x 64 over 16384 17 us where this says 3.2)
   const auto alone = [&](const GemmArgs& g) {
     return g.m <= kFewTokens ? 3.0 + (double)g.n * (double)g.k / 5e6 : plan_of(g.m, g.n, g.k, storage).cost;
   };
@@ -136,7 +138,9 @@ static hipError_t product(Gemm8Args& args, int storage, void* workspace, hipStre
   g.splits = 1;
   if (g.m <= kFewTokens) {
     // 32 rows of B to a workgroup where 16 make more workgroups than CUs (one row of 4096 -> 6144 4.8 us, else 5.7; 64 rows of
-    // 2048 -> 6144 5.2, else 8.1; one row of 4096 -> 4096 4.8, with 16 4.5), or a checkpoint's blocks ask for it
+    // 2048 -> 6144 5.2, else 8.1; one row of 4096 -> 4096 4.8, with 16 4.5), or a checkpoint's blocks ask for it.  (dW of 64
+    // outputs and less comes here too, and does not split k over workgroups: 64 x 64 over 16384 tokens takes 17 us, 72 x 64
+    // in a tile whose k is split 9.3 with its join; 64 x 4096 18, 72 x 4096 23; 64 x 64 over 4096 tokens 6.5, 72 x 64 8.5)
     const bool wide = g.ck.codes != nullptr || g.n > 16 * kCUs;
     return t.few[g.m <= 16 ? 0 : g.m <= 32 ? 1 : 2][wide](args, stream);
   }
